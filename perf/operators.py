@@ -298,6 +298,10 @@ def work(case):
 
 # ---- the definitions in 64 bits
 
+def _pow2(e):
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _exact_mx(x):
     rows, k = x.shape
     full = torch.zeros(rows, -(-k // GROUP) * GROUP, dtype=torch.float64, device=x.device)
@@ -306,7 +310,7 @@ def _exact_mx(x):
     top = g.abs().max(dim=1).values
     # floor(log2) of a positive binary64 is its exponent field
     e = torch.where(top > 0, (top.view(torch.int64) >> 52) - 1023 - 2, -127).clamp(min=-127)
-    unit = ((e + 1023) << 52).view(torch.float64)[:, None]
+    unit = _pow2(e)[:, None]
     a = g.abs() / unit
     index = torch.zeros_like(a, dtype=torch.int64)
     for i in range(7):                  # halves between neighbours; a tie goes to the even code
@@ -320,7 +324,7 @@ def _exact_weights(q, s, k):
     code = torch.empty(q.shape[0], q.shape[1] * 2, dtype=torch.int64, device=q.device)
     code[:, 0::2], code[:, 1::2] = (q % 16).long(), (q // 16).long()
     v = torch.tensor(_E2M1, dtype=torch.float64, device=q.device)[code % 8] * (1 - 2 * (code // 8)).double()
-    return (v * torch.pow(2.0, (s.double() - 127).repeat_interleave(GROUP, dim=1)))[:, :k]
+    return (v * _pow2(s.long() - 127).repeat_interleave(GROUP, dim=1))[:, :k]
 
 
 def _exact_e4m3(x, mode):
@@ -330,11 +334,11 @@ def _exact_e4m3(x, mode):
     top = g.abs().max(dim=1, keepdim=True).values.clamp(min=1e-12)
     scale = top / 448
     if mode == "block_pow2":
-        scale = torch.pow(2.0, torch.ceil(torch.log2(scale)))
+        m, e = torch.frexp(scale)       # the smallest power of two that is not less
+        scale = _pow2(torch.where(m == 0.5, e - 1, e))
     t = g / scale
     # steps of 2^(exponent - 3), none below 2^-9
-    e = ((t.abs().clamp(min=2.0 ** -6).view(torch.int64) >> 52) - 1023 - 3).double()
-    step = torch.pow(2.0, e)
+    step = _pow2((t.abs().clamp(min=2.0 ** -6).view(torch.int64) >> 52) - 1023 - 3)
     v = (torch.round(t / step) * step).clamp(-448, 448)
     return v.reshape(rows, k), scale.reshape(-1) if mode == "row" else scale.reshape(rows, -1)
 
