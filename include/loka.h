@@ -300,6 +300,105 @@ loka_status loka_fp8_linear_norm_xq(const loka_gemm_desc* desc, const void* x_bf
                                     const uint8_t* wq, const float* sw, const void* gamma_bf16, const void* beta_bf16,
                                     void* out_bf16, float* y_fp32, void* hip_stream);
 
+/* ---------------------------------------------------------------- MXFP4: 4-bit codes with a scale per 32 elements
+ * Microscaled 4-bit floating point: groups of 32 consecutive elements of a row share a power-of-two scale, held as its
+ * biased exponent in one byte (E8M0), and every element is an e2m1 code (magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6).  gfx950's
+ * scaled matrix instruction takes both as they lie in memory, at twice the rate of its FP8 form, so a layer that tolerates
+ * the format reads a quarter of the bf16 bytes per weight: the recipe for layers bound by their weights' traffic.
+ *
+ * Stored form of a [rows, cols] operand whose products contract over cols; colsp = cols rounded up to a multiple of 128:
+ *   q       [rows, colsp / 2] bytes; byte i holds element 2i in its low half and 2i + 1 in its high half
+ *   scales  [rows, colsp / 32] bytes; scale = 2^(byte - 127)
+ * Elements past cols are zero codes; a group with nothing but such elements has scale byte 0.
+ *
+ * Per group: amax = max|x|;  e = max(floor(log2(amax)) - 2, -127) (-127 where amax is 0);  byte = e + 127;
+ *   code = e2m1(x / 2^e), rounded to nearest, ties to the even code, magnitudes above 6 to 6, the sign kept (also of zeros).
+ * A group with a NaN or an infinity gets byte 255 and zero codes: all of its values are NaN, and so is every product sum
+ * that it enters.  Bit-exact with this recipe.
+ *
+ *   x_bf16  [rows, ld] bf16, ld >= cols, aligned to 2 bytes (rows that start on multiples of 16 bytes are read in wide loads)
+ *   transpose_out != 0: the operand is the transpose, [cols, rows], whose groups run along the ROWS of x: codes
+ *   [cols, rowsp / 2], scales [cols, rowsp / 32], rowsp = rows up to a multiple of 128.  What weights [K, N] take for the
+ *   forward product, and X and dY for dW = X^T dY.
+ * Any rows >= 1 and cols >= 1 (each at most 2^31 - 1; the stored form may exceed 4 GB).  q 16-byte, scales 4-byte aligned. */
+int64_t loka_mxfp4_padded(int64_t cols);          /* cols up to a multiple of 128; -1 for cols <= 0.  Host only. */
+loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
+                                uint8_t* scales, void* hip_stream);
+/* The values of a stored operand as bf16 [rows, ld], ld >= cols (columns cols .. ld - 1 are left as they are): exact for
+ * every byte that quantization writes (at most 252); values beyond bf16's range, which larger bytes can stand for, are infinite. */
+loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, void* out_bf16,
+                                  int64_t ld, void* hip_stream);
+
+/* Y[m,n] = sum_k x[m,k] w[n,k] over MXFP4 operands, fp32 accumulation on the scaled matrix instruction, for `batch`
+ * problems of one shape.  Of `desc` M, N, K, batch, the strides and norm, act and variant are read; norm must be
+ * LOKA_NORM_NONE, act LOKA_ACT_NONE, variant -1 (LOKA_ERR_UNSUPPORTED otherwise).  Any M, N, K >= 1.
+ *   xq, sx  [batch] stored operands [M, K]; strideX = elements between problems in the stored form, at least
+ *           M * loka_mxfp4_padded(K) and a multiple of 128, or 0 = shared (the scales of
+ *           problem g start at byte g * strideX / 32)
+ *   wq, sw  likewise [N, K] with strideW
+ *   out_bf16 [batch][M, N] bf16 and / or y_fp32 [batch][M, N] fp32, strideO elements apart; at least one is not NULL.
+ *           16-byte aligned; rows are N elements apart, whatever N.
+ * Workspace: loka_mxfp4_gemm_workspace(desc) bytes (partial sums, where a long contraction is split over workgroups
+ * because there are few output tiles; added in a fixed order: results do not change from call to call).  NULL / less: the
+ * product runs unsplit, adding in another order.  16-byte aligned, not shared with a call still running. */
+size_t loka_mxfp4_gemm_workspace(const loka_gemm_desc* desc);
+loka_status loka_mxfp4_gemm(const loka_gemm_desc* desc, const uint8_t* xq, const uint8_t* sx, const uint8_t* wq,
+                            const uint8_t* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
+                            void* hip_stream);
+
+/* A layer with kept 4-bit weights on bf16 activations, for any number of rows: loka_mxfp4_quantize(x) and loka_mxfp4_gemm
+ * in one call, with the same codes.  At most 16 rows (single tokens, small serving batches) are one launch that quantizes
+ * x in the registers of the product kernel; more rows are quantized into the workspace first.
+ *   x_bf16 [M, ld] with ld >= K elements, aligned to 2 bytes; desc->batch must be 1 (LOKA_ERR_UNSUPPORTED); strides are not read.
+ * Workspace: loka_mxfp4_linear_workspace(desc) bytes (0 for at most 16 rows), 16-byte aligned; LOKA_ERR_WORKSPACE when less. */
+size_t loka_mxfp4_linear_workspace(const loka_gemm_desc* desc);
+loka_status loka_mxfp4_linear(const loka_gemm_desc* desc, const void* x_bf16, int64_t ld, const uint8_t* wq,
+                              const uint8_t* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
+                              void* hip_stream);
+
+/* ---------------------------------------------------------------- residual addition + RMSNorm + quantization
+ * The step between two layers of a residual stream, in one pass over it:
+ *   h = x + residual (fp32; the norm sees this sum, h_out its rounding to bf16)
+ *   rstd = 1 / sqrt(mean_j(h_j^2) + eps);   y_j = h_j * rstd * gamma_j
+ * and y leaves in the form in which the next layer takes it:
+ *   LOKA_RMS_OUT_BF16   y_out [rows, cols] bf16
+ *   LOKA_RMS_OUT_E4M3   y_out [rows, cols] codes, y_scales fp32 in out_mode (LOKA_SCALE_ROW, LOKA_SCALE_BLOCK_1x128 or its
+ *                       _POW2 form), by the recipe of loka_quantize applied to the fp32 y: an operand of loka_fp8_gemm_norm
+ *   LOKA_RMS_OUT_MXFP4  y_out, y_scales (bytes) in the stored form above, from the fp32 y: an operand of loka_mxfp4_gemm
+ * For the backward pass the same call leaves an 8-bit checkpoint of h in place of a bf16 copy: hq [rows, cols] e4m3 codes
+ * and hs, their fp32 scales in ckpt_mode (the three modes above), by the recipe of loka_quantize applied to the fp32 h, and
+ * rstd [rows] fp32.  hq and hs both or neither; each of h_out, rstd, residual (h = x) and gamma (1) may be NULL.
+ * A row with a NaN or an infinity: bf16 and MXFP4 values that are NaN by the formula are NaN, and an e4m3 scale group that
+ * holds such a value has a NaN scale.  The sum of squares is held in fp32: it has to stay below 3.4e38.
+ * cols % 16 == 0 and at most 65536; cols % 128 == 0 for the block modes.  ld_x, ld_r (row strides of x and residual, in
+ * elements) multiples of 8 and at least cols; outputs are contiguous.  Pointers 16-byte aligned (scales and rstd: 4).
+ * h_out may be x or residual itself (same row stride); no other outputs may overlap inputs. */
+typedef enum { LOKA_RMS_OUT_BF16 = 0, LOKA_RMS_OUT_E4M3 = 1, LOKA_RMS_OUT_MXFP4 = 2 } loka_rms_out;
+typedef struct {
+    int64_t rows, cols;
+    int64_t ld_x, ld_r;       /* row strides in elements: of x and residual (backward: of dy and dh) */
+    int32_t out;              /* loka_rms_out */
+    int32_t out_mode;         /* loka_scale_mode of y_scales (LOKA_RMS_OUT_E4M3; not read otherwise) */
+    int32_t ckpt_mode;        /* loka_scale_mode of hs (not read where hq is NULL) */
+    float eps;                /* >= 0 */
+} loka_rms_desc;
+loka_status loka_add_rmsnorm(const loka_rms_desc* desc, const void* x_bf16, const void* residual_bf16, const void* gamma_bf16,
+                             void* h_out_bf16, void* y_out, void* y_scales, uint8_t* hq, float* hs, float* rstd,
+                             void* hip_stream);
+
+/* Its backward pass from the 8-bit checkpoint: with h = code * scale and n = h * rstd,
+ *   dx_j = rstd * (dy_j gamma_j - n_j * mean_i(dy_i gamma_i n_i)) + dh_j        (the gradient of x and of residual alike)
+ *   dgamma_j = sum over rows of dy_j n_j
+ * dy bf16 [rows, ld_x]: the gradient of y; dh bf16 [rows, ld_r] or NULL: the gradient that reaches h past the norm; dx bf16
+ * [rows, cols] (required); dgamma fp32 [cols] or NULL.  rows, cols, ld_x, ld_r and ckpt_mode of `desc` are read, under the
+ * rules above.  dx may be dy or dh itself (same row stride).  The codes are e4m3 as hq; hs and rstd as loka_add_rmsnorm wrote them.
+ * Workspace: loka_rmsnorm_backward_workspace(desc) bytes, 16-byte aligned, for dgamma's partial sums (not needed without
+ * dgamma), which are added in a fixed order: results do not change from call to call. */
+size_t loka_rmsnorm_backward_workspace(const loka_rms_desc* desc);
+loka_status loka_rmsnorm_backward(const loka_rms_desc* desc, const void* dy_bf16, const uint8_t* hq, const float* hs,
+                                  const float* rstd, const void* gamma_bf16, const void* dh_bf16, void* dx_bf16,
+                                  float* dgamma, void* workspace, size_t ws_bytes, void* hip_stream);
+
 /* ---------------------------------------------------------------- probe reference
  * Yref = X . W from the UNQUANTIZED bf16 operands with fp32 accumulation: the
  * high-precision reference the probe measures FP8 against (Section 2.3, "Error

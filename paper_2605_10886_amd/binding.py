@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from collections import namedtuple
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
@@ -29,6 +30,7 @@ SCALE_TENSOR, SCALE_ROW, SCALE_COL, SCALE_BLOCK_1x128, SCALE_BLOCK_128x128, SCAL
 NORM_NONE, NORM_LAYERNORM, NORM_RMSNORM, NORM_BLOCKNORM = range(4)
 NORMS = {"none": NORM_NONE, "layernorm": NORM_LAYERNORM, "rmsnorm": NORM_RMSNORM, "blocknorm": NORM_BLOCKNORM}
 ACT_NONE, ACT_HARDSWISH = 0, 1
+RMS_OUT_BF16, RMS_OUT_E4M3, RMS_OUT_MXFP4 = range(3)
 
 
 class GemmDesc(Structure):
@@ -36,6 +38,11 @@ class GemmDesc(Structure):
                 ("strideX", c_int64), ("strideW", c_int64), ("strideO", c_int64),
                 ("x_mode", c_int32), ("w_mode", c_int32), ("norm", c_int32), ("eps", c_float),
                 ("variant", c_int32), ("block_n", c_int32), ("act", c_int32)]
+
+
+class RmsDesc(Structure):
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("ld_x", c_int64), ("ld_r", c_int64),
+                ("out", c_int32), ("out_mode", c_int32), ("ckpt_mode", c_int32), ("eps", c_float)]
 
 
 class ProbeStats(Structure):
@@ -103,6 +110,20 @@ _SIGNATURES = [
                               POINTER(Candidate), c_int, POINTER(c_int), c_void_p]),
     ("loka_dispatch_clear", None, []),
     ("loka_default_variant", c_int, [POINTER(GemmDesc)]),
+    ("loka_mxfp4_padded", c_int64, [c_int64]),
+    ("loka_mxfp4_quantize", c_int, [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
+    ("loka_mxfp4_dequantize", c_int, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_void_p]),
+    ("loka_mxfp4_gemm_workspace", c_size_t, [POINTER(GemmDesc)]),
+    ("loka_mxfp4_gemm", c_int, [POINTER(GemmDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                c_size_t, c_void_p]),
+    ("loka_mxfp4_linear_workspace", c_size_t, [POINTER(GemmDesc)]),
+    ("loka_mxfp4_linear", c_int, [POINTER(GemmDesc), c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                  c_size_t, c_void_p]),
+    ("loka_add_rmsnorm", c_int, [POINTER(RmsDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                 c_void_p, c_void_p, c_void_p]),
+    ("loka_rmsnorm_backward_workspace", c_size_t, [POINTER(RmsDesc)]),
+    ("loka_rmsnorm_backward", c_int, [POINTER(RmsDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_void_p, c_void_p, c_size_t, c_void_p]),
 ]
 EXPORTS = [s[0] for s in _SIGNATURES]
 
@@ -259,6 +280,57 @@ def loka_fp8_gemm_norm_fp8out(desc: GemmDesc, xq, sx, wq, sw, gamma=None, beta=N
                               so=None, y=None, workspace=None):
     """Returns (codes uint8 [batch*M, N], row scales fp32 [batch*M], Y fp32 or None)."""
     return (_native or _host()).gemm_norm_fp8out(desc, xq, sx, wq, sw, gamma, beta, want_y, oq, so, y, workspace)
+
+
+def make_mxfp4_desc(M, N, K, batch=1, shared_w=False) -> GemmDesc:
+    """What loka_mxfp4_gemm and loka_mxfp4_linear take; problems of a batch follow each other in the stored form."""
+    kp = loka_mxfp4_padded(K)
+    return GemmDesc(M, N, K, batch, M * kp, 0 if shared_w else N * kp, M * N, 0, 0, NORM_NONE, 0.0, -1, 0, ACT_NONE)
+
+
+def loka_mxfp4_padded(cols: int) -> int:
+    return int(lib().loka_mxfp4_padded(int(cols)))
+
+
+def loka_mxfp4_quantize(x: torch.Tensor, transpose_out: bool = False):
+    """x bf16 [rows, cols] -> (codes uint8 [rows, colsp / 2], scales uint8 [rows, colsp / 32]), groups of 32 along the row;
+    transpose_out: of the transpose, (codes [cols, rowsp / 2], scales [cols, rowsp / 32]), groups down the columns of x."""
+    return (_native or _host()).mxfp4_quantize(x, transpose_out)
+
+
+def loka_mxfp4_dequantize(q, scales, cols: int, out=None):
+    """The values of stored codes as bf16 [rows, cols]."""
+    return (_native or _host()).mxfp4_dequantize(q, scales, cols, out)
+
+
+def loka_mxfp4_gemm(desc: GemmDesc, xq, sx, wq, sw, want_out: bool = True, want_y: bool = False, out=None, y=None, workspace=None):
+    """X W^T of stored operands [batch, M, K] and [batch, N, K].  Returns (bf16 [batch*M, N] or None, fp32 likewise or None)."""
+    return (_native or _host()).mxfp4_gemm(desc, xq, sx, wq, sw, want_out, want_y, out, y, workspace)
+
+
+def loka_mxfp4_linear(desc: GemmDesc, x, wq, sw, want_out: bool = True, want_y: bool = False, out=None, y=None, workspace=None):
+    """A layer with stored weights [N, K] on bf16 x [M, K], quantized in the call.  Returns (bf16 [M, N] or None, fp32 or None)."""
+    return (_native or _host()).mxfp4_linear(desc, x, wq, sw, want_out, want_y, out, y, workspace)
+
+
+RmsNormOut = namedtuple("RmsNormOut", "h y scales hq hs rstd")
+
+
+def loka_add_rmsnorm(x, residual=None, gamma=None, eps: float = 1e-5, out: int = RMS_OUT_E4M3, out_mode: int = SCALE_ROW,
+                     ckpt_mode=None, want_h=None, want_rstd=None, h_out=None) -> RmsNormOut:
+    """RMSNorm of x + residual.  y: bf16, e4m3 codes or MXFP4 codes, with `scales`; h: the sum in bf16 (by default where there
+    is a residual); hq, hs, rstd: the 8-bit checkpoint of the sum that loka_rmsnorm_backward reads (where ckpt_mode is given).
+    What is not asked for is None."""
+    return RmsNormOut(*(_native or _host()).add_rmsnorm(x, residual, gamma, eps, out, out_mode, ckpt_mode,
+                                                        residual is not None if want_h is None else want_h,
+                                                        ckpt_mode is not None if want_rstd is None else want_rstd, h_out))
+
+
+def loka_rmsnorm_backward(dy, hq, hs, rstd, gamma=None, dh=None, ckpt_mode: int = SCALE_BLOCK_1x128, want_dgamma: bool = True,
+                          dx=None, workspace=None):
+    """The gradient of loka_add_rmsnorm's input from its checkpoint; dh: the gradient that reaches the sum past the norm.
+    Returns (dx bf16 [rows, cols], dgamma fp32 [cols] or None)."""
+    return (_native or _host()).rmsnorm_backward(dy, hq, hs, rstd, gamma, dh, ckpt_mode, want_dgamma, dx, workspace)
 
 
 def loka_bf16_gemm(desc: GemmDesc, x, w, yref=None, workspace=None):

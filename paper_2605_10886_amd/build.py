@@ -20,7 +20,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libloka.so")
 HOST = os.path.join(HERE, "_host.so")
-SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_panel32.hip", "gemm_wreg.hip", "gemm_strip.hip", "probe.hip", "dispatch.hip", "tracker.hip", "ceiling.hip"]
+SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_panel32.hip", "gemm_wreg.hip", "gemm_strip.hip", "probe.hip", "dispatch.hip", "tracker.hip", "ceiling.hip",
+           "mxfp4.hip", "mxfp4_gemm.hip", "rmsnorm.hip"]
 
 # -packed-fp32-ops off: packed fp32 VALU forms are kept out of the generated code.
 # No fast-math: divisions and square roots stay correctly rounded, no FMA contraction

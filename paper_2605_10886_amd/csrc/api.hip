@@ -47,6 +47,21 @@ int default_variant(const loka_gemm_desc*);
 // tracker.hip
 size_t tracker_workspace_bytes(int64_t, int64_t);
 loka_status tracker_update_launch(const void*, int64_t, int64_t, int64_t, int64_t, float*, float*, void*, hipStream_t);
+// mxfp4.hip
+loka_status mxfp4_quantize_launch(const void*, int64_t, int64_t, int64_t, int, uint8_t*, uint8_t*, hipStream_t);
+loka_status mxfp4_dequantize_launch(const uint8_t*, const uint8_t*, int64_t, int64_t, void*, int64_t, hipStream_t);
+// mxfp4_gemm.hip
+size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc*);
+loka_status mxfp4_gemm_launch(const loka_gemm_desc*, const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, void*, float*, void*,
+                              size_t, hipStream_t);
+bool mxfp4_linear_fused(const loka_gemm_desc*);
+loka_status mxfp4_linear_fused_launch(const loka_gemm_desc*, const void*, int64_t, const uint8_t*, const uint8_t*, void*, float*, hipStream_t);
+// rmsnorm.hip
+loka_status add_rmsnorm_launch(const loka_rms_desc*, const void*, const void*, const void*, void*, void*, void*, uint8_t*, float*, float*,
+                               hipStream_t);
+size_t rmsnorm_backward_workspace_bytes(int64_t, int64_t);
+loka_status rmsnorm_backward_launch(const loka_rms_desc*, const void*, const uint8_t*, const float*, const float*, const void*, const void*,
+                                    void*, float*, void*, hipStream_t);
 
 static bool mode_ok(int m) { return m >= LOKA_SCALE_TENSOR && m <= LOKA_SCALE_BLOCK_128x128_POW2; }       // modes a GEMM operand can have
 static bool quant_mode_ok(int m) { return m >= LOKA_SCALE_TENSOR && m <= LOKA_SCALE_BLOCK_128x1; }
@@ -416,6 +431,147 @@ loka_status loka_tracker_update(const void* x_bf16, int64_t B, int64_t K, int64_
     if (!workspace || ws_bytes < tracker_workspace_bytes(B, K)) return LOKA_ERR_WORKSPACE;
     if (!aligned16(workspace)) return LOKA_ERR_ALIGN;
     return tracker_update_launch(x_bf16, B, K, ld, n_old, mu, sigma, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+// ---- MXFP4
+int64_t loka_mxfp4_padded(int64_t cols) { return cols <= 0 ? -1 : (cols + 127) / 128 * 128; }
+
+static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
+                                uint8_t* scales, void* hip_stream) {
+    if (!x_bf16 || !q || !scales) return LOKA_ERR_NULL;
+    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (!aligned_to(x_bf16, 2) || !aligned16(q) || !aligned_to(scales, 4)) return LOKA_ERR_ALIGN;
+    return mxfp4_quantize_launch(x_bf16, rows, cols, ld, transpose_out, q, scales, static_cast<hipStream_t>(hip_stream));
+}
+
+loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, void* out_bf16, int64_t ld,
+                                  void* hip_stream) {
+    if (!q || !scales || !out_bf16) return LOKA_ERR_NULL;
+    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (!aligned_to(out_bf16, 2) || !aligned16(q) || !aligned_to(scales, 4)) return LOKA_ERR_ALIGN;
+    return mxfp4_dequantize_launch(q, scales, rows, cols, out_bf16, ld, static_cast<hipStream_t>(hip_stream));
+}
+
+// Shape rules of the products, shared by the workspace queries and the calls (linear: strides and batch are not read).
+static loka_status validate_mxfp4(const loka_gemm_desc* d, bool linear) {
+    if (!d) return LOKA_ERR_NULL;
+    if (d->M <= 0 || d->N <= 0 || d->K <= 0 || d->batch <= 0) return LOKA_ERR_SHAPE;
+    if (d->M > INT32_MAX || d->N > INT32_MAX || d->K > INT32_MAX || d->batch > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (d->norm != LOKA_NORM_NONE || d->act != LOKA_ACT_NONE || d->variant != -1) return LOKA_ERR_UNSUPPORTED;
+    if (linear) return d->batch == 1 ? LOKA_OK : LOKA_ERR_UNSUPPORTED;
+    if (d->batch > 1) {
+        const int64_t Kp = loka_mxfp4_padded(d->K);
+        if (d->strideX < 0 || d->strideW < 0 || d->strideO < d->M * d->N) return LOKA_ERR_SHAPE;
+        if ((d->strideX && d->strideX < d->M * Kp) || (d->strideW && d->strideW < d->N * Kp)) return LOKA_ERR_SHAPE;
+        if (d->strideX % 128 || d->strideW % 128) return LOKA_ERR_ALIGN;
+    }
+    return LOKA_OK;
+}
+
+size_t loka_mxfp4_gemm_workspace(const loka_gemm_desc* desc) {
+    return validate_mxfp4(desc, false) != LOKA_OK ? 0 : mxfp4_gemm_workspace_bytes(desc);
+}
+
+loka_status loka_mxfp4_gemm(const loka_gemm_desc* desc, const uint8_t* xq, const uint8_t* sx, const uint8_t* wq, const uint8_t* sw,
+                            void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes, void* hip_stream) {
+    if (!desc || !xq || !sx || !wq || !sw || (!out_bf16 && !y_fp32)) return LOKA_ERR_NULL;
+    const loka_status st = validate_mxfp4(desc, false);
+    if (st != LOKA_OK) return st;
+    if (!aligned16(xq) || !aligned16(wq) || !aligned_to(sx, 4) || !aligned_to(sw, 4) || !aligned16(out_bf16) || !aligned16(y_fp32) ||
+        !aligned16(workspace))
+        return LOKA_ERR_ALIGN;
+    return mxfp4_gemm_launch(desc, xq, sx, wq, sw, out_bf16, y_fp32, workspace, workspace ? ws_bytes : 0,
+                             static_cast<hipStream_t>(hip_stream));
+}
+
+// The workspace of the layer: codes of x, then their scales, then the product's own.
+static size_t linear_codes_bytes(const loka_gemm_desc* d) {
+    const size_t n = static_cast<size_t>(d->M) * static_cast<size_t>(loka_mxfp4_padded(d->K));
+    return n / 2 + (n / 32 + 15) / 16 * 16;
+}
+size_t loka_mxfp4_linear_workspace(const loka_gemm_desc* desc) {
+    if (validate_mxfp4(desc, true) != LOKA_OK || mxfp4_linear_fused(desc)) return 0;
+    return linear_codes_bytes(desc) + mxfp4_gemm_workspace_bytes(desc);
+}
+
+loka_status loka_mxfp4_linear(const loka_gemm_desc* desc, const void* x_bf16, int64_t ld, const uint8_t* wq, const uint8_t* sw,
+                              void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes, void* hip_stream) {
+    if (!desc || !x_bf16 || !wq || !sw || (!out_bf16 && !y_fp32)) return LOKA_ERR_NULL;
+    const loka_status st = validate_mxfp4(desc, true);
+    if (st != LOKA_OK) return st;
+    if (ld < desc->K) return LOKA_ERR_SHAPE;
+    if (!aligned_to(x_bf16, 2) || !aligned16(wq) || !aligned_to(sw, 4) || !aligned16(out_bf16) || !aligned16(y_fp32)) return LOKA_ERR_ALIGN;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (mxfp4_linear_fused(desc)) return mxfp4_linear_fused_launch(desc, x_bf16, ld, wq, sw, out_bf16, y_fp32, stream);
+    const size_t need = loka_mxfp4_linear_workspace(desc);
+    if (!workspace || ws_bytes < need) return LOKA_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return LOKA_ERR_ALIGN;
+    uint8_t* const xq = static_cast<uint8_t*>(workspace);
+    uint8_t* const sx = xq + static_cast<size_t>(desc->M) * static_cast<size_t>(loka_mxfp4_padded(desc->K)) / 2;
+    const size_t used = linear_codes_bytes(desc);
+    const loka_status sq = mxfp4_quantize_launch(x_bf16, desc->M, desc->K, ld, 0, xq, sx, stream);
+    if (sq != LOKA_OK) return sq;
+    return mxfp4_gemm_launch(desc, xq, sx, wq, sw, out_bf16, y_fp32, xq + used, ws_bytes - used, stream);
+}
+
+// ---- residual addition + RMSNorm
+static bool rms_mode_ok(int m) { return m == LOKA_SCALE_ROW || is_block_x(m); }
+
+// Shape rules shared by the forward pass, the backward pass and its workspace query.
+static loka_status validate_rms(const loka_rms_desc* d) {
+    if (!d) return LOKA_ERR_NULL;
+    if (d->rows <= 0 || d->cols <= 0 || d->cols % 16) return LOKA_ERR_SHAPE;
+    if (d->rows > INT32_MAX || d->cols > 65536) return LOKA_ERR_SHAPE;
+    return LOKA_OK;
+}
+// ... and those of a matrix with scales in `mode`
+static loka_status validate_rms_mode(const loka_rms_desc* d, int mode) {
+    if (!rms_mode_ok(mode)) return LOKA_ERR_UNSUPPORTED;
+    return is_block_x(mode) && d->cols % 128 ? LOKA_ERR_SHAPE : LOKA_OK;
+}
+
+loka_status loka_add_rmsnorm(const loka_rms_desc* desc, const void* x_bf16, const void* residual_bf16, const void* gamma_bf16,
+                             void* h_out_bf16, void* y_out, void* y_scales, uint8_t* hq, float* hs, float* rstd, void* hip_stream) {
+    if (!desc || !x_bf16 || !y_out) return LOKA_ERR_NULL;
+    loka_status st = validate_rms(desc);
+    if (st != LOKA_OK) return st;
+    if (desc->out < LOKA_RMS_OUT_BF16 || desc->out > LOKA_RMS_OUT_MXFP4 || !(desc->eps >= 0.f)) return LOKA_ERR_UNSUPPORTED;
+    if ((desc->out != LOKA_RMS_OUT_BF16 && !y_scales) || (hq != nullptr) != (hs != nullptr)) return LOKA_ERR_NULL;
+    if (desc->out == LOKA_RMS_OUT_E4M3 && (st = validate_rms_mode(desc, desc->out_mode)) != LOKA_OK) return st;
+    if (hq && (st = validate_rms_mode(desc, desc->ckpt_mode)) != LOKA_OK) return st;
+    if (desc->ld_x < desc->cols || (residual_bf16 && desc->ld_r < desc->cols)) return LOKA_ERR_SHAPE;
+    if (desc->ld_x % 8 || (residual_bf16 && desc->ld_r % 8)) return LOKA_ERR_ALIGN;
+    if (!aligned16(x_bf16) || !aligned16(residual_bf16) || !aligned16(gamma_bf16) || !aligned16(h_out_bf16) || !aligned16(y_out) ||
+        !aligned16(hq) || !aligned_to(y_scales, 4) || !aligned_to(hs, 4) || !aligned_to(rstd, 4))
+        return LOKA_ERR_ALIGN;
+    return add_rmsnorm_launch(desc, x_bf16, residual_bf16, gamma_bf16, h_out_bf16, y_out, y_scales, hq, hs, rstd,
+                              static_cast<hipStream_t>(hip_stream));
+}
+
+size_t loka_rmsnorm_backward_workspace(const loka_rms_desc* desc) {
+    return validate_rms(desc) != LOKA_OK ? 0 : rmsnorm_backward_workspace_bytes(desc->rows, desc->cols);
+}
+
+loka_status loka_rmsnorm_backward(const loka_rms_desc* desc, const void* dy_bf16, const uint8_t* hq, const float* hs, const float* rstd,
+                                  const void* gamma_bf16, const void* dh_bf16, void* dx_bf16, float* dgamma, void* workspace,
+                                  size_t ws_bytes, void* hip_stream) {
+    if (!desc || !dy_bf16 || !hq || !hs || !rstd || !dx_bf16) return LOKA_ERR_NULL;
+    loka_status st = validate_rms(desc);
+    if (st != LOKA_OK) return st;
+    if ((st = validate_rms_mode(desc, desc->ckpt_mode)) != LOKA_OK) return st;
+    if (desc->ld_x < desc->cols || (dh_bf16 && desc->ld_r < desc->cols)) return LOKA_ERR_SHAPE;
+    if (desc->ld_x % 8 || (dh_bf16 && desc->ld_r % 8)) return LOKA_ERR_ALIGN;
+    if (!aligned16(dy_bf16) || !aligned16(hq) || !aligned16(gamma_bf16) || !aligned16(dh_bf16) || !aligned16(dx_bf16) ||
+        !aligned_to(hs, 4) || !aligned_to(rstd, 4) || !aligned_to(dgamma, 4))
+        return LOKA_ERR_ALIGN;
+    if (dgamma) {
+        if (!workspace || ws_bytes < rmsnorm_backward_workspace_bytes(desc->rows, desc->cols)) return LOKA_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return LOKA_ERR_ALIGN;
+    }
+    return rmsnorm_backward_launch(desc, dy_bf16, hq, hs, rstd, gamma_bf16, dh_bf16, dx_bf16, dgamma, workspace,
+                                   static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

@@ -294,6 +294,267 @@ PyObject* tracker_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- MXFP4 and the residual norm.  Their buffers' sizes follow from the arguments, so every tensor is looked at before its
+// address is handed on; the calls run on the tensors' own device, on that device's current stream.
+PyObject* refuse(const char* what) {
+    PyErr_SetString(PyExc_AssertionError, what);
+    return nullptr;
+}
+// bf16 [rows, cols] with contiguous rows
+bool is_rows(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 && t.dim() == 2 && (t.stride(1) == 1 || t.size(1) == 1); }
+bool is_rows_of(const at::Tensor& t, int64_t rows, int64_t cols) { return is_rows(t) && t.size(0) == rows && t.size(1) == cols; }
+// a contiguous tensor of at least n elements
+bool holds(const at::Tensor& t, at::ScalarType type, int64_t n) { return t.scalar_type() == type && t.is_contiguous() && t.numel() >= n; }
+// row stride of a matrix; of a single row it is free
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8; }
+bool on_gpu(const at::Device& dev, std::initializer_list<const at::Tensor*> ts) {
+    if (!dev.is_cuda()) return false;
+    for (const at::Tensor* t : ts)
+        if (t && t->defined() && t->device() != dev) return false;
+    return true;
+}
+at::Tensor given(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
+template <class T>
+T* at_or_null(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr; }
+void* stream_of(const at::Device& dev) { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+
+// mxfp4_quantize(x, transpose_out) -> (codes, scales)
+PyObject* mxfp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 2)) return nullptr;
+    const at::Tensor& x = tensor(a[0]);
+    const int tr = PyObject_IsTrue(a[1]);
+    if (tr < 0) return nullptr;
+    if (!is_rows(x)) return refuse("x: bf16 [rows, cols] with contiguous rows");
+    const int64_t rows = x.size(0), cols = x.size(1);
+    if (rows <= 0 || cols <= 0) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_quantize");
+    const at::Device dev = x.device();
+    if (!on_gpu(dev, {})) return refuse("x: a tensor on the GPU");
+    const c10::DeviceGuard guard(dev);
+    const int64_t r = tr ? cols : rows, kp = loka_mxfp4_padded(tr ? rows : cols);
+    at::Tensor q = empty({r, kp / 2}, at::kByte, dev), s = empty({r, kp / 32}, at::kByte, dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_mxfp4_quantize(ptr(x), rows, cols, row_stride(x), tr, static_cast<uint8_t*>(ptr(q)), static_cast<uint8_t*>(ptr(s)), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_mxfp4_quantize");
+    return pack({q, s});
+    END_HANDLE_TH_ERRORS
+}
+
+// codes and scales of a stored operand of `rows` rows of `cols` elements
+bool is_stored(const at::Tensor& q, const at::Tensor& s, int64_t rows, int64_t cols) {
+    const int64_t kp = loka_mxfp4_padded(cols);
+    return holds(q, at::kByte, rows * (kp / 2)) && holds(s, at::kByte, rows * (kp / 32));
+}
+
+// mxfp4_dequantize(q, scales, cols, out) -> out
+PyObject* mxfp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 4)) return nullptr;
+    const at::Tensor &q = tensor(a[0]), &s = tensor(a[1]);
+    const long long cols = PyLong_AsLongLong(a[2]);
+    if (cols == -1 && PyErr_Occurred()) return nullptr;
+    if (q.dim() != 2 || cols <= 0) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_dequantize");
+    const int64_t rows = q.size(0);
+    if (q.size(1) != loka_mxfp4_padded(cols) / 2 || !is_stored(q, s, rows, cols)) return refuse("q, scales: uint8 [rows, padded cols / 2] and [rows, padded cols / 32]");
+    const at::Device dev = q.device();
+    at::Tensor out = given(a[3]);
+    if (!on_gpu(dev, {&s, &out})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (!out.defined()) out = empty({rows, cols}, at::kBFloat16, dev);
+    else if (!is_rows_of(out, rows, cols)) return refuse("out: bf16 [rows, cols] with contiguous rows");
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_mxfp4_dequantize(static_cast<uint8_t*>(ptr(q)), static_cast<uint8_t*>(ptr(s)), rows, cols, ptr(out), row_stride(out), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_mxfp4_dequantize");
+    return wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// outputs of a product: out (where wanted or given) and y (likewise); false with an exception set
+bool product_outputs(PyObject* want_out, PyObject* want_y, PyObject* out_o, PyObject* y_o, int64_t numel, int64_t rows, int64_t cols, const at::Device& dev,
+                     at::Tensor& out, at::Tensor& y) {
+    const int wo = PyObject_IsTrue(want_out), wy = PyObject_IsTrue(want_y);
+    if (wo < 0 || wy < 0) return false;
+    if (wo || out_o != Py_None) out = given_or(out_o, {rows, cols}, at::kBFloat16, dev);
+    if (wy || y_o != Py_None) y = given_or(y_o, {rows, cols}, at::kFloat, dev);
+    if ((out.defined() && !holds(out, at::kBFloat16, numel)) || (y.defined() && !holds(y, at::kFloat, numel))) {
+        refuse("out, y: contiguous bf16 / fp32 [batch * M, N]");
+        return false;
+    }
+    if (!on_gpu(dev, {&out, &y})) {
+        refuse("tensors on one GPU");
+        return false;
+    }
+    return true;
+}
+// elements that `batch` problems `stride` apart span, `each` of them the last (0: shared)
+int64_t span(int64_t batch, int64_t stride, int64_t each) { return (batch - 1) * stride + each; }
+constexpr int64_t kMost = INT64_C(1) << 31, kMostElements = INT64_C(1) << 46;      // of a size; of a whole operand
+bool sizes_ok(const loka_gemm_desc& d) {
+    return d.M > 0 && d.N > 0 && d.K > 0 && d.batch > 0 && d.M < kMost && d.N < kMost && d.K < kMost && d.batch < kMost &&
+           d.strideX >= 0 && d.strideW >= 0 && d.strideO >= 0 && d.strideX < kMostElements && d.strideW < kMostElements &&
+           d.strideO < kMostElements && d.batch * (d.strideO / 1024 + 1) < kMostElements / 1024 &&
+           d.batch * (d.strideX / 1024 + 1) < kMostElements / 1024 && d.batch * (d.strideW / 1024 + 1) < kMostElements / 1024;
+}
+
+// mxfp4_gemm(desc, xq, sx, wq, sw, want_out, want_y, out, y, workspace) -> (out or None, y or None)
+PyObject* mxfp4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 10)) return nullptr;
+    const loka_gemm_desc d = desc_of(a[0]);
+    const at::Tensor &xq = tensor(a[1]), &sx = tensor(a[2]), &wq = tensor(a[3]), &sw = tensor(a[4]);
+    if (!sizes_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_gemm");
+    const int64_t kp = loka_mxfp4_padded(d.K);
+    const int64_t nx = span(d.batch, d.strideX, d.M * kp), nw = span(d.batch, d.strideW, d.N * kp);
+    if (!holds(xq, at::kByte, nx / 2) || !holds(sx, at::kByte, nx / 32) || !holds(wq, at::kByte, nw / 2) || !holds(sw, at::kByte, nw / 32))
+        return refuse("xq, sx, wq, sw: stored operands [batch, M, K] and [batch, N, K], contiguous uint8");
+    const at::Device dev = xq.device();
+    at::Tensor ws = given(a[9]);
+    if (!on_gpu(dev, {&sx, &wq, &sw, &ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor out, y;
+    if (!product_outputs(a[5], a[6], a[7], a[8], span(d.batch, d.batch > 1 ? d.strideO : 0, d.M * d.N), d.batch * d.M, d.N, dev, out, y)) return nullptr;
+    if (!ws.defined()) ws = scratch(loka_mxfp4_gemm_workspace(&d), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_mxfp4_gemm(&d, static_cast<uint8_t*>(ptr(xq)), static_cast<uint8_t*>(ptr(sx)), static_cast<uint8_t*>(ptr(wq)),
+                               static_cast<uint8_t*>(ptr(sw)), at_or_null<void>(out), at_or_null<float>(y), at_or_null<void>(ws),
+                               ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_mxfp4_gemm");
+    return pack({out, y});
+    END_HANDLE_TH_ERRORS
+}
+
+// mxfp4_linear(desc, x, wq, sw, want_out, want_y, out, y, workspace) -> (out or None, y or None)
+PyObject* mxfp4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 9)) return nullptr;
+    const loka_gemm_desc d = desc_of(a[0]);
+    const at::Tensor &x = tensor(a[1]), &wq = tensor(a[2]), &sw = tensor(a[3]);
+    if (!sizes_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_linear");
+    if (!is_rows_of(x, d.M, d.K)) return refuse("x: bf16 [M, K] with contiguous rows");
+    if (!is_stored(wq, sw, d.N, d.K)) return refuse("wq, sw: a stored operand [N, K], contiguous uint8");
+    const at::Device dev = x.device();
+    at::Tensor ws = given(a[8]);
+    if (!on_gpu(dev, {&wq, &sw, &ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor out, y;
+    if (!product_outputs(a[4], a[5], a[6], a[7], d.M * d.N, d.M, d.N, dev, out, y)) return nullptr;
+    if (!ws.defined()) ws = scratch(loka_mxfp4_linear_workspace(&d), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_mxfp4_linear(&d, ptr(x), row_stride(x), static_cast<uint8_t*>(ptr(wq)), static_cast<uint8_t*>(ptr(sw)), at_or_null<void>(out),
+                                 at_or_null<float>(y), at_or_null<void>(ws), ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_mxfp4_linear");
+    return pack({out, y});
+    END_HANDLE_TH_ERRORS
+}
+
+// add_rmsnorm(x, residual, gamma, eps, out, out_mode, ckpt_mode, want_h, want_rstd, h_out) -> (h, y, scales, hq, hs, rstd)
+PyObject* add_rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 10)) return nullptr;
+    const at::Tensor& x = tensor(a[0]);
+    const at::Tensor res = given(a[1]), gamma = given(a[2]);
+    const double eps = PyFloat_AsDouble(a[3]);
+    const long out = PyLong_AsLong(a[4]), out_mode = PyLong_AsLong(a[5]);
+    const bool ckpt = a[6] != Py_None;
+    const long ckpt_mode = ckpt ? PyLong_AsLong(a[6]) : 0;
+    const int want_h = PyObject_IsTrue(a[7]), want_rstd = PyObject_IsTrue(a[8]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!is_rows(x)) return refuse("x: bf16 [rows, cols] with contiguous rows");
+    loka_rms_desc d{};
+    d.rows = x.size(0);
+    d.cols = x.size(1);
+    d.ld_x = row_stride(x);
+    d.out = static_cast<int32_t>(out);
+    d.out_mode = static_cast<int32_t>(out_mode);
+    d.ckpt_mode = static_cast<int32_t>(ckpt_mode);
+    d.eps = static_cast<float>(eps);
+    if (res.defined() && !is_rows_of(res, d.rows, d.cols)) return refuse("residual: bf16 [rows, cols] with contiguous rows");
+    d.ld_r = res.defined() ? row_stride(res) : 0;
+    if (gamma.defined() && !(holds(gamma, at::kBFloat16, d.cols) && gamma.numel() == d.cols)) return refuse("gamma: contiguous bf16 [cols]");
+    if (d.rows <= 0 || d.cols <= 0) return fail(LOKA_ERR_SHAPE, "loka_add_rmsnorm");
+    const bool e4m3 = out == LOKA_RMS_OUT_E4M3, mx = out == LOKA_RMS_OUT_MXFP4;
+    const int64_t groups = e4m3 ? loka_scale_count(static_cast<loka_scale_mode>(out_mode), d.rows, d.cols) : 0;
+    const int64_t hgroups = ckpt ? loka_scale_count(static_cast<loka_scale_mode>(ckpt_mode), d.rows, d.cols) : 0;
+    if (groups < 0 || hgroups < 0) return fail(LOKA_ERR_SHAPE, "loka_scale_count");
+    const at::Device dev = x.device();
+    at::Tensor h = given(a[9]);
+    if (!on_gpu(dev, {&res, &gamma, &h})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (h.defined()) {
+        if (!(holds(h, at::kBFloat16, d.rows * d.cols) && is_rows_of(h, d.rows, d.cols))) return refuse("h_out: contiguous bf16 [rows, cols]");
+    } else if (want_h) {
+        h = empty({d.rows, d.cols}, at::kBFloat16, dev);
+    }
+    const int64_t kp = loka_mxfp4_padded(d.cols);
+    at::Tensor y = mx ? empty({d.rows, kp / 2}, at::kByte, dev) : empty({d.rows, d.cols}, e4m3 ? at::kByte : at::kBFloat16, dev), s, hq, hs, rstd;
+    if (e4m3) s = out_mode == LOKA_SCALE_ROW ? empty({groups}, at::kFloat, dev) : empty({d.rows, groups / d.rows}, at::kFloat, dev);
+    if (mx) s = empty({d.rows, kp / 32}, at::kByte, dev);
+    if (ckpt) {
+        hq = empty({d.rows, d.cols}, at::kByte, dev);
+        hs = ckpt_mode == LOKA_SCALE_ROW ? empty({hgroups}, at::kFloat, dev) : empty({d.rows, hgroups / d.rows}, at::kFloat, dev);
+    }
+    if (want_rstd) rstd = empty({d.rows}, at::kFloat, dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_add_rmsnorm(&d, ptr(x), at_or_null<void>(res), at_or_null<void>(gamma), at_or_null<void>(h), ptr(y), at_or_null<void>(s),
+                                at_or_null<uint8_t>(hq), at_or_null<float>(hs), at_or_null<float>(rstd), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_add_rmsnorm");
+    return pack({h, y, s, hq, hs, rstd});
+    END_HANDLE_TH_ERRORS
+}
+
+// rmsnorm_backward(dy, hq, hs, rstd, gamma, dh, ckpt_mode, want_dgamma, dx, workspace) -> (dx, dgamma or None)
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 10)) return nullptr;
+    const at::Tensor &dy = tensor(a[0]), &hq = tensor(a[1]), &hs = tensor(a[2]), &rstd = tensor(a[3]);
+    const at::Tensor gamma = given(a[4]), dh = given(a[5]);
+    const long mode = PyLong_AsLong(a[6]);
+    const int want_dgamma = PyObject_IsTrue(a[7]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!is_rows(dy)) return refuse("dy: bf16 [rows, cols] with contiguous rows");
+    loka_rms_desc d{};
+    d.rows = dy.size(0);
+    d.cols = dy.size(1);
+    d.ld_x = row_stride(dy);
+    d.ckpt_mode = static_cast<int32_t>(mode);
+    if (dh.defined() && !is_rows_of(dh, d.rows, d.cols)) return refuse("dh: bf16 [rows, cols] with contiguous rows");
+    d.ld_r = dh.defined() ? row_stride(dh) : 0;
+    if (d.rows <= 0 || d.cols <= 0) return fail(LOKA_ERR_SHAPE, "loka_rmsnorm_backward");
+    const int64_t groups = loka_scale_count(static_cast<loka_scale_mode>(mode), d.rows, d.cols);
+    if (groups < 0) return fail(LOKA_ERR_SHAPE, "loka_scale_count");
+    if (!holds(hq, at::kByte, d.rows * d.cols) || hq.numel() != d.rows * d.cols || !holds(hs, at::kFloat, groups) || hs.numel() != groups ||
+        !holds(rstd, at::kFloat, d.rows) || rstd.numel() != d.rows)
+        return refuse("hq, hs, rstd: contiguous uint8 [rows, cols], its fp32 scales, fp32 [rows]");
+    if (gamma.defined() && !(holds(gamma, at::kBFloat16, d.cols) && gamma.numel() == d.cols)) return refuse("gamma: contiguous bf16 [cols]");
+    const at::Device dev = dy.device();
+    at::Tensor dx = given(a[8]), ws = given(a[9]);
+    if (!on_gpu(dev, {&hq, &hs, &rstd, &gamma, &dh, &dx, &ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (!dx.defined()) dx = empty({d.rows, d.cols}, at::kBFloat16, dev);
+    else if (!(holds(dx, at::kBFloat16, d.rows * d.cols) && is_rows_of(dx, d.rows, d.cols))) return refuse("dx: contiguous bf16 [rows, cols]");
+    at::Tensor dg = want_dgamma ? empty({d.cols}, at::kFloat, dev) : at::Tensor();
+    if (!ws.defined() && want_dgamma) ws = scratch(loka_rmsnorm_backward_workspace(&d), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_rmsnorm_backward(&d, ptr(dy), static_cast<uint8_t*>(ptr(hq)), static_cast<float*>(ptr(hs)), static_cast<float*>(ptr(rstd)),
+                                     at_or_null<void>(gamma), at_or_null<void>(dh), ptr(dx), at_or_null<float>(dg), at_or_null<void>(ws),
+                                     ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_rmsnorm_backward");
+    return pack({dx, dg});
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XSETREF(g_error, cls);
@@ -304,6 +565,8 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 PyMethodDef kMethods[] = {
     LOKA_FAST(quantize), LOKA_FAST(gemm_norm), LOKA_FAST(gemm_norm_fp8out), LOKA_FAST(linear_norm), LOKA_FAST(linear_norm_xq),
     LOKA_FAST(bf16_gemm), LOKA_FAST(probe_error), LOKA_FAST(tracker_update),
+    LOKA_FAST(mxfp4_quantize), LOKA_FAST(mxfp4_dequantize), LOKA_FAST(mxfp4_gemm), LOKA_FAST(mxfp4_linear), LOKA_FAST(add_rmsnorm),
+    LOKA_FAST(rmsnorm_backward),
     {"set_error", &set_error, METH_O, "the exception class raised for a status other than LOKA_OK"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", "marshalling of the per-step calls", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
