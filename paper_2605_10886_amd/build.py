@@ -34,8 +34,9 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-cont
 # which bind the scheduler but not the machine-code sinking pass that runs before it; that pass moves the SCALED
 # matrix instructions (which it takes for freely movable) out of their slots to the end of the loop body, behind
 # every LDS read, and the accumulators spill.  The pass is switched off for that file (its other kernels come out
-# the same, instruction for instruction, apart from a few address computations).
-EXTRA_FLAGS = {"gemm_panel32.hip": ["-mllvm", "-disable-machine-sink"]}
+# the same, instruction for instruction, apart from a few address computations).  mxfp4_gemm.hip: the same pass moves the first
+# half of a K tile's matrix instructions behind the barrier that the second half's operands wait for.
+EXTRA_FLAGS = {"gemm_panel32.hip": ["-mllvm", "-disable-machine-sink"], "mxfp4_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
 
 
 def _hipcc() -> str:

@@ -7,6 +7,7 @@
 // Which 32-groups of a row meet in one instruction is free as long as both operands agree: the four instructions of 512
 // consecutive elements take groups 4 g + s (g: lane / 16, s: instruction), so a lane reads 64 consecutive bytes of codes and
 // one word with the four scale bytes, which the instruction picks by its byte selector.
+#include "gemm_common.h"
 #include "mxfp4.h"
 
 namespace loka {
@@ -21,8 +22,14 @@ struct MxArgs {
     int64_t M, N, K, Kp;               // Kp: stored row length in elements
     int64_t ldx;
     int64_t strideX, strideW, strideO; // elements between problems
-    int64_t n_tiles, m_tiles;
+    int64_t n_tiles, m_tiles;          // stream kernel
     bool x_wide;                       // rows of x start on multiples of 16 bytes
+    // tile kernel: result tiles of a problem, K ranges and their length in K tiles, all tiles
+    int64_t batch;
+    int tiles_m, tiles_n, splits, k_per_split, total;
+    float* part;                       // [splits][batch][M][N]
+    // every XCD starts on consecutive tiles, which share operands
+    __device__ __forceinline__ int first_of(int block, int grid) const { return xcd_contiguous(block, grid); }
 };
 
 template <int S>
@@ -153,6 +160,212 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
     }
 }
 
+// ---------------------------------------------------------------------------------
+// Many rows: a workgroup of WM x WN waves computes a tile of the result, each wave TM x TN tiles of 16 x 16, on K tiles of 256
+// elements (128 bytes of codes a row) that loads bring straight into LDS, two K tiles in the ring.  The 16-byte chunks of a
+// row lie permuted, chunk c at place c ^ key(row), so that the 16 rows that a quarter wave reads at once use all 64 banks.
+// A lane takes groups 2 g and 2 g + 1 of a row for the K tile's two instructions, whose scale bytes are then neighbours:
+// one 16-bit LDS read for both.
+// The waves' W rows are dealt to the 16 x 16 tiles so that a lane's columns of a tile pair are 8 neighbours (coff_of).
+//
+// One barrier a K tile: its second half's operands are in registers when the barrier is passed, so the loads of the K tile
+// after next may go where this one lay, and the first operands of the next K tile are read behind the second half's matrix
+// instructions.  Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first K
+// tiles arrive while this one's values are stored.
+template <int TM_, int TN_, int WM_, int WN_>
+struct MxTile {
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+    static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 8, STAGE = OFF_SW + BN * 8;
+    static_assert(NW % 4 == 0 && BM % (32 * NW) == 0 && BN % (32 * NW) == 0 && TN % 2 == 0);
+};
+
+template <class C, bool SPLIT>
+__global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 2) void mx_tile_kernel(const MxArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wm = wave / C::WN, wn = wave % C::WN;
+    const int row_bytes = static_cast<int>(a.Kp >> 1), scale_bytes = static_cast<int>(a.Kp >> 5);
+    const int ktiles_all = static_cast<int>((a.Kp + 255) >> 8);
+    const bool ragged = (a.Kp & 255) != 0;
+    const int total = a.total;
+
+    // where this wave's loads put and find things
+    const int key_x = ((wave & 1) << 2) | (lane >> 4), key_w = ((lane >> 4) & 1) | ((wave & 3) << 1);
+    const int x_chunk = (lane & 7) ^ key_x, w_chunk = (lane & 7) ^ key_w;
+    const int x_lane = (lane >> 3) * row_bytes + x_chunk * 16, w_lane = (lane >> 3) * row_bytes + w_chunk * 16;
+    const int s_lane = (lane >> 1) * scale_bytes + (lane & 1) * 4;
+    // where it reads operands
+    const int x_at = (wm * C::TM * 16 + r) * 128, x_p = (2 * g) ^ (r >> 1);
+    const int w_row = wn * C::TN * 16 + (r >> 2) * 8 + (r & 3), w_p = (2 * g) ^ (((r >> 1) & 1) | ((r >> 2) << 1));
+    const int x_off[2] = {x_at + x_p * 16, x_at + (x_p ^ 1) * 16};
+    const int w_off[2] = {C::OFF_W + w_row * 128 + w_p * 16, C::OFF_W + w_row * 128 + (w_p ^ 1) * 16};
+    const int sx_off = C::OFF_SX + (wm * C::TM * 16 + r) * 8 + 2 * g, sw_off = C::OFF_SW + w_row * 8 + 2 * g;
+
+    struct Place { int m0, n0, k_first, k_count, split; int64_t prob; };
+    auto locate = [&](int t) __attribute__((always_inline)) {
+        Place p;
+        const int per = a.tiles_m * a.tiles_n;
+        const int o = t / per;
+        int tm, tn;
+        banded_tile(t - o * per, a.tiles_m, a.tiles_n, tm, tn);
+        p.prob = SPLIT ? o / a.splits : o;
+        p.split = SPLIT ? o - static_cast<int>(p.prob) * a.splits : 0;
+        p.k_first = p.split * a.k_per_split;
+        p.k_count = !SPLIT || p.k_first + a.k_per_split > ktiles_all ? ktiles_all - p.k_first : a.k_per_split;
+        p.m0 = tm * C::BM;
+        p.n0 = tn * C::BN;
+        return p;
+    };
+
+    // ---- the stream of K tiles: `ld_*` is the next one to request
+    int ld_tile = a.first_of(blockIdx.x, gridDim.x), ld_k = 0;
+    Place ld = locate(ld_tile < total ? ld_tile : 0);
+    __amdgpu_buffer_rsrc_t xr, wr, sxr, swr;
+    auto aim = [&]() __attribute__((always_inline)) {
+        const int64_t rows_x = a.M - ld.m0 < C::BM ? a.M - ld.m0 : C::BM, rows_w = a.N - ld.n0 < C::BN ? a.N - ld.n0 : C::BN;
+        const bool on = ld_tile < total;
+        auto make = [&](const uint8_t* base, int64_t bytes) __attribute__((always_inline)) {
+            return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, on ? static_cast<int>(bytes) : 0, 0x00020000);
+        };
+        xr = make(a.xq + ld.prob * (a.strideX >> 1) + static_cast<int64_t>(ld.m0) * row_bytes, rows_x * row_bytes);
+        wr = make(a.wq + ld.prob * (a.strideW >> 1) + static_cast<int64_t>(ld.n0) * row_bytes, rows_w * row_bytes);
+        sxr = make(a.sx + ld.prob * (a.strideX >> 5) + static_cast<int64_t>(ld.m0) * scale_bytes, rows_x * scale_bytes);
+        swr = make(a.sw + ld.prob * (a.strideW >> 5) + static_cast<int64_t>(ld.n0) * scale_bytes, rows_w * scale_bytes);
+    };
+    aim();
+    auto request = [&](int stage) __attribute__((always_inline)) {
+        const int kt = ld.k_first + ld_k;
+        const bool tail = ragged && kt == ktiles_all - 1;           // the last K tile is half one: the other half reads zeros
+        const int xl = tail && x_chunk >= 4 ? 0x7FFFFFFF : x_lane, wl = tail && w_chunk >= 4 ? 0x7FFFFFFF : w_lane;
+        const int sl = tail && (lane & 1) ? 0x7FFFFFFF : s_lane;
+#pragma unroll
+        for (int j = 0; j < C::BM / (8 * C::NW); ++j) {
+            const int grp = j * C::NW + wave;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + grp * 1024), 16, xl, grp * 8 * row_bytes + kt * 128, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < C::BN / (8 * C::NW); ++j) {
+            const int grp = j * C::NW + wave;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + grp * 1024), 16, wl, grp * 8 * row_bytes + kt * 128, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < C::BM / (32 * C::NW); ++j) {
+            const int grp = j * C::NW + wave;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, sl, grp * 32 * scale_bytes + kt * 8, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < C::BN / (32 * C::NW); ++j) {
+            const int grp = j * C::NW + wave;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + grp * 256), 4, sl, grp * 32 * scale_bytes + kt * 8, 0, 0);
+        }
+        if (++ld_k == ld.k_count) {
+            ld_k = 0;
+            ld_tile += gridDim.x;
+            ld = locate(ld_tile < total ? ld_tile : 0);
+            aim();
+        }
+    };
+
+    u32x4 fx[2][C::TM], fw[2][C::TN];
+    uint32_t sx[C::TM], sw[C::TN], sx_next[C::TM], sw_next[C::TN];
+    auto read = [&](int stage, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) fw[s][j] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[s] + (j >> 1) * 4096 + (j & 1) * 512);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) fx[s][i] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[s] + i * 2048);
+    };
+    auto read_scales = [&](int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j) sw_next[j] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + (j >> 1) * 256 + (j & 1) * 32);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) sx_next[i] = *reinterpret_cast<const uint16_t*>(smem + stage + sx_off + i * 128);
+    };
+    v4f acc[C::TM][C::TN];
+
+    int tile = ld_tile;
+    if (tile >= total) return;
+    Place at = ld;
+    request(0);
+    request(C::STAGE);
+    int stage = 0;
+    wait_vmcnt<0>();
+    lds_barrier();
+    read(0, 0);
+    read_scales(0);
+    for (; tile < total; tile += gridDim.x) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < at.k_count; ++k) {
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) sx[i] = sx_next[i];
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) sw[j] = sw_next[j];
+            read(stage, 1);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j) acc[i][j] = mx_mfma<0>(fw[0][j], fx[0][i], acc[i][j], sw[j], sx[i]);
+            wait_vmcnt<0>();                            // the next K tile has landed
+            lds_barrier();                              // ... for everyone, and everyone has this one's operands
+            request(stage);
+            stage ^= C::STAGE;
+            read(stage, 0);
+            read_scales(stage);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j) acc[i][j] = mx_mfma<1>(fw[1][j], fx[1][i], acc[i][j], sw[j], sx[i]);
+        }
+        // ---- lane (r, g) holds rows 16 i + r, columns coff_of(j) + 8 g + 0 .. 3
+        const int64_t n_first = at.n0 + wn * C::TN * 16 + g * 8;
+        float* const y = SPLIT ? a.part + (static_cast<int64_t>(at.split) * a.batch + at.prob) * a.M * a.N : a.y ? a.y + at.prob * a.strideO : nullptr;
+        uint16_t* const out = SPLIT || !a.out ? nullptr : a.out + at.prob * a.strideO;
+        const bool wide = (a.N & 7) == 0;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+            const int64_t m = at.m0 + (wm * C::TM + i) * 16 + r;
+            if (m < a.M) {
+#pragma unroll
+                for (int j = 0; j < C::TN; j += 2) {
+                    const int64_t n = n_first + j * 16, o = m * a.N + n;
+                    const v4f lo = acc[i][j], hi = acc[i][j + 1];
+                    if (wide && n < a.N) {
+                        if (out) *reinterpret_cast<u32x4*>(out + o) = u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)};
+                        if (y) {
+                            *reinterpret_cast<v4f*>(y + o) = lo;
+                            *reinterpret_cast<v4f*>(y + o + 4) = hi;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (n + e < a.N) {
+                                const float v = e < 4 ? lo[e & 3] : hi[e & 3];
+                                if (out) out[o + e] = static_cast<uint16_t>(f32_to_bf16_rne(v));
+                                if (y) y[o + e] = v;
+                            }
+                    }
+                }
+            }
+        }
+        if (tile + static_cast<int>(gridDim.x) < total) at = locate(tile + gridDim.x);
+    }
+    wait_vmcnt<0>();           // the requests past the end (zeros) land before the workgroup's LDS is given on
+}
+
+// Sums of the partial products of a split contraction, in order.
+__global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ part, int splits, int64_t n, int64_t per_problem, int64_t stride_o,
+                                                      uint16_t* __restrict__ out, float* __restrict__ y) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= n) return;
+    float s = part[i];
+    for (int k = 1; k < splits; ++k) s += part[k * n + i];
+    const int64_t prob = i / per_problem, o = prob * stride_o + (i - prob * per_problem);
+    if (out) out[o] = static_cast<uint16_t>(f32_to_bf16_rne(s));
+    if (y) y[o] = s;
+}
+
 template <int MT, int NT, bool FUSED>
 static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
     constexpr int NW = 8;
@@ -180,15 +393,75 @@ static MxArgs args_of(const loka_gemm_desc* d, const uint8_t* wq, const uint8_t*
     return a;
 }
 
-size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc*) { return 0; }
+// What runs a product: the stream kernel for few rows, else tiles of 128 x 128, or 256 x 256 where these fill the chip
+struct MxPlan { int kind; int tiles_m, tiles_n, splits, k_per_split; int64_t total; };
+static MxPlan plan_of(const loka_gemm_desc* d) {
+    MxPlan p{0, 0, 0, 1, 0, 0};
+    const int64_t Kp = mx_padded(d->K), ktiles = (Kp + 255) / 256;
+    if (d->M <= 32 || Kp >= (INT64_C(1) << 23)) return p;
+    auto tiles = [&](int64_t b) { return ((d->M + b - 1) / b) * ((d->N + b - 1) / b) * d->batch; };
+    p.kind = tiles(256) >= 256 ? 2 : 1;
+    const int b = p.kind == 2 ? 256 : 128;
+    p.tiles_m = static_cast<int>((d->M + b - 1) / b);
+    p.tiles_n = static_cast<int>((d->N + b - 1) / b);
+    p.total = tiles(b);
+    if (p.total < 256 && ktiles >= 8) {
+        int64_t s = 512 / p.total;
+        if (s > ktiles / 4) s = ktiles / 4;
+        p.k_per_split = static_cast<int>((ktiles + s - 1) / s);
+        p.splits = static_cast<int>((ktiles + p.k_per_split - 1) / p.k_per_split);
+        p.total *= p.splits;
+    }
+    return p;
+}
+
+size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc* d) {
+    const MxPlan p = plan_of(d);
+    return p.splits > 1 ? static_cast<size_t>(p.splits) * d->batch * d->M * d->N * 4 : 0;
+}
+
+template <class C, bool SPLIT>
+static loka_status tile_launch(const MxArgs& a, hipStream_t stream) {
+    const int64_t slots = C::STAGE > 40960 ? 256 : 512;
+    const uint32_t grid = static_cast<uint32_t>(a.total < slots ? a.total : slots);
+    // (on every call, a host-side table write: no process-wide state, and correct on whichever device is current)
+    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_tile_kernel<C, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * C::STAGE));
+    mx_tile_kernel<C, SPLIT><<<grid, 64 * C::NW, 2 * C::STAGE, stream>>>(a);
+    LOKA_HIP_TRY(hipGetLastError());
+    return LOKA_OK;
+}
 
 loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const uint8_t* sx, const uint8_t* wq, const uint8_t* sw,
-                              void* out_bf16, float* y, void*, size_t, hipStream_t stream) {
+                              void* out_bf16, float* y, void* ws, size_t ws_bytes, hipStream_t stream) {
     MxArgs a = args_of(d, wq, sw, out_bf16, y);
     a.xq = xq;
     a.sx = sx;
-    if (a.M <= 16) return stream_launch<1, 1, false>(a, d->batch, stream);
-    return stream_launch<2, 2, false>(a, d->batch, stream);
+    a.batch = d->batch;
+    MxPlan p = plan_of(d);
+    if (p.kind == 0 || p.total > INT32_MAX / 2) {
+        if (a.M <= 16) return stream_launch<1, 1, false>(a, d->batch, stream);
+        return stream_launch<2, 2, false>(a, d->batch, stream);
+    }
+    if (p.splits > 1 && ws_bytes < mxfp4_gemm_workspace_bytes(d)) {       // no room: unsplit
+        p.total /= p.splits;
+        p.splits = 1;
+    }
+    a.tiles_m = p.tiles_m;
+    a.tiles_n = p.tiles_n;
+    a.splits = p.splits;
+    a.k_per_split = p.k_per_split;
+    a.total = static_cast<int>(p.total);
+    a.part = static_cast<float*>(ws);
+    using Large = MxTile<4, 8, 4, 2>;
+    using Small = MxTile<4, 4, 2, 2>;
+    if (p.splits == 1) return p.kind == 2 ? tile_launch<Large, false>(a, stream) : tile_launch<Small, false>(a, stream);
+    const loka_status st = tile_launch<Small, true>(a, stream);
+    if (st != LOKA_OK) return st;
+    const int64_t per = a.M * a.N, n = per * d->batch;
+    if (n >= kMaxThreads) return LOKA_ERR_SHAPE;
+    mx_join_kernel<<<static_cast<uint32_t>((n + 255) / 256), 256, 0, stream>>>(a.part, p.splits, n, per, d->batch > 1 ? d->strideO : per, a.out, a.y);
+    LOKA_HIP_TRY(hipGetLastError());
+    return LOKA_OK;
 }
 
 bool mxfp4_linear_fused(const loka_gemm_desc* d) { return d->M <= 16; }
