@@ -10,6 +10,8 @@
 #include "gemm_common.h"
 #include "mxfp4.h"
 
+#include <type_traits>
+
 namespace loka {
 
 constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
@@ -32,11 +34,11 @@ struct MxArgs {
     __device__ __forceinline__ int first_of(int block, int grid) const { return xcd_contiguous(block, grid); }
 };
 
-template <int S>
+template <int SA, int SB>
 __device__ __forceinline__ v4f mx_mfma(const u32x4 a, const u32x4 b, v4f c, uint32_t sa, uint32_t sb) {
     const v8i A = {static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(a.z), static_cast<int>(a.w), 0, 0, 0, 0};
     const v8i B = {static_cast<int>(b.x), static_cast<int>(b.y), static_cast<int>(b.z), static_cast<int>(b.w), 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, S, static_cast<int>(sa), S, static_cast<int>(sb));
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
 }
 
 // A lane's four groups of 512 elements: codes and the word of their scale bytes.  Groups past the stored row are zero codes
@@ -125,10 +127,10 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                acc[i][j] = mx_mfma<0>(w[j].c[0], x[i].c[0], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<1>(w[j].c[1], x[i].c[1], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<2>(w[j].c[2], x[i].c[2], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<3>(w[j].c[3], x[i].c[3], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<0, 0>(w[j].c[0], x[i].c[0], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<1, 1>(w[j].c[1], x[i].c[1], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<2, 2>(w[j].c[2], x[i].c[2], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<3, 3>(w[j].c[3], x[i].c[3], acc[i][j], w[j].s, x[i].s);
             }
     }
 #pragma unroll
@@ -180,8 +182,7 @@ struct MxTile {
 };
 
 template <class C, bool SPLIT>
-__global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 2) void mx_tile_kernel(const MxArgs a) {
-    extern __shared__ __align__(16) uint8_t smem[];
+__device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wm = wave / C::WN, wn = wave % C::WN;
     const int row_bytes = static_cast<int>(a.Kp >> 1), scale_bytes = static_cast<int>(a.Kp >> 5);
@@ -233,31 +234,38 @@ __global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 
         swr = make(a.sw + ld.prob * (a.strideW >> 5) + static_cast<int64_t>(ld.n0) * scale_bytes, rows_w * scale_bytes);
     };
     aim();
-    auto request = [&](int stage) __attribute__((always_inline)) {
+    // load i of a wave's share of a K tile: X codes, W codes, X scales, W scales
+    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), LSX = C::BM / (32 * C::NW), LSW = C::BN / (32 * C::NW), LOADS = LX + LW + LSX + LSW;
+    int ld_x, ld_w, ld_s, ld_off, ld_soff;
+    auto begin_request = [&]() __attribute__((always_inline)) {
         const int kt = ld.k_first + ld_k;
         const bool tail = ragged && kt == ktiles_all - 1;           // the last K tile is half one: the other half reads zeros
-        const int xl = tail && x_chunk >= 4 ? 0x7FFFFFFF : x_lane, wl = tail && w_chunk >= 4 ? 0x7FFFFFFF : w_lane;
-        const int sl = tail && (lane & 1) ? 0x7FFFFFFF : s_lane;
+        ld_x = tail && x_chunk >= 4 ? 0x7FFFFFFF : x_lane;
+        ld_w = tail && w_chunk >= 4 ? 0x7FFFFFFF : w_lane;
+        ld_s = tail && (lane & 1) ? 0x7FFFFFFF : s_lane;
+        ld_off = wave * 8 * row_bytes + kt * 128;
+        ld_soff = wave * 32 * scale_bytes + kt * 8;
+    };
+    auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
+        if (i < LX)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + (i * C::NW + wave) * 1024), 16, ld_x,
+                                                     ld_off + i * C::NW * 8 * row_bytes, 0, 0);
+        else if (i < LX + LW)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_w,
+                                                     ld_off + (i - LX) * C::NW * 8 * row_bytes, 0, 0);
+        else if (i < LX + LW + LSX)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + ((i - LX - LW) * C::NW + wave) * 256), 4, ld_s,
+                                                     ld_soff + (i - LX - LW) * C::NW * 32 * scale_bytes, 0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + ((i - LX - LW - LSX) * C::NW + wave) * 256), 4, ld_s,
+                                                     ld_soff + (i - LX - LW - LSX) * C::NW * 32 * scale_bytes, 0, 0);
+    };
+    auto request = [&](int stage) __attribute__((always_inline)) {
+        begin_request();
 #pragma unroll
-        for (int j = 0; j < C::BM / (8 * C::NW); ++j) {
-            const int grp = j * C::NW + wave;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + grp * 1024), 16, xl, grp * 8 * row_bytes + kt * 128, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < C::BN / (8 * C::NW); ++j) {
-            const int grp = j * C::NW + wave;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + grp * 1024), 16, wl, grp * 8 * row_bytes + kt * 128, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < C::BM / (32 * C::NW); ++j) {
-            const int grp = j * C::NW + wave;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, sl, grp * 32 * scale_bytes + kt * 8, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < C::BN / (32 * C::NW); ++j) {
-            const int grp = j * C::NW + wave;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + grp * 256), 4, sl, grp * 32 * scale_bytes + kt * 8, 0, 0);
-        }
+        for (int i = 0; i < LOADS; ++i) request_one(stage, i);
+    };
+    auto advance = [&]() __attribute__((always_inline)) {
         if (++ld_k == ld.k_count) {
             ld_k = 0;
             ld_tile += gridDim.x;
@@ -266,19 +274,23 @@ __global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 
         }
     };
 
+    // (scales: two 16 x 16 tiles' pairs of bytes in a register)
     u32x4 fx[2][C::TM], fw[2][C::TN];
-    uint32_t sx[C::TM], sw[C::TN], sx_next[C::TM], sw_next[C::TN];
-    auto read = [&](int stage, int s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < C::TN; ++j) fw[s][j] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[s] + (j >> 1) * 4096 + (j & 1) * 512);
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i) fx[s][i] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[s] + i * 2048);
+    u16x2 sx[C::TM / 2], sw[C::TN / 2], sx_next[C::TM / 2], sw_next[C::TN / 2];
+    constexpr int READS = C::TM + C::TN;
+    // operand i of a half, in the order in which the half uses them
+    auto read_one = [&](int stage, int s, int i) __attribute__((always_inline)) {
+        constexpr int order = 2;               // two W tiles, two X tiles, the other W tiles, the other X tiles
+        const bool w = i < order || (i >= 2 * order && i < order + C::TN);
+        const int k = i < order ? i : i < 2 * order ? i - order : i < order + C::TN ? i - order : i - C::TN;
+        if (w) fw[s][k] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[s] + (k >> 1) * 4096 + (k & 1) * 512);
+        else fx[s][k] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[s] + k * 2048);
     };
     auto read_scales = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j) sw_next[j] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + (j >> 1) * 256 + (j & 1) * 32);
+        for (int j = 0; j < C::TN; ++j) sw_next[j >> 1][j & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + (j >> 1) * 256 + (j & 1) * 32);
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i) sx_next[i] = *reinterpret_cast<const uint16_t*>(smem + stage + sx_off + i * 128);
+        for (int i = 0; i < C::TM; ++i) sx_next[i >> 1][i & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sx_off + i * 128);
     };
     v4f acc[C::TM][C::TN];
 
@@ -286,11 +298,14 @@ __global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 
     if (tile >= total) return;
     Place at = ld;
     request(0);
+    advance();
     request(C::STAGE);
+    advance();
     int stage = 0;
     wait_vmcnt<0>();
     lds_barrier();
-    read(0, 0);
+#pragma unroll
+    for (int i = 0; i < READS; ++i) read_one(0, 0, i);
     read_scales(0);
     for (; tile < total; tile += gridDim.x) {
 #pragma unroll
@@ -299,24 +314,49 @@ __global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 
             for (int j = 0; j < C::TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
         for (int k = 0; k < at.k_count; ++k) {
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i) sx[i] = sx_next[i];
+            for (int i = 0; i < C::TM / 2; ++i) sx[i] = sx_next[i];
 #pragma unroll
-            for (int j = 0; j < C::TN; ++j) sw[j] = sw_next[j];
-            read(stage, 1);
+            for (int j = 0; j < C::TN / 2; ++j) sw[j] = sw_next[j];
+            // matrix instructions first .. last of a half
+            constexpr int MM = C::TM * C::TN;
+            auto multiply = [&](auto s_c, int first, int last) __attribute__((always_inline)) {
+                constexpr int S = decltype(s_c)::value;
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i)
+                for (int k = 0; k < MM; ++k) {
+                    if (k < first || k >= last) continue;
+                    const int i = (k / (2 * C::TN)) * 2 + ((k >> 1) & 1), j = (k % (2 * C::TN)) / 4 * 2 + (k & 1);
+                    const uint32_t a = __builtin_bit_cast(uint32_t, sw[j / 2]), b = __builtin_bit_cast(uint32_t, sx[i / 2]);
+                    if (j & 1) acc[i][j] = i & 1 ? mx_mfma<2 + S, 2 + S>(fw[S][j], fx[S][i], acc[i][j], a, b) : mx_mfma<2 + S, S>(fw[S][j], fx[S][i], acc[i][j], a, b);
+                    else acc[i][j] = i & 1 ? mx_mfma<S, 2 + S>(fw[S][j], fx[S][i], acc[i][j], a, b) : mx_mfma<S, S>(fw[S][j], fx[S][i], acc[i][j], a, b);
+                }
+            };
+            // An LDS read, or a load, between matrix instructions: a burst of them holds the issue stage up.
 #pragma unroll
-                for (int j = 0; j < C::TN; ++j) acc[i][j] = mx_mfma<0>(fw[0][j], fx[0][i], acc[i][j], sw[j], sx[i]);
+            for (int i = 0; i < READS; ++i) {
+                read_one(stage, 1, i);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(std::integral_constant<int, 0>{}, MM * i / READS, MM * (i + 1) / READS);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             wait_vmcnt<0>();                            // the next K tile has landed
             lds_barrier();                              // ... for everyone, and everyone has this one's operands
-            request(stage);
+            const int freed = stage;
             stage ^= C::STAGE;
-            read(stage, 0);
+            begin_request();
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+                multiply(std::integral_constant<int, 1>{}, MM * i / READS, MM * i / READS + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int l = LOADS * i / READS; l < LOADS * (i + 1) / READS; ++l) request_one(freed, l);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(std::integral_constant<int, 1>{}, MM * i / READS + 1, MM * (i + 1) / READS);
+                __builtin_amdgcn_sched_barrier(0);
+                read_one(stage, 0, i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             read_scales(stage);
-#pragma unroll
-            for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < C::TN; ++j) acc[i][j] = mx_mfma<1>(fw[1][j], fx[1][i], acc[i][j], sw[j], sx[i]);
+            advance();
         }
         // ---- lane (r, g) holds rows 16 i + r, columns coff_of(j) + 8 g + 0 .. 3
         const int64_t n_first = at.n0 + wn * C::TN * 16 + g * 8;
@@ -352,6 +392,12 @@ __global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 
         if (tile + static_cast<int>(gridDim.x) < total) at = locate(tile + gridDim.x);
     }
     wait_vmcnt<0>();           // the requests past the end (zeros) land before the workgroup's LDS is given on
+}
+
+template <class C, bool SPLIT>
+__global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 2) void mx_tile_kernel(const MxArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    mx_tiles<C, SPLIT>(a, smem);
 }
 
 // Sums of the partial products of a split contraction, in order.
