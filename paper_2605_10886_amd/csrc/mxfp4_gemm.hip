@@ -165,7 +165,8 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 // ---------------------------------------------------------------------------------
 // Many rows: a workgroup of WM x WN waves computes a tile of the result, each wave TM x TN tiles of 16 x 16, on K tiles of 256
 // elements (128 bytes of codes a row) that loads bring straight into LDS, two K tiles in the ring.  The 16-byte chunks of a
-// row lie permuted, chunk c at place c ^ key(row), so that the 16 rows that a quarter wave reads at once use all 64 banks.
+// row lie permuted, chunk c at place c ^ key(row): LDS serves a 16-byte read 16 lanes at a time, 8 of one g and 8 of the next
+// (rows 0 - 3, 12 - 15 and 4 - 11, or the other way round), and with key = bits 2, 1, 3 of r these use all 64 banks.
 // A lane takes groups 2 g and 2 g + 1 of a row for the K tile's two instructions, whose scale bytes are then neighbours:
 // one 16-bit LDS read for both.
 // The waves' W rows are dealt to the 16 x 16 tiles so that a lane's columns of a tile pair are 8 neighbours (coff_of).
@@ -191,16 +192,19 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     const int total = a.total;
 
     // where this wave's loads put and find things
-    const int key_x = ((wave & 1) << 2) | (lane >> 4), key_w = ((lane >> 4) & 1) | ((wave & 3) << 1);
+    const int key_x = ((wave & 1) << 2) | (((lane >> 4) & 1) << 1) | (lane >> 5);
+    const int key_w = (wave & 1) | (((lane >> 4) & 1) << 1) | ((wave & 2) << 1);
     const int x_chunk = (lane & 7) ^ key_x, w_chunk = (lane & 7) ^ key_w;
     const int x_lane = (lane >> 3) * row_bytes + x_chunk * 16, w_lane = (lane >> 3) * row_bytes + w_chunk * 16;
-    const int s_lane = (lane >> 1) * scale_bytes + (lane & 1) * 4;
+    // (scales lie in the order in which the operand tiles read them, 8 bytes a row)
+    const int sx_lane = (lane >> 1) * scale_bytes + (lane & 1) * 4;
+    const int sw_lane = (((lane >> 3) & 3) * 8 + (lane >> 5) * 4 + ((lane >> 1) & 3)) * scale_bytes + (lane & 1) * 4;
     // where it reads operands
-    const int x_at = (wm * C::TM * 16 + r) * 128, x_p = (2 * g) ^ (r >> 1);
-    const int w_row = wn * C::TN * 16 + (r >> 2) * 8 + (r & 3), w_p = (2 * g) ^ (((r >> 1) & 1) | ((r >> 2) << 1));
+    const int x_at = (wm * C::TM * 16 + r) * 128, x_p = (2 * g) ^ (((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1));
+    const int w_row = wn * C::TN * 16 + (r >> 2) * 8 + (r & 3), w_p = (2 * g) ^ (((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1));
     const int x_off[2] = {x_at + x_p * 16, x_at + (x_p ^ 1) * 16};
     const int w_off[2] = {C::OFF_W + w_row * 128 + w_p * 16, C::OFF_W + w_row * 128 + (w_p ^ 1) * 16};
-    const int sx_off = C::OFF_SX + (wm * C::TM * 16 + r) * 8 + 2 * g, sw_off = C::OFF_SW + w_row * 8 + 2 * g;
+    const int sx_off = C::OFF_SX + (wm * C::TM * 16 + r) * 8 + 2 * g, sw_off = C::OFF_SW + (wn * C::TN * 16 + r) * 8 + 2 * g;
 
     struct Place { int m0, n0, k_first, k_count, split; int64_t prob; };
     auto locate = [&](int t) __attribute__((always_inline)) {
@@ -236,13 +240,14 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     aim();
     // load i of a wave's share of a K tile: X codes, W codes, X scales, W scales
     constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), LSX = C::BM / (32 * C::NW), LSW = C::BN / (32 * C::NW), LOADS = LX + LW + LSX + LSW;
-    int ld_x, ld_w, ld_s, ld_off, ld_soff;
+    int ld_x, ld_w, ld_sx, ld_sw, ld_off, ld_soff;
     auto begin_request = [&]() __attribute__((always_inline)) {
         const int kt = ld.k_first + ld_k;
         const bool tail = ragged && kt == ktiles_all - 1;           // the last K tile is half one: the other half reads zeros
         ld_x = tail && x_chunk >= 4 ? 0x7FFFFFFF : x_lane;
         ld_w = tail && w_chunk >= 4 ? 0x7FFFFFFF : w_lane;
-        ld_s = tail && (lane & 1) ? 0x7FFFFFFF : s_lane;
+        ld_sx = tail && (lane & 1) ? 0x7FFFFFFF : sx_lane;
+        ld_sw = tail && (lane & 1) ? 0x7FFFFFFF : sw_lane;
         ld_off = wave * 8 * row_bytes + kt * 128;
         ld_soff = wave * 32 * scale_bytes + kt * 8;
     };
@@ -254,10 +259,10 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_w,
                                                      ld_off + (i - LX) * C::NW * 8 * row_bytes, 0, 0);
         else if (i < LX + LW + LSX)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + ((i - LX - LW) * C::NW + wave) * 256), 4, ld_s,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + ((i - LX - LW) * C::NW + wave) * 256), 4, ld_sx,
                                                      ld_soff + (i - LX - LW) * C::NW * 32 * scale_bytes, 0, 0);
         else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + ((i - LX - LW - LSX) * C::NW + wave) * 256), 4, ld_s,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + ((i - LX - LW - LSX) * C::NW + wave) * 256), 4, ld_sw,
                                                      ld_soff + (i - LX - LW - LSX) * C::NW * 32 * scale_bytes, 0, 0);
     };
     auto request = [&](int stage) __attribute__((always_inline)) {
@@ -288,7 +293,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     };
     auto read_scales = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j) sw_next[j >> 1][j & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + (j >> 1) * 256 + (j & 1) * 32);
+        for (int j = 0; j < C::TN; ++j) sw_next[j >> 1][j & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + j * 128);
 #pragma unroll
         for (int i = 0; i < C::TM; ++i) sx_next[i >> 1][i & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sx_off + i * 128);
     };
