@@ -30,6 +30,7 @@ struct MxArgs {
     int64_t batch;
     int tiles_m, tiles_n, splits, k_per_split, total;
     float* part;                       // [splits][batch][M][N]
+    bool wide;                         // rows of whole 16-byte runs, a tile's within 32-bit offsets
     // every XCD starts on consecutive tiles, which share operands
     __device__ __forceinline__ int first_of(int block, int grid) const { return xcd_contiguous(block, grid); }
 };
@@ -163,48 +164,54 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 }
 
 // ---------------------------------------------------------------------------------
-// Many rows: a workgroup of WM x WN waves computes a tile of the result, each wave TM x TN tiles of 16 x 16, on K tiles of 256
-// elements (128 bytes of codes a row) that loads bring straight into LDS, two K tiles in the ring.  The 16-byte chunks of a
+// Many rows: a workgroup of WM x WN x WK waves computes a tile of the result, each wave TM x TN tiles of 16 x 16, on K tiles of
+// 256 elements (128 bytes of codes a row) that loads bring straight into LDS, R of them in a ring.  The 16-byte chunks of a
 // row lie permuted, chunk c at place c ^ key(row): LDS serves a 16-byte read 16 lanes at a time, 8 of one g and 8 of the next
 // (rows 0 - 3, 12 - 15 and 4 - 11, or the other way round), and with key = bits 2, 1, 3 of r these use all 64 banks.
-// A lane takes groups 2 g and 2 g + 1 of a row for the K tile's two instructions, whose scale bytes are then neighbours:
-// one 16-bit LDS read for both.
+// A lane takes groups 2 g and 2 g + 1 of a row for the two instructions of a K tile (halves s = 0, 1), whose scale bytes are
+// then neighbours: one 16-bit LDS read for both.  WK = 1: a wave multiplies both halves; WK = 2: its own half of every
+// K tile, and two waves add up at the end (two waves on a SIMD where the tile gives only four).
 // The waves' W rows are dealt to the 16 x 16 tiles so that a lane's columns of a tile pair are 8 neighbours (coff_of).
 //
-// One barrier a K tile: its second half's operands are in registers when the barrier is passed, so the loads of the K tile
-// after next may go where this one lay, and the first operands of the next K tile are read behind the second half's matrix
-// instructions.  Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first K
-// tiles arrive while this one's values are stored.
-template <int TM_, int TN_, int WM_, int WN_>
+// One barrier a K tile: its last operands are in registers when the barrier is passed, so the loads of a K tile R further on
+// may go where this one lay, and the first operands of the next K tile are read between the matrix instructions that follow.
+// Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first K tiles arrive
+// while this one's values are stored, and nothing waits for the stores where their number is known (see `late`).
+template <int TM_, int TN_, int WM_, int WN_, int WK_, int R_>
 struct MxTile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WK = WK_, R = R_, NW = WM * WN * WK, BM = WM * TM * 16, BN = WN * TN * 16;
     static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 8, STAGE = OFF_SW + BN * 8;
-    static_assert(NW % 4 == 0 && BM % (32 * NW) == 0 && BN % (32 * NW) == 0 && TN % 2 == 0);
+    static constexpr int XCH = WM * WN * 64 * TN * 16;              // WK = 2: one row of 16 x 16 tiles of every wave
+    static constexpr int LDS = R * STAGE + (WK == 2 ? 2 * XCH : 0), PER_CU = 163840 / LDS;
+    static_assert(NW % 4 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (BM + BN) % (32 * NW) == 0 && TM % 2 == 0 && TN % 2 == 0);
+    static_assert(WK == 1 || (WK == 2 && TM == 4));
 };
 
 template <class C, bool SPLIT>
 __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
+    constexpr int TM = C::TM, TN = C::TN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int wm = wave / C::WN, wn = wave % C::WN;
+    const int kg = C::WK == 2 ? wave / (C::WM * C::WN) : 0, wmn = C::WK == 2 ? wave % (C::WM * C::WN) : wave;
+    const int wm = wmn / C::WN, wn = wmn % C::WN;
     const int row_bytes = static_cast<int>(a.Kp >> 1), scale_bytes = static_cast<int>(a.Kp >> 5);
     const int ktiles_all = static_cast<int>((a.Kp + 255) >> 8);
     const bool ragged = (a.Kp & 255) != 0;
     const int total = a.total;
 
-    // where this wave's loads put and find things
+    // where this wave's loads put and find things (8 rows a load, every NW-th group of them)
     const int key_x = ((wave & 1) << 2) | (((lane >> 4) & 1) << 1) | (lane >> 5);
     const int key_w = (wave & 1) | (((lane >> 4) & 1) << 1) | ((wave & 2) << 1);
     const int x_chunk = (lane & 7) ^ key_x, w_chunk = (lane & 7) ^ key_w;
     const int x_lane = (lane >> 3) * row_bytes + x_chunk * 16, w_lane = (lane >> 3) * row_bytes + w_chunk * 16;
-    // (scales lie in the order in which the operand tiles read them, 8 bytes a row)
+    // (scales, 8 bytes a row, lie in the order in which the operand tiles read them: on neighbouring banks)
     const int sx_lane = (lane >> 1) * scale_bytes + (lane & 1) * 4;
     const int sw_lane = (((lane >> 3) & 3) * 8 + (lane >> 5) * 4 + ((lane >> 1) & 3)) * scale_bytes + (lane & 1) * 4;
     // where it reads operands
-    const int x_at = (wm * C::TM * 16 + r) * 128, x_p = (2 * g) ^ (((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1));
-    const int w_row = wn * C::TN * 16 + (r >> 2) * 8 + (r & 3), w_p = (2 * g) ^ (((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1));
-    const int x_off[2] = {x_at + x_p * 16, x_at + (x_p ^ 1) * 16};
-    const int w_off[2] = {C::OFF_W + w_row * 128 + w_p * 16, C::OFF_W + w_row * 128 + (w_p ^ 1) * 16};
-    const int sx_off = C::OFF_SX + (wm * C::TM * 16 + r) * 8 + 2 * g, sw_off = C::OFF_SW + (wn * C::TN * 16 + r) * 8 + 2 * g;
+    const int key_r = ((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1), at_p = ((2 * g) ^ key_r) * 16;
+    const int x_at = (wm * TM * 16 + r) * 128, w_at = C::OFF_W + (wn * TN * 16 + (r >> 2) * 8 + (r & 3)) * 128;
+    const int first_p = kg ? at_p ^ 16 : at_p;             // (of the wave's own half, WK = 2)
+    const int x_off[2] = {x_at + first_p, x_at + (at_p ^ 16)}, w_off[2] = {w_at + first_p, w_at + (at_p ^ 16)};
+    const int sx_off = C::OFF_SX + (wm * TM * 16 + r) * 8 + 2 * g + kg, sw_off = C::OFF_SW + (wn * TN * 16 + r) * 8 + 2 * g + kg;
 
     struct Place { int m0, n0, k_first, k_count, split; int64_t prob; };
     auto locate = [&](int t) __attribute__((always_inline)) {
@@ -222,13 +229,14 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         return p;
     };
 
-    // ---- the stream of K tiles: `ld_*` is the next one to request
+    // ---- the stream of K tiles: `ld` is the next one to request
     int ld_tile = a.first_of(blockIdx.x, gridDim.x), ld_k = 0;
-    Place ld = locate(ld_tile < total ? ld_tile : 0);
+    if (ld_tile >= total) return;
+    Place ld = locate(ld_tile);
     __amdgpu_buffer_rsrc_t xr, wr, sxr, swr;
     auto aim = [&]() __attribute__((always_inline)) {
         const int64_t rows_x = a.M - ld.m0 < C::BM ? a.M - ld.m0 : C::BM, rows_w = a.N - ld.n0 < C::BN ? a.N - ld.n0 : C::BN;
-        const bool on = ld_tile < total;
+        const bool on = ld_tile < total;                   // (past the end: zeros, so that every K tile requests as many loads)
         auto make = [&](const uint8_t* base, int64_t bytes) __attribute__((always_inline)) {
             return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, on ? static_cast<int>(bytes) : 0, 0x00020000);
         };
@@ -238,8 +246,8 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         swr = make(a.sw + ld.prob * (a.strideW >> 5) + static_cast<int64_t>(ld.n0) * scale_bytes, rows_w * scale_bytes);
     };
     aim();
-    // load i of a wave's share of a K tile: X codes, W codes, X scales, W scales
-    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), LSX = C::BM / (32 * C::NW), LSW = C::BN / (32 * C::NW), LOADS = LX + LW + LSX + LSW;
+    // load i of a wave's share of a K tile: X codes, W codes, scales of X, then of W
+    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), LS = (C::BM + C::BN) / (32 * C::NW), LOADS = LX + LW + LS;
     int ld_x, ld_w, ld_sx, ld_sw, ld_off, ld_soff;
     auto begin_request = [&]() __attribute__((always_inline)) {
         const int kt = ld.k_first + ld_k;
@@ -249,26 +257,24 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         ld_sx = tail && (lane & 1) ? 0x7FFFFFFF : sx_lane;
         ld_sw = tail && (lane & 1) ? 0x7FFFFFFF : sw_lane;
         ld_off = wave * 8 * row_bytes + kt * 128;
-        ld_soff = wave * 32 * scale_bytes + kt * 8;
+        ld_soff = kt * 8;
     };
     auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
-        if (i < LX)
+        if (i < LX) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + (i * C::NW + wave) * 1024), 16, ld_x,
                                                      ld_off + i * C::NW * 8 * row_bytes, 0, 0);
-        else if (i < LX + LW)
+        } else if (i < LX + LW) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_w,
                                                      ld_off + (i - LX) * C::NW * 8 * row_bytes, 0, 0);
-        else if (i < LX + LW + LSX)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + ((i - LX - LW) * C::NW + wave) * 256), 4, ld_sx,
-                                                     ld_soff + (i - LX - LW) * C::NW * 32 * scale_bytes, 0, 0);
-        else
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SW + ((i - LX - LW - LSX) * C::NW + wave) * 256), 4, ld_sw,
-                                                     ld_soff + (i - LX - LW - LSX) * C::NW * 32 * scale_bytes, 0, 0);
-    };
-    auto request = [&](int stage) __attribute__((always_inline)) {
-        begin_request();
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) request_one(stage, i);
+        } else {                                           // 32 rows a load: those of X first, then those of W
+            const int grp = (i - LX - LW) * C::NW + wave;
+            if (grp < C::BM / 32)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, ld_sx,
+                                                         ld_soff + grp * 32 * scale_bytes, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(swr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, ld_sw,
+                                                         ld_soff + (grp - C::BM / 32) * 32 * scale_bytes, 0, 0);
+        }
     };
     auto advance = [&]() __attribute__((always_inline)) {
         if (++ld_k == ld.k_count) {
@@ -279,119 +285,179 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         }
     };
 
-    // (scales: two 16 x 16 tiles' pairs of bytes in a register)
-    u32x4 fx[2][C::TM], fw[2][C::TN];
-    u16x2 sx[C::TM / 2], sw[C::TN / 2], sx_next[C::TM / 2], sw_next[C::TN / 2];
-    constexpr int READS = C::TM + C::TN;
-    // operand i of a half, in the order in which the half uses them
-    auto read_one = [&](int stage, int s, int i) __attribute__((always_inline)) {
-        constexpr int order = 2;               // two W tiles, two X tiles, the other W tiles, the other X tiles
-        const bool w = i < order || (i >= 2 * order && i < order + C::TN);
-        const int k = i < order ? i : i < 2 * order ? i - order : i < order + C::TN ? i - order : i - C::TN;
-        if (w) fw[s][k] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[s] + (k >> 1) * 4096 + (k & 1) * 512);
-        else fx[s][k] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[s] + k * 2048);
+    // ---- operands: two sets; scales: two 16 x 16 tiles' bytes in a register
+    constexpr int READS = TM + TN, MM = TM * TN;
+    u32x4 fx[2][TM], fw[2][TN];
+    u16x2 sx[TM / 2], sw[TN / 2];
+    // operand i of half `half` into set `set`, in the order in which they are used: two W tiles, two X tiles, the other W, the other X
+    auto read_one = [&](int stage, int set, int half, int i) __attribute__((always_inline)) {
+        const bool w = i < 2 || (i >= 4 && i < 2 + TN);
+        const int k = i < 2 ? i : i < 4 ? i - 2 : i < 2 + TN ? i - 2 : i - TN;
+        if (w) fw[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[half] + (k >> 1) * 4096 + (k & 1) * 512);
+        else fx[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[half] + k * 2048);
     };
     auto read_scales = [&](int stage) __attribute__((always_inline)) {
+        auto one = [&](const uint8_t* p) __attribute__((always_inline)) {
+            return C::WK == 2 ? static_cast<uint16_t>(*p) : *reinterpret_cast<const uint16_t*>(p);
+        };
 #pragma unroll
-        for (int j = 0; j < C::TN; ++j) sw_next[j >> 1][j & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sw_off + j * 128);
+        for (int j = 0; j < TN; ++j) sw[j >> 1][j & 1] = one(smem + stage + sw_off + j * 128);
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i) sx_next[i >> 1][i & 1] = *reinterpret_cast<const uint16_t*>(smem + stage + sx_off + i * 128);
+        for (int i = 0; i < TM; ++i) sx[i >> 1][i & 1] = one(smem + stage + sx_off + i * 128);
     };
-    v4f acc[C::TM][C::TN];
-
-    int tile = ld_tile;
-    if (tile >= total) return;
+    v4f acc[TM][TN];
+    // matrix instructions first .. last - 1 of the operands in a set
+    auto multiply = [&](auto set_c, int first, int last) __attribute__((always_inline)) {
+        constexpr int SET = decltype(set_c)::value, S = C::WK == 1 ? SET : 0;      // S: the scale's byte
+#pragma unroll
+        for (int k = 0; k < MM; ++k) {
+            if (k < first || k >= last) continue;
+            const int i = (k / (2 * TN)) * 2 + ((k >> 1) & 1), j = (k % (2 * TN)) / 4 * 2 + (k & 1);
+            const uint32_t a_ = __builtin_bit_cast(uint32_t, sw[j / 2]), b_ = __builtin_bit_cast(uint32_t, sx[i / 2]);
+            if (j & 1) acc[i][j] = i & 1 ? mx_mfma<2 + S, 2 + S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_) : mx_mfma<2 + S, S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_);
+            else acc[i][j] = i & 1 ? mx_mfma<S, 2 + S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_) : mx_mfma<S, S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_);
+        }
+    };
+    int tile = ld_tile, stage = 0;
     Place at = ld;
-    request(0);
-    advance();
-    request(C::STAGE);
-    advance();
-    int stage = 0;
-    wait_vmcnt<0>();
+    for (int k = 0; k < C::R; ++k) {
+        begin_request();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) request_one(k * C::STAGE, i);
+        advance();
+    }
+    wait_vmcnt<(C::R - 1) * LOADS>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read_one(0, 0, i);
+    for (int i = 0; i < READS; ++i) read_one(0, 0, 0, i);
     read_scales(0);
+    // Where a tile's values left in STORES stores, the loads of the K tiles that were requested before them are awaited with the
+    // stores in flight: `late` K tiles from there.
+    constexpr int STORES = TM * TN / 2 / C::WK, NEWER = (C::R - 2) * LOADS;
+    static_assert(NEWER + STORES <= 63);
+    int late = 0;
+
+    // The matrix instructions of one set, and between them (a burst would hold the issue stage up) the LDS reads of the next
+    // operands and, where a K tile ends, the loads into the place that it leaves.
+    auto halves = [&]() __attribute__((always_inline)) {        // WK = 1, the first half
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            read_one(stage, 1, 1, i);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(std::integral_constant<int, 0>{}, MM * i / READS, MM * (i + 1) / READS);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto finish = [&](auto set_c) __attribute__((always_inline)) {
+        constexpr int SET = decltype(set_c)::value;
+        if (late > 0) { --late; wait_vmcnt<NEWER + STORES>(); }
+        else wait_vmcnt<NEWER>();                               // the next K tile has landed
+        lds_barrier();                                          // ... for everyone, and everyone has this one's operands
+        const int freed = stage;
+        stage = stage + C::STAGE == C::R * C::STAGE ? 0 : stage + C::STAGE;
+        begin_request();
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            multiply(set_c, MM * i / READS, MM * i / READS + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int l = LOADS * i / READS; l < LOADS * (i + 1) / READS; ++l) request_one(freed, l);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(set_c, MM * i / READS + 1, MM * (i + 1) / READS);
+            __builtin_amdgcn_sched_barrier(0);
+            read_one(stage, C::WK == 2 ? SET ^ 1 : 0, 0, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        read_scales(stage);
+        advance();
+    };
+
     for (; tile < total; tile += gridDim.x) {
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < C::TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < at.k_count; ++k) {
-#pragma unroll
-            for (int i = 0; i < C::TM / 2; ++i) sx[i] = sx_next[i];
-#pragma unroll
-            for (int j = 0; j < C::TN / 2; ++j) sw[j] = sw_next[j];
-            // matrix instructions first .. last of a half
-            constexpr int MM = C::TM * C::TN;
-            auto multiply = [&](auto s_c, int first, int last) __attribute__((always_inline)) {
-                constexpr int S = decltype(s_c)::value;
-#pragma unroll
-                for (int k = 0; k < MM; ++k) {
-                    if (k < first || k >= last) continue;
-                    const int i = (k / (2 * C::TN)) * 2 + ((k >> 1) & 1), j = (k % (2 * C::TN)) / 4 * 2 + (k & 1);
-                    const uint32_t a = __builtin_bit_cast(uint32_t, sw[j / 2]), b = __builtin_bit_cast(uint32_t, sx[i / 2]);
-                    if (j & 1) acc[i][j] = i & 1 ? mx_mfma<2 + S, 2 + S>(fw[S][j], fx[S][i], acc[i][j], a, b) : mx_mfma<2 + S, S>(fw[S][j], fx[S][i], acc[i][j], a, b);
-                    else acc[i][j] = i & 1 ? mx_mfma<S, 2 + S>(fw[S][j], fx[S][i], acc[i][j], a, b) : mx_mfma<S, S>(fw[S][j], fx[S][i], acc[i][j], a, b);
-                }
-            };
-            // An LDS read, or a load, between matrix instructions: a burst of them holds the issue stage up.
-#pragma unroll
-            for (int i = 0; i < READS; ++i) {
-                read_one(stage, 1, i);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(std::integral_constant<int, 0>{}, MM * i / READS, MM * (i + 1) / READS);
-                __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+        if constexpr (C::WK == 1) {
+            for (int k = 0; k < at.k_count; ++k) {
+                halves();
+                finish(std::integral_constant<int, 1>{});
             }
-            wait_vmcnt<0>();                            // the next K tile has landed
-            lds_barrier();                              // ... for everyone, and everyone has this one's operands
-            const int freed = stage;
-            stage ^= C::STAGE;
-            begin_request();
-#pragma unroll
-            for (int i = 0; i < READS; ++i) {
-                multiply(std::integral_constant<int, 1>{}, MM * i / READS, MM * i / READS + 1);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int l = LOADS * i / READS; l < LOADS * (i + 1) / READS; ++l) request_one(freed, l);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(std::integral_constant<int, 1>{}, MM * i / READS + 1, MM * (i + 1) / READS);
-                __builtin_amdgcn_sched_barrier(0);
-                read_one(stage, 0, i);
-                __builtin_amdgcn_sched_barrier(0);
+        } else {
+            for (int k = 0; k + 1 < at.k_count; k += 2) {
+                finish(std::integral_constant<int, 0>{});
+                finish(std::integral_constant<int, 1>{});
             }
-            read_scales(stage);
-            advance();
+            if (at.k_count & 1) {                               // the next tile starts on set 0 again
+                finish(std::integral_constant<int, 0>{});
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fx[0][i] = fx[1][i];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fw[0][j] = fw[1][j];
+            }
+            // the two halves' sums: wave (kg) keeps rows 2 kg, 2 kg + 1 of its 16 x 16 tiles, and hands the others over
+            v4f* const mine = reinterpret_cast<v4f*>(smem + C::R * C::STAGE + kg * C::XCH) + wmn * 64 + lane;
+            const v4f* const theirs = reinterpret_cast<const v4f*>(smem + C::R * C::STAGE + (kg ^ 1) * C::XCH) + wmn * 64 + lane;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) mine[j * (C::WM * C::WN * 64)] = kg ? acc[i][j] : acc[2 + i][j];
+                lds_barrier();
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = (kg ? acc[2 + i][j] : acc[i][j]) + theirs[j * (C::WM * C::WN * 64)];
+                if (i == 0) lds_barrier();
+            }
         }
         // ---- lane (r, g) holds rows 16 i + r, columns coff_of(j) + 8 g + 0 .. 3
-        const int64_t n_first = at.n0 + wn * C::TN * 16 + g * 8;
+        constexpr int ROWS = TM / C::WK;
+        const int m_wave = (wm * TM + kg * ROWS) * 16, n_wave = wn * TN * 16;
         float* const y = SPLIT ? a.part + (static_cast<int64_t>(at.split) * a.batch + at.prob) * a.M * a.N : a.y ? a.y + at.prob * a.strideO : nullptr;
         uint16_t* const out = SPLIT || !a.out ? nullptr : a.out + at.prob * a.strideO;
-        const bool wide = (a.N & 7) == 0;
+        const int el = lane_id(), er = el & 15, eg = el >> 4;       // (not kept through the loop, nor what follows from them)
+        if (a.wide) {                  // whole runs of 8 columns, 32-bit offsets in a tile's rows; what is past the result is dropped
+            const int64_t rows = a.M - at.m0 < C::BM ? a.M - at.m0 : C::BM;
+            const int N = static_cast<int>(a.N), n_lane = at.n0 + n_wave + eg * 8, o_lane = (m_wave + er) * N + n_lane;
+            // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
+            // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
+            if (out) {
+                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000);
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i) {
-            const int64_t m = at.m0 + (wm * C::TM + i) * 16 + r;
-            if (m < a.M) {
+                for (int j = 0; j < TN; j += 2) {
+                    const bool in = n_lane + j * 16 < N;
 #pragma unroll
-                for (int j = 0; j < C::TN; j += 2) {
-                    const int64_t n = n_first + j * 16, o = m * a.N + n;
-                    const v4f lo = acc[i][j], hi = acc[i][j + 1];
-                    if (wide && n < a.N) {
-                        if (out) *reinterpret_cast<u32x4*>(out + o) = u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)};
-                        if (y) {
-                            *reinterpret_cast<v4f*>(y + o) = lo;
-                            *reinterpret_cast<v4f*>(y + o + 4) = hi;
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (n + e < a.N) {
-                                const float v = e < 4 ? lo[e & 3] : hi[e & 3];
-                                if (out) out[o + e] = static_cast<uint16_t>(f32_to_bf16_rne(v));
-                                if (y) y[o + e] = v;
-                            }
+                    for (int i = 0; i < ROWS; ++i) {
+                        const v4f lo = acc[i][j], hi = acc[i][j + 1];
+                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)},
+                                                               o, in ? (o_lane + i * 16 * N + j * 16) * 2 : 0x7FFFFFFF, 0, 0);
                     }
                 }
+            }
+            if (y) {
+                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(y + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 4), 0x00020000);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int n = (j >> 1) * 32 + (j & 1) * 4;
+                    const bool in = n_lane + n < N;
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i)
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), o, in ? (o_lane + i * 16 * N + n) * 4 : 0x7FFFFFFF, 0, 0);
+                }
+            }
+            late = out && !y ? C::R - 1 : 0;
+        } else {
+            late = 0;
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const int64_t m = at.m0 + m_wave + i * 16 + er;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t n = at.n0 + n_wave + eg * 8 + (j >> 1) * 32 + (j & 1) * 4 + e, o = m * a.N + n;
+                        if (m < a.M && n < a.N) {
+                            if (out) out[o] = static_cast<uint16_t>(f32_to_bf16_rne(acc[i][j][e]));
+                            if (y) y[o] = acc[i][j][e];
+                        }
+                    }
             }
         }
         if (tile + static_cast<int>(gridDim.x) < total) at = locate(tile + gridDim.x);
@@ -400,7 +466,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
 }
 
 template <class C, bool SPLIT>
-__global__ __launch_bounds__(64 * C::NW, C::STAGE > 40960 ? C::NW / 4 : C::NW / 2) void mx_tile_kernel(const MxArgs a) {
+__global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void mx_tile_kernel(const MxArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     mx_tiles<C, SPLIT>(a, smem);
 }
@@ -473,11 +539,11 @@ size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc* d) {
 
 template <class C, bool SPLIT>
 static loka_status tile_launch(const MxArgs& a, hipStream_t stream) {
-    const int64_t slots = C::STAGE > 40960 ? 256 : 512;
+    const int64_t slots = 256 * C::PER_CU;
     const uint32_t grid = static_cast<uint32_t>(a.total < slots ? a.total : slots);
     // (on every call, a host-side table write: no process-wide state, and correct on whichever device is current)
-    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_tile_kernel<C, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * C::STAGE));
-    mx_tile_kernel<C, SPLIT><<<grid, 64 * C::NW, 2 * C::STAGE, stream>>>(a);
+    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_tile_kernel<C, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS));
+    mx_tile_kernel<C, SPLIT><<<grid, 64 * C::NW, C::LDS, stream>>>(a);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }
@@ -503,8 +569,9 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     a.k_per_split = p.k_per_split;
     a.total = static_cast<int>(p.total);
     a.part = static_cast<float*>(ws);
-    using Large = MxTile<4, 8, 4, 2>;
-    using Small = MxTile<4, 4, 2, 2>;
+    a.wide = a.N % 8 == 0 && a.N < (INT64_C(1) << 21);
+    using Large = MxTile<4, 8, 4, 2, 1, 2>;
+    using Small = MxTile<4, 4, 2, 2, 2, 3>;
     if (p.splits == 1) return p.kind == 2 ? tile_launch<Large, false>(a, stream) : tile_launch<Small, false>(a, stream);
     const loka_status st = tile_launch<Small, true>(a, stream);
     if (st != LOKA_OK) return st;
