@@ -10,6 +10,7 @@
 #include "gemm_common.h"
 #include "mxfp4.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace loka {
@@ -183,7 +184,7 @@ struct MxTile {
     static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 8, STAGE = OFF_SW + BN * 8;
     static constexpr int XCH = WM * WN * 64 * TN * 16;              // WK = 2: one row of 16 x 16 tiles of every wave
     static constexpr int LDS = R * STAGE + (WK == 2 ? 2 * XCH : 0), PER_CU = 163840 / LDS;
-    static_assert(NW % 4 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (BM + BN) % (32 * NW) == 0 && TM % 2 == 0 && TN % 2 == 0);
+    static_assert(NW % 4 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 32 == 0 && BN % 32 == 0 && TM % 2 == 0 && TN % 2 == 0);
     static_assert(WK == 1 || (WK == 2 && TM == 4));
 };
 
@@ -247,7 +248,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     };
     aim();
     // load i of a wave's share of a K tile: X codes, W codes, scales of X, then of W
-    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), LS = (C::BM + C::BN) / (32 * C::NW), LOADS = LX + LW + LS;
+    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), SROWS = (C::BM + C::BN) / 32, LS = (SROWS + C::NW - 1) / C::NW, LOADS = LX + LW + LS;
     int ld_x, ld_w, ld_sx, ld_sw, ld_off, ld_soff;
     auto begin_request = [&]() __attribute__((always_inline)) {
         const int kt = ld.k_first + ld_k;
@@ -266,8 +267,8 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         } else if (i < LX + LW) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_w,
                                                      ld_off + (i - LX) * C::NW * 8 * row_bytes, 0, 0);
-        } else {                                           // 32 rows a load: those of X first, then those of W
-            const int grp = (i - LX - LW) * C::NW + wave;
+        } else {                                           // 32 rows a load: those of X first, then those of W (a load too many repeats one)
+            const int at_ = (i - LX - LW) * C::NW + wave, grp = at_ < SROWS ? at_ : at_ - SROWS;
             if (grp < C::BM / 32)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, ld_sx,
                                                          ld_soff + grp * 32 * scale_bytes, 0, 0);
@@ -494,6 +495,23 @@ static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
     return LOKA_OK;
 }
 
+// Rows and columns of a workgroup: as many rows as there are (up to 64), and as many columns as leave a workgroup for every CU,
+// since each reads (and, fused, quantizes) all of x.
+template <bool FUSED>
+static loka_status stream_any(const MxArgs& a, int64_t batch, hipStream_t stream) {
+    const int64_t runs = (a.N + 15) / 16 * batch;          // of 16 columns
+    if (a.M <= 16) {
+        if (runs >= 1024) return stream_launch<1, 4, FUSED>(a, batch, stream);
+        if (runs >= 512) return stream_launch<1, 2, FUSED>(a, batch, stream);
+        return stream_launch<1, 1, FUSED>(a, batch, stream);
+    }
+    if constexpr (FUSED) return LOKA_ERR_UNSUPPORTED;
+    else {
+        if (a.M <= 32) return runs >= 512 ? stream_launch<2, 2, false>(a, batch, stream) : stream_launch<2, 1, false>(a, batch, stream);
+        return runs >= 512 ? stream_launch<4, 2, false>(a, batch, stream) : stream_launch<4, 1, false>(a, batch, stream);
+    }
+}
+
 static MxArgs args_of(const loka_gemm_desc* d, const uint8_t* wq, const uint8_t* sw, void* out_bf16, float* y) {
     MxArgs a{};
     a.wq = wq;
@@ -510,25 +528,44 @@ static MxArgs args_of(const loka_gemm_desc* d, const uint8_t* wq, const uint8_t*
     return a;
 }
 
-// What runs a product: the stream kernel for few rows, else tiles of 128 x 128, or 256 x 256 where these fill the chip
-struct MxPlan { int kind; int tiles_m, tiles_n, splits, k_per_split; int64_t total; };
+// What runs a product: the stream kernel for up to 64 rows, else the tile kernel in the form expected to be fastest, and in how
+// many ranges of K tiles.  The estimates are microseconds fitted to measured launches (measured / estimated): a result tile
+// costs its form a fixed part and a part per K tile, times the rounds in which the chip takes them.
+//   256 x 256            8192 x 8192 x 8192 295 / 294, 4096 x 4096 x 4096 43.5 / 43, 16384 x 4096 x 1024 60 / 60
+//   128 x 128, K halves  8192 x 8192 x 8192 417 / 415, 4096 x 4096 x 4096 59 / 59, 1024 x 4096 x 16384 53.5 / 53, 2048^3 11.8 / 11.9
+//   128 x 128, 4 waves   4096 x 4096 x 4096 53 / 53, 2048^3 11.5 / 11.5, 5013 x 720 x 1008 8.0 / 8.0, 2048 x 768 x 256 6.0 / 5.4
+enum { MX_STREAM = 0, MX_LARGE = 1, MX_HALVES = 2, MX_SMALL = 3 };
+struct MxPlan { int kind, tiles_m, tiles_n, splits, k_per_split; int64_t total; };
 static MxPlan plan_of(const loka_gemm_desc* d) {
-    MxPlan p{0, 0, 0, 1, 0, 0};
-    const int64_t Kp = mx_padded(d->K), ktiles = (Kp + 255) / 256;
-    if (d->M <= 32 || Kp >= (INT64_C(1) << 23)) return p;
-    auto tiles = [&](int64_t b) { return ((d->M + b - 1) / b) * ((d->N + b - 1) / b) * d->batch; };
-    p.kind = tiles(256) >= 256 ? 2 : 1;
-    const int b = p.kind == 2 ? 256 : 128;
+    MxPlan p{MX_STREAM, 0, 0, 1, 0, 0};
+    const int64_t Kp = mx_padded(d->K), k = (Kp + 255) / 256;
+    if (d->M <= 64 || Kp >= (INT64_C(1) << 23)) return p;              // (a tile's rows within 32-bit offsets)
+    auto tiles = [&](int64_t b) { return static_cast<double>((d->M + b - 1) / b) * static_cast<double>((d->N + b - 1) / b) * static_cast<double>(d->batch); };
+    auto rounds = [](double t, double slots) { return std::ceil(t / slots); };
+    const double t256 = tiles(256), t128 = tiles(128), bytes = static_cast<double>(d->M) * static_cast<double>(d->N) * static_cast<double>(d->batch) * 8.0;
+    if (t128 > 1e9) return p;
+    double best = 4.0 + rounds(t256, 256) * (5.5 + 2.1 * static_cast<double>(k));
+    p.kind = MX_LARGE;
+    const double small = t128 <= 256 ? 4.5 + 0.88 * static_cast<double>(k) : 4.5 + rounds(t128, 512) * (1.0 + 1.45 * static_cast<double>(k));
+    if (small < best) {
+        best = small;
+        p.kind = MX_SMALL;
+    }
+    for (int64_t s = 1; s <= 64 && s <= k && (s == 1 || static_cast<double>(s) * t128 <= 1024); s *= 2) {
+        const double per = std::ceil(static_cast<double>(k) / static_cast<double>(s));
+        const double us = 4.0 + rounds(t128 * static_cast<double>(s), 256) * (2.0 + 0.74 * per) + (s > 1 ? 3.0 + bytes * static_cast<double>(s) / 4.5e6 : 0.0);
+        if (us < best) {
+            best = us;
+            p.kind = MX_HALVES;
+            p.splits = static_cast<int>(s);
+        }
+    }
+    const int b = p.kind == MX_LARGE ? 256 : 128;
     p.tiles_m = static_cast<int>((d->M + b - 1) / b);
     p.tiles_n = static_cast<int>((d->N + b - 1) / b);
-    p.total = tiles(b);
-    if (p.total < 256 && ktiles >= 8) {
-        int64_t s = 512 / p.total;
-        if (s > ktiles / 4) s = ktiles / 4;
-        p.k_per_split = static_cast<int>((ktiles + s - 1) / s);
-        p.splits = static_cast<int>((ktiles + p.k_per_split - 1) / p.k_per_split);
-        p.total *= p.splits;
-    }
+    p.k_per_split = static_cast<int>((k + p.splits - 1) / p.splits);
+    p.splits = static_cast<int>((k + p.k_per_split - 1) / p.k_per_split);
+    p.total = static_cast<int64_t>(tiles(b)) * p.splits;
     return p;
 }
 
@@ -555,10 +592,7 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     a.sx = sx;
     a.batch = d->batch;
     MxPlan p = plan_of(d);
-    if (p.kind == 0 || p.total > INT32_MAX / 2) {
-        if (a.M <= 16) return stream_launch<1, 1, false>(a, d->batch, stream);
-        return stream_launch<2, 2, false>(a, d->batch, stream);
-    }
+    if (p.kind == MX_STREAM) return stream_any<false>(a, d->batch, stream);
     if (p.splits > 1 && ws_bytes < mxfp4_gemm_workspace_bytes(d)) {       // no room: unsplit
         p.total /= p.splits;
         p.splits = 1;
@@ -571,9 +605,12 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     a.part = static_cast<float*>(ws);
     a.wide = a.N % 8 == 0 && a.N < (INT64_C(1) << 21);
     using Large = MxTile<4, 8, 4, 2, 1, 2>;
-    using Small = MxTile<4, 4, 2, 2, 2, 3>;
-    if (p.splits == 1) return p.kind == 2 ? tile_launch<Large, false>(a, stream) : tile_launch<Small, false>(a, stream);
-    const loka_status st = tile_launch<Small, true>(a, stream);
+    using Halves = MxTile<4, 4, 2, 2, 2, 3>;
+    using Small = MxTile<4, 4, 2, 2, 1, 2>;
+    if (p.kind == MX_LARGE) return tile_launch<Large, false>(a, stream);
+    if (p.kind == MX_SMALL) return tile_launch<Small, false>(a, stream);
+    if (p.splits == 1) return tile_launch<Halves, false>(a, stream);
+    const loka_status st = tile_launch<Halves, true>(a, stream);
     if (st != LOKA_OK) return st;
     const int64_t per = a.M * a.N, n = per * d->batch;
     if (n >= kMaxThreads) return LOKA_ERR_SHAPE;
@@ -591,7 +628,7 @@ loka_status mxfp4_linear_fused_launch(const loka_gemm_desc* d, const void* x_bf1
     a.x = static_cast<const uint16_t*>(x_bf16);
     a.ldx = ld;
     a.x_wide = aligned16(x_bf16) && ld % 8 == 0;
-    return stream_launch<1, 1, true>(a, 1, stream);
+    return stream_any<true>(a, 1, stream);
 }
 
 }  // namespace loka
