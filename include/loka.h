@@ -370,7 +370,7 @@ loka_status loka_mxfp4_linear(const loka_gemm_desc* desc, const void* x_bf16, in
  * rstd [rows] fp32.  hq and hs both or neither; each of h_out, rstd, residual (h = x) and gamma (1) may be NULL.
  * A row with a NaN or an infinity: bf16 and MXFP4 values that are NaN by the formula are NaN, and an e4m3 scale group that
  * holds such a value has a NaN scale.  The sum of squares is held in fp32: it has to stay below 3.4e38.
- * cols % 16 == 0 and at most 65536; cols % 128 == 0 for the block modes.  ld_x, ld_r (row strides of x and residual, in
+ * cols % 16 == 0 and at most 32768; cols % 128 == 0 for the block modes.  ld_x, ld_r (row strides of x and residual, in
  * elements) multiples of 8 and at least cols; outputs are contiguous.  Pointers 16-byte aligned (scales and rstd: 4).
  * h_out may be x or residual itself (same row stride); no other outputs may overlap inputs. */
 typedef enum { LOKA_RMS_OUT_BF16 = 0, LOKA_RMS_OUT_E4M3 = 1, LOKA_RMS_OUT_MXFP4 = 2 } loka_rms_out;

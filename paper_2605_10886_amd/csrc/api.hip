@@ -523,7 +523,7 @@ static bool rms_mode_ok(int m) { return m == LOKA_SCALE_ROW || is_block_x(m); }
 static loka_status validate_rms(const loka_rms_desc* d) {
     if (!d) return LOKA_ERR_NULL;
     if (d->rows <= 0 || d->cols <= 0 || d->cols % 16) return LOKA_ERR_SHAPE;
-    if (d->rows > INT32_MAX || d->cols > 65536) return LOKA_ERR_SHAPE;
+    if (d->rows > INT32_MAX || d->cols > 32768) return LOKA_ERR_SHAPE;
     return LOKA_OK;
 }
 // ... and those of a matrix with scales in `mode`

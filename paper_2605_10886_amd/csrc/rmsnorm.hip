@@ -219,52 +219,67 @@ __device__ __forceinline__ void e4m3_values(const u32x2 w, float (&f)[8]) {
 }
 
 // Layout of rows and chunks as above; a workgroup walks over rows, adding dgamma's terms of its columns in registers, and
-// leaves one row of partial sums.
-template <int T, int CPL>
+// leaves one row of partial sums.  A row stays in its loaded form (11 registers a chunk, 16 as fp32) between its two
+// uses, so that the next row's loads are in flight while this one is reduced (PREFETCH; not in 1024 threads, which have half
+// the registers).
+template <int T, int CPL, bool PREFETCH>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(const RmsBackArgs a) {
     constexpr int WG = T < 256 ? 256 : T, RPW = WG / T;
     __shared__ float red[2][WG / 64];
     const int tid = static_cast<int>(threadIdx.x), t = tid % T, sub = tid / T;
     const int chunks = a.cols >> 3;
-    float dg[CPL][8];
-#pragma unroll
-    for (int j = 0; j < CPL; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dg[j][i] = 0.f;
-    u32x4 g[CPL];
-#pragma unroll
-    for (int j = 0; j < CPL; ++j) {
-        g[j] = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-        if (a.gamma && t + j * T < chunks) g[j] = *reinterpret_cast<const u32x4*>(a.gamma + (t + j * T) * 8);
-    }
-    int turn = 0;
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * RPW; base < a.rows; base += static_cast<int64_t>(gridDim.x) * RPW, turn ^= 1) {
-        const int64_t row = base + sub;
-        const bool live = row < a.rows;
-        float n[CPL][8], d[CPL][8], sum = 0.f;
-        const float rstd = live ? a.rstd[row] : 0.f;
+    struct Row { u32x4 dy[CPL], dh[CPL]; u32x2 q[CPL]; float s[CPL], rstd; };
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        Row v;
+        v.rstd = row < a.rows ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int j = 0; j < CPL; ++j) {
             const int c = t + j * T;
-            u32x4 dv = u32x4{0u, 0u, 0u, 0u};
-            u32x2 q = u32x2{0u, 0u};
-            float s = 0.f;
-            if (live && c < chunks) {
-                dv = *reinterpret_cast<const u32x4*>(a.dy + row * a.ld_dy + c * 8);
-                q = *reinterpret_cast<const u32x2*>(a.hq + (row * chunks + c) * 8);
-                s = a.ckpt_mode == kModeRow ? a.hs[row] : a.hs[row * (a.cols >> 7) + (c >> 4)];
+            v.dy[j] = v.dh[j] = u32x4{0u, 0u, 0u, 0u};
+            v.q[j] = u32x2{0u, 0u};
+            v.s[j] = 0.f;
+            if (row < a.rows && c < chunks) {
+                v.dy[j] = *reinterpret_cast<const u32x4*>(a.dy + row * a.ld_dy + c * 8);
+                v.q[j] = *reinterpret_cast<const u32x2*>(a.hq + (row * chunks + c) * 8);
+                v.s[j] = a.ckpt_mode == kModeRow ? a.hs[row] : a.hs[row * (a.cols >> 7) + (c >> 4)];
+                if (PREFETCH && a.dh) v.dh[j] = *reinterpret_cast<const u32x4*>(a.dh + row * a.ld_dh + c * 8);
             }
-            unpack8(dv, d[j]);
-            e4m3_values(q, n[j]);
-            float gf[8];
-            unpack8(g[j], gf);
-            s *= rstd;
+        }
+        return v;
+    };
+    auto gamma_of = [&](int j) __attribute__((always_inline)) {
+        if (a.gamma && t + j * T < chunks) return *reinterpret_cast<const u32x4*>(a.gamma + (t + j * T) * 8);
+        return u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    };
+    constexpr bool KEEP = T < 1024;    // gamma in registers
+    float dg[CPL][8];
+    u32x4 g[KEEP ? CPL : 1];
+#pragma unroll
+    for (int j = 0; j < CPL; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dg[j][i] = 0.f;
+        if (KEEP) g[j] = gamma_of(j);
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * RPW;
+    int64_t base = static_cast<int64_t>(blockIdx.x) * RPW;
+    Row v = load(base + sub);
+    for (int turn = 0; base < a.rows; base += step, turn ^= 1) {
+        const int64_t row = base + sub;
+        Row next;
+        if (PREFETCH) next = load(row + step);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) {
+            float d[8], n[8], gf[8];
+            unpack8(v.dy[j], d);
+            e4m3_values(v.q[j], n);
+            unpack8(KEEP ? g[KEEP ? j : 0] : gamma_of(j), gf);
+            v.s[j] *= v.rstd;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                n[j][i] *= s;
-                dg[j][i] = __builtin_fmaf(d[j][i], n[j][i], dg[j][i]);
-                d[j][i] *= gf[i];
-                sum = __builtin_fmaf(d[j][i], n[j][i], sum);
+                n[i] *= v.s[j];
+                dg[j][i] = __builtin_fmaf(d[i], n[i], dg[j][i]);
+                sum = __builtin_fmaf(d[i] * gf[i], n[i], sum);
             }
         }
         sum = lanes_sum<T>(sum);
@@ -279,26 +294,31 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(con
 #pragma unroll
         for (int j = 0; j < CPL; ++j) {
             const int c = t + j * T;
-            if (live && c < chunks) {
-                float e[8];
-                u32x4 rv = u32x4{0u, 0u, 0u, 0u};
-                if (a.dh) rv = *reinterpret_cast<const u32x4*>(a.dh + row * a.ld_dh + c * 8);
-                unpack8(rv, e);
+            if (row < a.rows && c < chunks) {
+                float d[8], n[8], gf[8], e[8];
+                unpack8(v.dy[j], d);
+                e4m3_values(v.q[j], n);
+                unpack8(KEEP ? g[KEEP ? j : 0] : gamma_of(j), gf);
+                if (!PREFETCH && a.dh) v.dh[j] = *reinterpret_cast<const u32x4*>(a.dh + row * a.ld_dh + c * 8);
+                unpack8(v.dh[j], e);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = __builtin_fmaf(rstd, __builtin_fmaf(-mean, n[j][i], d[j][i]), e[i]);
+                for (int i = 0; i < 8; ++i) e[i] = __builtin_fmaf(v.rstd, __builtin_fmaf(-mean, n[i] * v.s[j], d[i] * gf[i]), e[i]);
                 u32x4 o;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(e[2 * i], e[2 * i + 1]);
                 *reinterpret_cast<u32x4*>(a.dx + row * a.cols + c * 8) = o;
             }
         }
+        if (PREFETCH) v = next;
+        else v = load(row + step);
     }
     if (!a.partial) return;
+    float* const mine = a.partial + static_cast<int64_t>(blockIdx.x) * a.cols;
     if (T >= WG) {
 #pragma unroll
         for (int j = 0; j < CPL; ++j)
             if (t + j * T < chunks) {
-                float* p = a.partial + static_cast<int64_t>(blockIdx.x) * a.cols + (t + j * T) * 8;
+                float* p = mine + (t + j * T) * 8;
                 *reinterpret_cast<v4f*>(p) = v4f{dg[j][0], dg[j][1], dg[j][2], dg[j][3]};
                 *reinterpret_cast<v4f*>(p + 4) = v4f{dg[j][4], dg[j][5], dg[j][6], dg[j][7]};
             }
@@ -310,31 +330,37 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(con
 #pragma unroll
                 for (int j = 0; j < CPL; ++j)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float* p = joined + (t + j * T) * 8 + i;
-                        *p = k ? *p + dg[j][i] : dg[j][i];
+                    for (int i = 0; i < 2; ++i) {
+                        v4f* p = reinterpret_cast<v4f*>(joined + (t + j * T) * 8 + 4 * i);
+                        const v4f x = v4f{dg[j][4 * i], dg[j][4 * i + 1], dg[j][4 * i + 2], dg[j][4 * i + 3]};
+                        *p = k ? *p + x : x;
                     }
             }
             __syncthreads();
         }
-        for (int c = tid; c < a.cols; c += WG) a.partial[static_cast<int64_t>(blockIdx.x) * a.cols + c] = joined[c];
+        for (int c = tid * 4; c < a.cols; c += WG * 4) *reinterpret_cast<v4f*>(mine + c) = *reinterpret_cast<const v4f*>(joined + c);
     }
 }
 
-// dgamma: 32 columns a workgroup, 8 slices of the partial rows
+// dgamma: 32 columns a workgroup (8 lanes of 4), 32 slices of the partial rows, added in order
 __global__ __launch_bounds__(256) void rmsnorm_dgamma_kernel(const float* __restrict__ partial, int n, int cols, float* __restrict__ dgamma) {
-    __shared__ float red[8][32];
-    const int k = threadIdx.x & 31, s = threadIdx.x >> 5;
+    __shared__ float red[32][33];
+    const int k = (threadIdx.x & 7) * 4, s = threadIdx.x >> 3;
     const int c = blockIdx.x * 32 + k;
-    float sum = 0.f;
-    if (c < cols)
-        for (int i = s; i < n; i += 8) sum += partial[static_cast<int64_t>(i) * cols + c];
-    red[s][k] = sum;
-    __syncthreads();
-    if (s == 0 && c < cols) {
+    v4f sum = v4f{0.f, 0.f, 0.f, 0.f};
+    if (c < cols) {
+#pragma unroll 4
+        for (int i = s; i < n; i += 32) sum += *reinterpret_cast<const v4f*>(partial + static_cast<int64_t>(i) * cols + c);
+    }
 #pragma unroll
-        for (int i = 1; i < 8; ++i) sum += red[i][k];
-        dgamma[c] = sum;
+    for (int i = 0; i < 4; ++i) red[s][k + i] = sum[i];
+    __syncthreads();
+    const int col = static_cast<int>(threadIdx.x);
+    if (col < 32 && blockIdx.x * 32 + col < cols) {
+        float total = red[0][col];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) total += red[i][col];
+        dgamma[blockIdx.x * 32 + col] = total;
     }
 }
 
@@ -374,16 +400,29 @@ loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void
     a.out_mode = d->out == LOKA_RMS_OUT_E4M3 ? kernel_mode(d->out_mode) : kModeNone;
     a.ckpt_mode = hq ? kernel_mode(d->ckpt_mode) : kModeNone;
     a.eps = d->eps;
+    // Lanes of a row: few where there are rows enough to fill the chip (several rows a wave, no exchange over LDS), many for few
+    // rows, whose time is a row's latency.
     const int chunks = a.cols / 8;
-    if (chunks <= 64) return forward_launch<16, 4>(a, stream);
-    if (chunks <= 512) return forward_launch<64, 8>(a, stream);
-    if (chunks <= 2048) return forward_launch<256, 8>(a, stream);
-    return forward_launch<1024, 8>(a, stream);
+    if (a.rows >= 2048) {
+        if (chunks <= 16) return forward_launch<16, 1>(a, stream);
+        if (chunks <= 32) return forward_launch<16, 2>(a, stream);
+        if (chunks <= 64) return forward_launch<16, 4>(a, stream);
+        if (chunks <= 128) return forward_launch<32, 4>(a, stream);
+        if (chunks <= 256) return forward_launch<64, 4>(a, stream);
+        if (chunks <= 512) return forward_launch<64, 8>(a, stream);
+    }
+    if (chunks <= 64) return forward_launch<64, 1>(a, stream);
+    if (chunks <= 128) return forward_launch<64, 2>(a, stream);
+    if (chunks <= 256) return forward_launch<256, 1>(a, stream);
+    if (chunks <= 512) return forward_launch<256, 2>(a, stream);
+    if (chunks <= 1024) return forward_launch<256, 4>(a, stream);
+    if (chunks <= 2048) return forward_launch<512, 4>(a, stream);
+    return forward_launch<1024, 4>(a, stream);
 }
 
-// Workgroups of the backward pass: enough to fill the chip, few enough that the partial sums stay small beside the rows
+// Workgroups of the backward pass: two a CU, which keep enough loads in flight, so that the partial sums stay small beside the rows
 static int64_t backward_groups(int64_t rows, int cols) {
-    const int rpw = cols <= 512 ? 16 : cols <= 4096 ? 4 : 1;
+    const int rpw = cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 2048 ? 4 : 1;
     const int64_t most = (rows + rpw - 1) / rpw;
     return most < 512 ? most : 512;
 }
@@ -392,9 +431,9 @@ size_t rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     return static_cast<size_t>(backward_groups(rows, static_cast<int>(cols))) * static_cast<size_t>(cols) * 4;
 }
 
-template <int T, int CPL>
+template <int T, int CPL, bool PREFETCH = true>
 static void backward_launch(const RmsBackArgs& a, int64_t groups, hipStream_t stream) {
-    rmsnorm_backward_kernel<T, CPL><<<static_cast<uint32_t>(groups), T < 256 ? 256 : T, 0, stream>>>(a);
+    rmsnorm_backward_kernel<T, CPL, PREFETCH><<<static_cast<uint32_t>(groups), T < 256 ? 256 : T, 0, stream>>>(a);
 }
 
 loka_status rmsnorm_backward_launch(const loka_rms_desc* d, const void* dy, const uint8_t* hq, const float* hs, const float* rstd,
@@ -415,10 +454,15 @@ loka_status rmsnorm_backward_launch(const loka_rms_desc* d, const void* dy, cons
     a.ckpt_mode = kernel_mode(d->ckpt_mode);
     const int64_t groups = backward_groups(a.rows, a.cols);
     const int chunks = a.cols / 8;
-    if (chunks <= 64) backward_launch<16, 4>(a, groups, stream);
-    else if (chunks <= 512) backward_launch<64, 8>(a, groups, stream);
-    else if (chunks <= 2048) backward_launch<256, 8>(a, groups, stream);
-    else backward_launch<1024, 8>(a, groups, stream);
+    if (chunks <= 16) backward_launch<16, 1>(a, groups, stream);
+    else if (chunks <= 32) backward_launch<32, 1>(a, groups, stream);
+    else if (chunks <= 64) backward_launch<64, 1>(a, groups, stream);
+    else if (chunks <= 128) backward_launch<64, 2>(a, groups, stream);
+    else if (chunks <= 256) backward_launch<64, 4>(a, groups, stream);
+    else if (chunks <= 512) backward_launch<256, 2>(a, groups, stream);
+    else if (chunks <= 1024) backward_launch<256, 4>(a, groups, stream);
+    else if (chunks <= 2048) backward_launch<1024, 2>(a, groups, stream);
+    else backward_launch<1024, 4, false>(a, groups, stream);
     LOKA_HIP_TRY(hipGetLastError());
     if (dgamma) {
         rmsnorm_dgamma_kernel<<<static_cast<uint32_t>((a.cols + 31) / 32), 256, 0, stream>>>(a.partial, static_cast<int>(groups), a.cols, dgamma);

@@ -49,7 +49,7 @@ def _check_e4m3(q, s, v, mode, what):
 
 
 SHAPES = [(1, 16), (1, 4096), (3, 128), (5, 208), (64, 256), (33, 512), (17, 640), (9, 1008), (130, 1024), (4, 2048), (300, 4096), (7, 4112), (3, 8192),
-          (2, 16384), (5, 16400), (2, 65536), (1000, 128)]
+          (2, 16384), (5, 16400), (2, 32768), (1000, 128), (2050, 128), (2049, 240), (2060, 512), (2048, 1008), (2051, 1920), (2053, 4096)]
 
 
 @pytest.mark.parametrize("residual,gamma", [(True, True), (False, True), (True, False)])

@@ -79,7 +79,7 @@ def test_residual_norm():
         return B.RmsDesc(rows, cols, ld_x, ld_r, out, out_mode, ckpt_mode, eps)
 
     assert _rms(desc(), x=None) == _rms(desc(), y=None) == _rms(desc(), s=None) == _rms(desc(), hq=FAKE) == _rms(desc(), hs=FAKE) == B.LOKA_ERR_NULL
-    for kw in (dict(rows=0), dict(rows=-4), dict(rows=1 << 31), dict(cols=0), dict(cols=120), dict(cols=65552, ld_x=65552), dict(ld_x=248)):
+    for kw in (dict(rows=0), dict(rows=-4), dict(rows=1 << 31), dict(cols=0), dict(cols=120), dict(cols=32784, ld_x=32784), dict(ld_x=248)):
         assert _rms(desc(**kw)) == B.LOKA_ERR_SHAPE, kw
         assert _back(desc(**kw)) == B.LOKA_ERR_SHAPE, kw
     assert _rms(desc(ld_r=248), res=FAKE) == _back(desc(ld_r=248), dh=FAKE) == B.LOKA_ERR_SHAPE
