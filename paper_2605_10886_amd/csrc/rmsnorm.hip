@@ -400,29 +400,23 @@ loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void
     a.out_mode = d->out == LOKA_RMS_OUT_E4M3 ? kernel_mode(d->out_mode) : kModeNone;
     a.ckpt_mode = hq ? kernel_mode(d->ckpt_mode) : kModeNone;
     a.eps = d->eps;
-    // Lanes of a row: few where there are rows enough to fill the chip (several rows a wave, no exchange over LDS), many for few
-    // rows, whose time is a row's latency.
+    // One or two chunks a lane wherever lanes suffice: more rows than registers hold at once stay in flight (a wave a row, 8 chunks a
+    // lane: 32768 x 4096 with the checkpoint 217 us, here 193; 4096 x 2048 15.1 and 12.9).
     const int chunks = a.cols / 8;
-    if (a.rows >= 2048) {
-        if (chunks <= 16) return forward_launch<16, 1>(a, stream);
-        if (chunks <= 32) return forward_launch<16, 2>(a, stream);
-        if (chunks <= 64) return forward_launch<16, 4>(a, stream);
-        if (chunks <= 128) return forward_launch<32, 4>(a, stream);
-        if (chunks <= 256) return forward_launch<64, 4>(a, stream);
-        if (chunks <= 512) return forward_launch<64, 8>(a, stream);
-    }
+    if (chunks <= 16) return forward_launch<16, 1>(a, stream);
+    if (chunks <= 32) return forward_launch<32, 1>(a, stream);
     if (chunks <= 64) return forward_launch<64, 1>(a, stream);
     if (chunks <= 128) return forward_launch<64, 2>(a, stream);
     if (chunks <= 256) return forward_launch<256, 1>(a, stream);
     if (chunks <= 512) return forward_launch<256, 2>(a, stream);
-    if (chunks <= 1024) return forward_launch<256, 4>(a, stream);
+    if (chunks <= 1024) return forward_launch<512, 2>(a, stream);
     if (chunks <= 2048) return forward_launch<512, 4>(a, stream);
     return forward_launch<1024, 4>(a, stream);
 }
 
 // Workgroups of the backward pass: two a CU, which keep enough loads in flight, so that the partial sums stay small beside the rows
 static int64_t backward_groups(int64_t rows, int cols) {
-    const int rpw = cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 2048 ? 4 : 1;
+    const int rpw = cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1;
     const int64_t most = (rows + rpw - 1) / rpw;
     return most < 512 ? most : 512;
 }
@@ -458,7 +452,7 @@ loka_status rmsnorm_backward_launch(const loka_rms_desc* d, const void* dy, cons
     else if (chunks <= 32) backward_launch<32, 1>(a, groups, stream);
     else if (chunks <= 64) backward_launch<64, 1>(a, groups, stream);
     else if (chunks <= 128) backward_launch<64, 2>(a, groups, stream);
-    else if (chunks <= 256) backward_launch<64, 4>(a, groups, stream);
+    else if (chunks <= 256) backward_launch<256, 1>(a, groups, stream);
     else if (chunks <= 512) backward_launch<256, 2>(a, groups, stream);
     else if (chunks <= 1024) backward_launch<256, 4>(a, groups, stream);
     else if (chunks <= 2048) backward_launch<1024, 2>(a, groups, stream);

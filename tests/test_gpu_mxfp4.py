@@ -61,6 +61,17 @@ def test_strides_and_alignment(ld, offset, transpose):
         assert torch.equal(out[:, :90].double(), P.mx_values(wq, ws)[:, :90]) and bool((out[:, 90:] == 7).all())
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 7), (9, 1), (5, 33), (300, 31), (257, 1003), (1008, 5013), (3, 70001)])
+def test_values_of_rows_that_start_anywhere(rows, cols):
+    x = _wide(rows, cols, seed=rows)
+    x[rows // 2, cols // 2] = float("nan")
+    q, s = B.loka_mxfp4_quantize(x)
+    want = P.mx_values(q, s)[:, :cols]
+    for out in (None, torch.empty(rows * cols + 1, dtype=torch.bfloat16, device=DEV)[1:].view(rows, cols)):      # aligned or not
+        v = B.loka_mxfp4_dequantize(q, s, cols, out=out).double()
+        assert torch.equal(torch.isnan(v), torch.isnan(want)) and torch.equal(torch.nan_to_num(v), torch.nan_to_num(want))
+
+
 def test_every_bf16_value_ties_and_special_groups():
     # every finite bf16 with every group maximum from its own exponent up to three above, and the halves between codes
     allb = torch.arange(65536, device=DEV, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
