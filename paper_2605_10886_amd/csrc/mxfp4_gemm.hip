@@ -63,7 +63,7 @@ __device__ __forceinline__ MxPiece mx_read_piece(const uint8_t* q, const uint8_t
     p.s = in ? s : 0x7F7F7F7Fu;
     return p;
 }
-// The same from bf16 rows, two ways.  Few rows (ROWS, 4 or 16): the wave quantizes 512 elements of a row at a time, 8 a lane as
+// The same from bf16 rows, two ways.  Few rows (ROWS, 2 or 16): the wave quantizes 512 elements of a row at a time, 8 a lane as
 // they lie in memory, and turns the codes in its part of LDS (a lane that read its own row's groups would make every
 // 16-byte load a cache line of its own).
 constexpr int kTurn = 256 + 16;        // bytes of a row there: codes, scales
@@ -141,7 +141,7 @@ __device__ __forceinline__ void in_order() {
 // Few rows: bound by the weights' traffic.  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
 // take 512-element pieces of the contraction in turn, straight from memory into registers, and add their partial sums in LDS
 // in wave order.
-// QUANT 0: stored X.  1, 4, 16: bf16 X of up to 16 rows (MT = 1): by groups, by rows of up to 4 or of up to 16.
+// QUANT 0: stored X.  1, 2, 16: bf16 X of up to 16 rows (MT = 1): by groups, by rows (up to 2, 16).
 template <int MT, int NT, int NW, int QUANT>
 __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];       // partial sums [NW][MT * NT][64]; before them, the waves' rows of x
@@ -694,8 +694,8 @@ loka_status mxfp4_linear_fused_launch(const loka_gemm_desc* d, const void* x_bf1
     a.x = static_cast<const uint16_t*>(x_bf16);
     a.ldx = ld;
     a.x_whole = aligned16(x_bf16) && ld % 8 == 0 && a.K % 8 == 0;
-    // (measured, by rows / by groups: 4 x 4096 x 4096 ROWS4, 16 x 4096 x 4096 ROWS16 us)
-    if (a.M <= 4) return stream_columns<1, 4>(a, 1, stream);
+    // (by rows / by groups, us: 1 x 4096 x 4096 4.0 / 4.5, 2 rows 4.2 / 4.5, 3 rows 4.5 / 4.5, 4 rows 4.8 / 4.4, 1 x 4096 x 16384 9.2 / 10.7)
+    if (a.M <= 2) return stream_columns<1, 2>(a, 1, stream);
     if (a.x_whole && a.K < (INT64_C(1) << 30)) return stream_columns<1, 1>(a, 1, stream);
     return stream_launch<1, 1, 16>(a, 1, stream);
 }
