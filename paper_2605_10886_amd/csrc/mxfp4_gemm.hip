@@ -17,6 +17,8 @@ namespace loka {
 
 constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
 
+typedef float v16f __attribute__((ext_vector_type(16)));
+
 struct MxArgs {
     const uint8_t *xq, *sx, *wq, *sw;
     const uint16_t* x;                 // fused quantization: bf16 [M, ldx]
@@ -41,6 +43,13 @@ __device__ __forceinline__ v4f mx_mfma(const u32x4 a, const u32x4 b, v4f c, uint
     const v8i A = {static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(a.z), static_cast<int>(a.w), 0, 0, 0, 0};
     const v8i B = {static_cast<int>(b.x), static_cast<int>(b.y), static_cast<int>(b.z), static_cast<int>(b.w), 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
+}
+
+template <int S>
+__device__ __forceinline__ v16f mx_mfma32(const u32x4 a, const u32x4 b, v16f c, uint32_t sa, uint32_t sb) {
+    const v8i A = {static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(a.z), static_cast<int>(a.w), 0, 0, 0, 0};
+    const v8i B = {static_cast<int>(b.x), static_cast<int>(b.y), static_cast<int>(b.z), static_cast<int>(b.w), 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, 4, S, static_cast<int>(sa), S, static_cast<int>(sb));
 }
 
 // A lane's four groups of 512 elements: codes and the word of their scale bytes.  Groups past the stored row are zero codes
@@ -229,33 +238,36 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 }
 
 // ---------------------------------------------------------------------------------
-// Many rows: a workgroup of WM x WN x WK waves computes a tile of the result, each wave TM x TN tiles of 16 x 16, on K tiles of
+// Many rows: a workgroup of WM x WN x WK waves computes a tile of the result, each wave TM x TN tiles of 32 x 32, on K tiles of
 // 256 elements (128 bytes of codes a row) that loads bring straight into LDS, R of them in a ring.  The 16-byte chunks of a
-// row lie permuted, chunk c at place c ^ key(row): LDS serves a 16-byte read 16 lanes at a time, 8 of one g and 8 of the next
-// (rows 0 - 3, 12 - 15 and 4 - 11, or the other way round), and with key = bits 2, 1, 3 of r these use all 64 banks.
-// A lane takes groups 2 g and 2 g + 1 of a row for the two instructions of a K tile (halves s = 0, 1), whose scale bytes are
-// then neighbours: one 16-bit LDS read for both.  WK = 1: a wave multiplies both halves; WK = 2: its own half of every
-// K tile, and two waves add up at the end (two waves on a SIMD where the tile gives only four).
-// The waves' W rows are dealt to the 16 x 16 tiles so that a lane's columns of a tile pair are 8 neighbours (coff_of).
+// row lie permuted, chunk c at place c ^ (row / 2 % 8), so that the rows that an LDS read serves at once use all 64 banks.
+//
+// v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds row r = l % 32, one group of 32 elements (of the two: h = l / 32) and its scale
+// byte.  The four instructions of a K tile (quarters s) take groups 4 h + s, so a lane's four scale bytes are one word.
+// From registers, on changing operands, this form sustains 6.6 PFLOP/s on 4-bit codes and the 16 x 16 x 128 form 5.8, which
+// the 16-byte encoding holds at 24 cycles an instruction.  WK = 1: a wave multiplies all quarters; WK = 2: two of them, and
+// two waves add up at the end (two waves on a SIMD where the tile gives only four).
+// W's rows are dealt to the instruction's so that a lane's values are two runs of 8 columns.
 //
 // One barrier a K tile: its last operands are in registers when the barrier is passed, so the loads of a K tile R further on
 // may go where this one lay, and the first operands of the next K tile are read between the matrix instructions that follow.
-// Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first K tiles arrive
-// while this one's values are stored, and nothing waits for the stores where their number is known (see `late`).
+// (The barrier costs some 800 cycles of a K tile's 3800: K tiles of 128 elements, with four in the ring, took 8192 x 8192 x
+// 8192 from 300 to 388 us.)  Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first
+// K tiles arrive while this one's values are stored, and nothing waits for the stores where their number is known (see `late`).
 template <int TM_, int TN_, int WM_, int WN_, int WK_, int R_>
 struct MxTile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WK = WK_, R = R_, NW = WM * WN * WK, BM = WM * TM * 16, BN = WN * TN * 16;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WK = WK_, R = R_, NW = WM * WN * WK, BM = WM * TM * 32, BN = WN * TN * 32;
     static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 8, STAGE = OFF_SW + BN * 8;
-    static constexpr int XCH = WM * WN * 64 * TN * 16;              // WK = 2: one row of 16 x 16 tiles of every wave
+    static constexpr int XCH = WM * WN * 64 * 64;                   // WK = 2: one 32 x 32 tile of every wave
     static constexpr int LDS = R * STAGE + (WK == 2 ? 2 * XCH : 0), PER_CU = 163840 / LDS;
-    static_assert(NW % 4 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % 32 == 0 && BN % 32 == 0 && TM % 2 == 0 && TN % 2 == 0);
-    static_assert(WK == 1 || (WK == 2 && TM == 4));
+    static_assert(NW % 2 == 0 && BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && (BM + BN) % (32 * NW) == 0);
+    static_assert(WK == 1 || (WK == 2 && TM == 2));
 };
 
 template <class C, bool SPLIT>
 __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
-    constexpr int TM = C::TM, TN = C::TN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    constexpr int TM = C::TM, TN = C::TN, Q = 4 / C::WK;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
     const int kg = C::WK == 2 ? wave / (C::WM * C::WN) : 0, wmn = C::WK == 2 ? wave % (C::WM * C::WN) : wave;
     const int wm = wmn / C::WN, wn = wmn % C::WN;
     const int row_bytes = static_cast<int>(a.Kp >> 1), scale_bytes = static_cast<int>(a.Kp >> 5);
@@ -263,20 +275,21 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     const bool ragged = (a.Kp & 255) != 0;
     const int total = a.total;
 
-    // where this wave's loads put and find things (8 rows a load, every NW-th group of them)
-    const int key_x = ((wave & 1) << 2) | (((lane >> 4) & 1) << 1) | (lane >> 5);
-    const int key_w = (wave & 1) | (((lane >> 4) & 1) << 1) | ((wave & 2) << 1);
-    const int x_chunk = (lane & 7) ^ key_x, w_chunk = (lane & 7) ^ key_w;
-    const int x_lane = (lane >> 3) * row_bytes + x_chunk * 16, w_lane = (lane >> 3) * row_bytes + w_chunk * 16;
-    // (scales, 8 bytes a row, lie in the order in which the operand tiles read them: on neighbouring banks)
-    const int sx_lane = (lane >> 1) * scale_bytes + (lane & 1) * 4;
-    const int sw_lane = (((lane >> 3) & 3) * 8 + (lane >> 5) * 4 + ((lane >> 1) & 3)) * scale_bytes + (lane & 1) * 4;
+    // column, of the 32, that row r of the instruction's result stands for
+    const int n_of = (r >> 4) * 16 + ((r >> 2) & 1) * 8 + ((r >> 3) & 1) * 4 + (r & 3);
+    // where this wave's loads find things (8 rows a load, every NW-th group of them: of one parity)
+    const int chunk = (lane & 7) ^ (((wave & 1) << 2) | (lane >> 4)), c_lane = (lane >> 3) * row_bytes + chunk * 16;
+    // (scales of 32 rows a load: the four bytes of h = 0 of each, then those of h = 1, W's in the order of the instruction's rows)
+    const int sx_lane = r * scale_bytes + h * 4, sw_lane = n_of * scale_bytes + h * 4;
     // where it reads operands
-    const int key_r = ((r >> 3) << 2) | (((r >> 1) & 1) << 1) | ((r >> 2) & 1), at_p = ((2 * g) ^ key_r) * 16;
-    const int x_at = (wm * TM * 16 + r) * 128, w_at = C::OFF_W + (wn * TN * 16 + (r >> 2) * 8 + (r & 3)) * 128;
-    const int first_p = kg ? at_p ^ 16 : at_p;             // (of the wave's own half, WK = 2)
-    const int x_off[2] = {x_at + first_p, x_at + (at_p ^ 16)}, w_off[2] = {w_at + first_p, w_at + (at_p ^ 16)};
-    const int sx_off = C::OFF_SX + (wm * TM * 16 + r) * 8 + 2 * g + kg, sw_off = C::OFF_SW + (wn * TN * 16 + r) * 8 + 2 * g + kg;
+    const int x_row = wm * TM * 32 + r, w_row = wn * TN * 32 + n_of;
+    int x_off[Q], w_off[Q];
+#pragma unroll
+    for (int s = 0; s < Q; ++s) {
+        x_off[s] = x_row * 128 + ((4 * h + kg * 2 + s) ^ ((r >> 1) & 7)) * 16;
+        w_off[s] = C::OFF_W + w_row * 128 + ((4 * h + kg * 2 + s) ^ ((n_of >> 1) & 7)) * 16;
+    }
+    const int sx_off = C::OFF_SX + wm * TM * 256 + h * 128 + r * 4 + kg * 2, sw_off = C::OFF_SW + wn * TN * 256 + h * 128 + r * 4 + kg * 2;
 
     struct Place { int m0, n0, k_first, k_count, split; int64_t prob; };
     auto locate = [&](int t) __attribute__((always_inline)) {
@@ -312,27 +325,26 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     };
     aim();
     // load i of a wave's share of a K tile: X codes, W codes, scales of X, then of W
-    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), SROWS = (C::BM + C::BN) / 32, LS = (SROWS + C::NW - 1) / C::NW, LOADS = LX + LW + LS;
-    int ld_x, ld_w, ld_sx, ld_sw, ld_off, ld_soff;
+    constexpr int LX = C::BM / (8 * C::NW), LW = C::BN / (8 * C::NW), SROWS = (C::BM + C::BN) / 32, LS = SROWS / C::NW, LOADS = LX + LW + LS;
+    int ld_c, ld_sx, ld_sw, ld_off, ld_soff;
     auto begin_request = [&]() __attribute__((always_inline)) {
         const int kt = ld.k_first + ld_k;
         const bool tail = ragged && kt == ktiles_all - 1;           // the last K tile is half one: the other half reads zeros
-        ld_x = tail && x_chunk >= 4 ? 0x7FFFFFFF : x_lane;
-        ld_w = tail && w_chunk >= 4 ? 0x7FFFFFFF : w_lane;
-        ld_sx = tail && (lane & 1) ? 0x7FFFFFFF : sx_lane;
-        ld_sw = tail && (lane & 1) ? 0x7FFFFFFF : sw_lane;
+        ld_c = tail && chunk >= 4 ? 0x7FFFFFFF : c_lane;
+        ld_sx = tail && h ? 0x7FFFFFFF : sx_lane;
+        ld_sw = tail && h ? 0x7FFFFFFF : sw_lane;
         ld_off = wave * 8 * row_bytes + kt * 128;
         ld_soff = kt * 8;
     };
     auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
         if (i < LX) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + (i * C::NW + wave) * 1024), 16, ld_x,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(smem + stage + (i * C::NW + wave) * 1024), 16, ld_c,
                                                      ld_off + i * C::NW * 8 * row_bytes, 0, 0);
         } else if (i < LX + LW) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_w,
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + ((i - LX) * C::NW + wave) * 1024), 16, ld_c,
                                                      ld_off + (i - LX) * C::NW * 8 * row_bytes, 0, 0);
-        } else {                                           // 32 rows a load: those of X first, then those of W (a load too many repeats one)
-            const int at_ = (i - LX - LW) * C::NW + wave, grp = at_ < SROWS ? at_ : at_ - SROWS;
+        } else {                                           // 32 rows a load: those of X first, then those of W
+            const int grp = (i - LX - LW) * C::NW + wave;
             if (grp < C::BM / 32)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(sxr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_SX + grp * 256), 4, ld_sx,
                                                          ld_soff + grp * 32 * scale_bytes, 0, 0);
@@ -350,39 +362,37 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         }
     };
 
-    // ---- operands: two sets; scales: two 16 x 16 tiles' bytes in a register
+    // ---- operands: two sets, used in turn
     constexpr int READS = TM + TN, MM = TM * TN;
     u32x4 fx[2][TM], fw[2][TN];
-    u16x2 sx[TM / 2], sw[TN / 2];
-    // operand i of half `half` into set `set`, in the order in which they are used: two W tiles, two X tiles, the other W, the other X
-    auto read_one = [&](int stage, int set, int half, int i) __attribute__((always_inline)) {
-        const bool w = i < 2 || (i >= 4 && i < 2 + TN);
-        const int k = i < 2 ? i : i < 4 ? i - 2 : i < 2 + TN ? i - 2 : i - TN;
-        if (w) fw[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[half] + (k >> 1) * 4096 + (k & 1) * 512);
-        else fx[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[half] + k * 2048);
+    uint32_t sx[TM], sw[TN], sx_next[TM], sw_next[TN];
+    // operand i of the wave's quarter q, in the order in which they are used: one X tile, the W tiles, the other X tiles
+    auto read_one = [&](int stage, int q, int i) __attribute__((always_inline)) {
+        const int set = q & 1, k = i == 0 ? 0 : i <= TN ? i - 1 : i - TN;
+        if (i >= 1 && i <= TN) fw[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + w_off[q] + k * 4096);
+        else fx[set][k] = *reinterpret_cast<const u32x4*>(smem + stage + x_off[q] + k * 4096);
     };
     auto read_scales = [&](int stage) __attribute__((always_inline)) {
         auto one = [&](const uint8_t* p) __attribute__((always_inline)) {
-            return C::WK == 2 ? static_cast<uint16_t>(*p) : *reinterpret_cast<const uint16_t*>(p);
+            return C::WK == 2 ? static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
         };
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sw[j >> 1][j & 1] = one(smem + stage + sw_off + j * 128);
+        for (int j = 0; j < TN; ++j) sw_next[j] = one(smem + stage + sw_off + j * 256);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) sx[i >> 1][i & 1] = one(smem + stage + sx_off + i * 128);
+        for (int i = 0; i < TM; ++i) sx_next[i] = one(smem + stage + sx_off + i * 256);
     };
-    v4f acc[TM][TN];
-    // matrix instructions first .. last - 1 of the operands in a set
-    auto multiply = [&](auto set_c, int first, int last) __attribute__((always_inline)) {
-        constexpr int SET = decltype(set_c)::value, S = C::WK == 1 ? SET : 0;      // S: the scale's byte
+    v16f acc[TM][TN];
+    // matrix instructions first .. last - 1 of quarter q
+    auto multiply = [&](auto q_c, int first, int last) __attribute__((always_inline)) {
+        constexpr int q = decltype(q_c)::value;
 #pragma unroll
         for (int k = 0; k < MM; ++k) {
             if (k < first || k >= last) continue;
-            const int i = (k / (2 * TN)) * 2 + ((k >> 1) & 1), j = (k % (2 * TN)) / 4 * 2 + (k & 1);
-            const uint32_t a_ = __builtin_bit_cast(uint32_t, sw[j / 2]), b_ = __builtin_bit_cast(uint32_t, sx[i / 2]);
-            if (j & 1) acc[i][j] = i & 1 ? mx_mfma<2 + S, 2 + S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_) : mx_mfma<2 + S, S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_);
-            else acc[i][j] = i & 1 ? mx_mfma<S, 2 + S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_) : mx_mfma<S, S>(fw[SET][j], fx[SET][i], acc[i][j], a_, b_);
+            const int i = k / TN, j = k % TN;
+            acc[i][j] = mx_mfma32<q>(fw[q & 1][j], fx[q & 1][i], acc[i][j], sw[j], sx[i]);
         }
     };
+
     int tile = ld_tile, stage = 0;
     Place at = ld;
     for (int k = 0; k < C::R; ++k) {
@@ -394,27 +404,31 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     wait_vmcnt<(C::R - 1) * LOADS>();
     lds_barrier();
 #pragma unroll
-    for (int i = 0; i < READS; ++i) read_one(0, 0, 0, i);
+    for (int i = 0; i < READS; ++i) read_one(0, 0, i);
     read_scales(0);
     // Where a tile's values left in STORES stores, the loads of the K tiles that were requested before them are awaited with the
     // stores in flight: `late` K tiles from there.
-    constexpr int STORES = TM * TN / 2 / C::WK, NEWER = (C::R - 2) * LOADS;
+    constexpr int STORES = TM * TN * 2 / C::WK, NEWER = (C::R - 2) * LOADS;
     static_assert(NEWER + STORES <= 63);
     int late = 0;
 
-    // The matrix instructions of one set, and between them (a burst would hold the issue stage up) the LDS reads of the next
-    // operands and, where a K tile ends, the loads into the place that it leaves.
-    auto halves = [&]() __attribute__((always_inline)) {        // WK = 1, the first half
+    // A quarter's matrix instructions, and between them (a burst would hold the issue stage up) the LDS reads of the next
+    // operands, early enough to be there when they are wanted, ...
+    auto quarter = [&](auto q_c) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
-            read_one(stage, 1, 1, i);
+        for (int i = 0; i < MM; ++i) {
+            if (i < READS) read_one(stage, decltype(q_c)::value + 1, i);
+            if (i == MM - 1)
+#pragma unroll
+                for (int k = MM; k < READS; ++k) read_one(stage, decltype(q_c)::value + 1, k);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(std::integral_constant<int, 0>{}, MM * i / READS, MM * (i + 1) / READS);
+            multiply(q_c, i, i + 1);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    auto finish = [&](auto set_c) __attribute__((always_inline)) {
-        constexpr int SET = decltype(set_c)::value;
+    // ... and, where a K tile ends, the loads into the place that it leaves.
+    auto finish = [&]() __attribute__((always_inline)) {
+        const std::integral_constant<int, Q - 1> last;
         if (late > 0) { --late; wait_vmcnt<NEWER + STORES>(); }
         else wait_vmcnt<NEWER>();                               // the next K tile has landed
         lds_barrier();                                          // ... for everyone, and everyone has this one's operands
@@ -422,18 +436,18 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         stage = stage + C::STAGE == C::R * C::STAGE ? 0 : stage + C::STAGE;
         begin_request();
 #pragma unroll
-        for (int i = 0; i < READS; ++i) {
-            multiply(set_c, MM * i / READS, MM * i / READS + 1);
+        for (int i = 0; i < MM; ++i) {
+            multiply(last, i, i + 1);
             __builtin_amdgcn_sched_barrier(0);
+            if (i < READS) read_one(stage, 0, i);
+            if (i == MM - 1)
 #pragma unroll
-            for (int l = LOADS * i / READS; l < LOADS * (i + 1) / READS; ++l) request_one(freed, l);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(set_c, MM * i / READS + 1, MM * (i + 1) / READS);
-            __builtin_amdgcn_sched_barrier(0);
-            read_one(stage, C::WK == 2 ? SET ^ 1 : 0, 0, i);
+                for (int k = MM; k < READS; ++k) read_one(stage, 0, k);
+#pragma unroll
+            for (int l = LOADS * i / MM; l < LOADS * (i + 1) / MM; ++l) request_one(freed, l);
+            if (i == (READS < MM ? READS : MM - 1)) read_scales(stage);
             __builtin_amdgcn_sched_barrier(0);
         }
-        read_scales(stage);
         advance();
     };
 
@@ -441,83 +455,101 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-        if constexpr (C::WK == 1) {
-            for (int k = 0; k < at.k_count; ++k) {
-                halves();
-                finish(std::integral_constant<int, 1>{});
-            }
-        } else {
-            for (int k = 0; k + 1 < at.k_count; k += 2) {
-                finish(std::integral_constant<int, 0>{});
-                finish(std::integral_constant<int, 1>{});
-            }
-            if (at.k_count & 1) {                               // the next tile starts on set 0 again
-                finish(std::integral_constant<int, 0>{});
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fx[0][i] = fx[1][i];
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        for (int k = 0; k < at.k_count; ++k) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fw[0][j] = fw[1][j];
+            for (int i = 0; i < TM; ++i) sx[i] = sx_next[i];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) sw[j] = sw_next[j];
+            quarter(std::integral_constant<int, 0>{});
+            if constexpr (Q == 4) {
+                quarter(std::integral_constant<int, 1>{});
+                quarter(std::integral_constant<int, 2>{});
             }
-            // the two halves' sums: wave (kg) keeps rows 2 kg, 2 kg + 1 of its 16 x 16 tiles, and hands the others over
+            finish();
+        }
+        if constexpr (C::WK == 2) {
+            // the two halves' sums: wave (kg) keeps the 32 x 32 tiles of row kg, and hands the others over
             v4f* const mine = reinterpret_cast<v4f*>(smem + C::R * C::STAGE + kg * C::XCH) + wmn * 64 + lane;
             const v4f* const theirs = reinterpret_cast<const v4f*>(smem + C::R * C::STAGE + (kg ^ 1) * C::XCH) + wmn * 64 + lane;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int j = 0; j < TN; ++j) {
+                if (j) lds_barrier();
 #pragma unroll
-                for (int j = 0; j < TN; ++j) mine[j * (C::WM * C::WN * 64)] = kg ? acc[i][j] : acc[2 + i][j];
+                for (int e = 0; e < 4; ++e) {
+                    const v16f t = kg ? acc[0][j] : acc[1][j];
+                    mine[e * (C::WM * C::WN * 64)] = v4f{t[4 * e], t[4 * e + 1], t[4 * e + 2], t[4 * e + 3]};
+                }
                 lds_barrier();
+                if (kg) acc[0][j] = acc[1][j];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = (kg ? acc[2 + i][j] : acc[i][j]) + theirs[j * (C::WM * C::WN * 64)];
-                if (i == 0) lds_barrier();
+                for (int e = 0; e < 4; ++e) {
+                    const v4f t = theirs[e * (C::WM * C::WN * 64)];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[0][j][4 * e + i] += t[i];
+                }
             }
         }
-        // ---- lane (r, g) holds rows 16 i + r, columns coff_of(j) + 8 g + 0 .. 3
+        // ---- lane (r, h) holds rows 32 i + r, columns 32 j + 8 h + 0 .. 7 and 16 more.  Lanes of 16 exchange halves of their runs, so
+        // that four of them write 64 consecutive bytes of a row.
         constexpr int ROWS = TM / C::WK;
-        const int m_wave = (wm * TM + kg * ROWS) * 16, n_wave = wn * TN * 16;
+        const int m_wave = (wm * TM + kg * ROWS) * 32, n_wave = wn * TN * 32;
         float* const y = SPLIT ? a.part + (static_cast<int64_t>(at.split) * a.batch + at.prob) * a.M * a.N : a.y ? a.y + at.prob * a.strideO : nullptr;
         uint16_t* const out = SPLIT || !a.out ? nullptr : a.out + at.prob * a.strideO;
-        const int el = lane_id(), er = el & 15, eg = el >> 4;       // (not kept through the loop, nor what follows from them)
+        const int el = lane_id(), er = el & 15, es = (el >> 4) & 1, eh = el >> 5;       // (not kept through the loop, nor what follows from them)
         if (a.wide) {                  // whole runs of 8 columns, 32-bit offsets in a tile's rows; what is past the result is dropped
             const int64_t rows = a.M - at.m0 < C::BM ? a.M - at.m0 : C::BM;
-            const int N = static_cast<int>(a.N), n_lane = at.n0 + n_wave + eg * 8, o_lane = (m_wave + er) * N + n_lane;
+            const int N = static_cast<int>(a.N), n_lane = at.n0 + n_wave + eh * 8, o_lane = (m_wave + er) * N + n_lane;
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
             // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
+            auto store = [&](const __amdgpu_buffer_rsrc_t& o, u32x4 first, u32x4 second, int i, int n, int size) __attribute__((always_inline)) {
+                const bool in = n_lane + n < N;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const u32_pair t = __builtin_amdgcn_permlane16_swap(first[e], second[e], false, false);
+                    first[e] = t.x;
+                    second[e] = t.y;
+                }
+                const int off = (o_lane + i * 32 * N + n) * size;
+                __builtin_amdgcn_raw_buffer_store_b128(first, o, in ? off : 0x7FFFFFFF, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(second, o, in ? off + 16 * N * size : 0x7FFFFFFF, 0, 0);
+            };
             if (out) {
                 const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000);
 #pragma unroll
-                for (int j = 0; j < TN; j += 2) {
-                    const bool in = n_lane + j * 16 < N;
+                for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-                    for (int i = 0; i < ROWS; ++i) {
-                        const v4f lo = acc[i][j], hi = acc[i][j + 1];
-                        __builtin_amdgcn_raw_buffer_store_b128(u32x4{pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w)},
-                                                               o, in ? (o_lane + i * 16 * N + j * 16) * 2 : 0x7FFFFFFF, 0, 0);
+                    for (int j = 0; j < TN; ++j) {
+                        const v16f v = acc[i][j];
+                        store(o, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])},
+                              u32x4{pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15])}, i, j * 32 + es * 16, 2);
                     }
-                }
             }
             if (y) {
                 const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(y + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 4), 0x00020000);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int n = (j >> 1) * 32 + (j & 1) * 4;
-                    const bool in = n_lane + n < N;
+                for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-                    for (int i = 0; i < ROWS; ++i)
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), o, in ? (o_lane + i * 16 * N + n) * 4 : 0x7FFFFFFF, 0, 0);
-                }
+                    for (int j = 0; j < 2 * TN; ++j) {
+                        const v16f v = acc[i][j >> 1];
+                        auto word = [&](int e) __attribute__((always_inline)) { return __float_as_uint(v[(j & 1) * 8 + e]); };
+                        store(o, u32x4{word(0), word(1), word(2), word(3)}, u32x4{word(4), word(5), word(6), word(7)}, i, j * 16 + es * 4, 4);
+                    }
             }
             late = out && !y ? C::R - 1 : 0;
         } else {
             late = 0;
+            const int64_t n_lane = at.n0 + n_wave + eh * 8;
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
-                const int64_t m = at.m0 + m_wave + i * 16 + er;
+                const int64_t m = at.m0 + m_wave + i * 32 + es * 16 + er;
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t n = at.n0 + n_wave + eg * 8 + (j >> 1) * 32 + (j & 1) * 4 + e, o = m * a.N + n;
+                    for (int e = 0; e < 16; ++e) {
+                        const int64_t n = n_lane + j * 32 + (e >> 3) * 16 + (e & 7), o = m * a.N + n;
                         if (m < a.M && n < a.N) {
                             if (out) out[o] = static_cast<uint16_t>(f32_to_bf16_rne(acc[i][j][e]));
                             if (y) y[o] = acc[i][j][e];
@@ -671,9 +703,9 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     a.total = static_cast<int>(p.total);
     a.part = static_cast<float*>(ws);
     a.wide = a.N % 8 == 0 && a.N < (INT64_C(1) << 21) && (d->batch == 1 || d->strideO % 8 == 0);
-    using Large = MxTile<4, 8, 4, 2, 1, 2>;
-    using Halves = MxTile<4, 4, 2, 2, 2, 3>;
-    using Small = MxTile<4, 4, 2, 2, 1, 2>;
+    using Large = MxTile<2, 4, 4, 2, 1, 2>;
+    using Halves = MxTile<2, 2, 2, 2, 2, 3>;
+    using Small = MxTile<2, 2, 2, 2, 1, 2>;
     if (p.kind == MX_LARGE) return tile_launch<Large, false>(a, stream);
     if (p.kind == MX_SMALL) return tile_launch<Small, false>(a, stream);
     if (p.splits == 1) return tile_launch<Halves, false>(a, stream);
