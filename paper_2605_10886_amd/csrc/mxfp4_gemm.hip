@@ -625,7 +625,7 @@ static MxArgs args_of(const loka_gemm_desc* d, const uint8_t* wq, const uint8_t*
 // 512-element pieces of 16 columns, times the row tiles.
 //   256 x 256            8192 x 8192 x 8192 295 / 294, 4096 x 4096 x 4096 43.5 / 43, 16384 x 4096 x 1024 60 / 60
 //   128 x 128, K halves  8192 x 8192 x 8192 417 / 415, 4096 x 4096 x 4096 59 / 59, 1024 x 4096 x 16384 53.5 / 53, 2048^3 11.8 / 11.9
-//   128 x 128, 4 waves   4096 x 4096 x 4096 53 / 53, 2048^3 11.5 / 11.5, 5013 x 720 x 1008 8.0 / 8.0, 2048 x 768 x 256 6.0 / 5.4
+//   128 x 128, 4 waves   16384 x 4096 x 1024 68 / 67, 4096 x 4096 x 4096 53 / 55, 2048^3 11.5 / 11.5, 5013 x 720 x 1008 8.0 / 8.0, 2048 x 768 x 256 6.0 / 5.4
 //   stream               32 x 4096 x 4096 5.8 / 6.0, 32 x 16384 x 4096 13.1 / 13.3, 64 x 4096 x 4096 8.3 / 8.0, 128 x 4096 x 4096 14.2 / 12.5,
 //                        256 x 4096 x 4096 25 / 22, 256 x 768 x 2048 5.5 / 5.2
 enum { MX_STREAM = 0, MX_LARGE = 1, MX_HALVES = 2, MX_SMALL = 3 };
@@ -648,7 +648,7 @@ static MxPlan plan_of(const loka_gemm_desc* d) {
         p.splits = splits;
     };
     take(4.0 + rounds(t256, 256) * (5.5 + 2.1 * static_cast<double>(k)), MX_LARGE, 1);
-    take(t128 <= 256 ? 4.5 + 0.88 * static_cast<double>(k) : 4.5 + rounds(t128, 512) * (1.0 + 1.45 * static_cast<double>(k)), MX_SMALL, 1);
+    take(t128 <= 256 ? 4.5 + 0.88 * static_cast<double>(k) : 4.5 + rounds(t128, 512) * (2.0 + 1.45 * static_cast<double>(k)), MX_SMALL, 1);
     for (int64_t s = 1; s <= 64 && s <= k && (s == 1 || static_cast<double>(s) * t128 <= 1024); s *= 2) {
         const double per = std::ceil(static_cast<double>(k) / static_cast<double>(s));
         const double us = 4.0 + rounds(t128 * static_cast<double>(s), 256) * (2.0 + 0.74 * per) + (s > 1 ? 3.0 + bytes * static_cast<double>(s) / 4.5e6 : 0.0);
