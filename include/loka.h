@@ -321,7 +321,7 @@ loka_status loka_fp8_linear_norm_xq(const loka_gemm_desc* desc, const void* x_bf
  *   [cols, rowsp / 2], scales [cols, rowsp / 32], rowsp = rows up to a multiple of 128.  What weights [K, N] take for the
  *   forward product, and X and dY for dW = X^T dY.
  * Any rows >= 1 and cols >= 1 (each at most 2^31 - 1; the stored form may exceed 4 GB).  q 16-byte, scales 4-byte aligned. */
-int64_t loka_mxfp4_padded(int64_t cols);          /* cols up to a multiple of 128; -1 for cols <= 0.  Host only. */
+int64_t loka_mxfp4_padded(int64_t cols);          /* cols up to a multiple of 128; -1 for cols <= 0 or where that is no int64.  Host only. */
 loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                 uint8_t* scales, void* hip_stream);
 /* The values of a stored operand as bf16 [rows, ld], ld >= cols (columns cols .. ld - 1 are left as they are): exact for
@@ -337,7 +337,7 @@ loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64
  *           problem g start at byte g * strideX / 32)
  *   wq, sw  likewise [N, K] with strideW
  *   out_bf16 [batch][M, N] bf16 and / or y_fp32 [batch][M, N] fp32, strideO elements apart; at least one is not NULL.
- *           16-byte aligned; rows are N elements apart, whatever N.
+ *           16-byte aligned; rows are N elements apart, whatever N (with N and strideO multiples of 8, stores are 16 bytes wide).
  * Workspace: loka_mxfp4_gemm_workspace(desc) bytes (partial sums, where a long contraction is split over workgroups
  * because there are few output tiles; added in a fixed order: results do not change from call to call).  NULL / less: the
  * product runs unsplit, adding in another order.  16-byte aligned, not shared with a call still running. */
@@ -372,7 +372,7 @@ loka_status loka_mxfp4_linear(const loka_gemm_desc* desc, const void* x_bf16, in
  * holds such a value has a NaN scale.  The sum of squares is held in fp32: it has to stay below 3.4e38.
  * cols % 16 == 0 and at most 32768; cols % 128 == 0 for the block modes.  ld_x, ld_r (row strides of x and residual, in
  * elements) multiples of 8 and at least cols; outputs are contiguous.  Pointers 16-byte aligned (scales and rstd: 4).
- * h_out may be x or residual itself (same row stride); no other outputs may overlap inputs. */
+ * h_out may be x or residual itself, with a row stride of cols (LOKA_ERR_SHAPE otherwise); no other outputs may overlap inputs. */
 typedef enum { LOKA_RMS_OUT_BF16 = 0, LOKA_RMS_OUT_E4M3 = 1, LOKA_RMS_OUT_MXFP4 = 2 } loka_rms_out;
 typedef struct {
     int64_t rows, cols;
@@ -391,7 +391,7 @@ loka_status loka_add_rmsnorm(const loka_rms_desc* desc, const void* x_bf16, cons
  *   dgamma_j = sum over rows of dy_j n_j
  * dy bf16 [rows, ld_x]: the gradient of y; dh bf16 [rows, ld_r] or NULL: the gradient that reaches h past the norm; dx bf16
  * [rows, cols] (required); dgamma fp32 [cols] or NULL.  rows, cols, ld_x, ld_r and ckpt_mode of `desc` are read, under the
- * rules above.  dx may be dy or dh itself (same row stride).  The codes are e4m3 as hq; hs and rstd as loka_add_rmsnorm wrote them.
+ * rules above.  dx may be dy or dh itself, with a row stride of cols (LOKA_ERR_SHAPE otherwise).  The codes are e4m3 as hq; hs and rstd as loka_add_rmsnorm wrote them.
  * Workspace: loka_rmsnorm_backward_workspace(desc) bytes, 16-byte aligned, for dgamma's partial sums (not needed without
  * dgamma), which are added in a fixed order: results do not change from call to call. */
 size_t loka_rmsnorm_backward_workspace(const loka_rms_desc* desc);

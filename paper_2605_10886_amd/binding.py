@@ -321,9 +321,9 @@ def loka_add_rmsnorm(x, residual=None, gamma=None, eps: float = 1e-5, out: int =
     """RMSNorm of x + residual.  y: bf16, e4m3 codes or MXFP4 codes, with `scales`; h: the sum in bf16 (by default where there
     is a residual); hq, hs, rstd: the 8-bit checkpoint of the sum that loka_rmsnorm_backward reads (where ckpt_mode is given).
     What is not asked for is None."""
-    return RmsNormOut(*(_native or _host()).add_rmsnorm(x, residual, gamma, eps, out, out_mode, ckpt_mode,
-                                                        residual is not None if want_h is None else want_h,
-                                                        ckpt_mode is not None if want_rstd is None else want_rstd, h_out))
+    return tuple.__new__(RmsNormOut, (_native or _host()).add_rmsnorm(x, residual, gamma, eps, out, out_mode, ckpt_mode,
+                                                                      residual is not None if want_h is None else want_h,
+                                                                      ckpt_mode is not None if want_rstd is None else want_rstd, h_out))
 
 
 def loka_rmsnorm_backward(dy, hq, hs, rstd, gamma=None, dh=None, ckpt_mode: int = SCALE_BLOCK_1x128, want_dgamma: bool = True,

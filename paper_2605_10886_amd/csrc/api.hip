@@ -434,7 +434,7 @@ loka_status loka_tracker_update(const void* x_bf16, int64_t B, int64_t K, int64_
 }
 
 // ---- MXFP4
-int64_t loka_mxfp4_padded(int64_t cols) { return cols <= 0 ? -1 : (cols + 127) / 128 * 128; }
+int64_t loka_mxfp4_padded(int64_t cols) { return cols <= 0 || cols > INT64_MAX - 127 ? -1 : (cols + 127) / 128 * 128; }
 
 static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -526,6 +526,10 @@ static loka_status validate_rms(const loka_rms_desc* d) {
     if (d->rows > INT32_MAX || d->cols > 32768) return LOKA_ERR_SHAPE;
     return LOKA_OK;
 }
+// An output over an input (contiguous rows over rows `ld` apart) has to have its row stride: each element is then read before it is written.
+static bool rms_in_place_ok(const loka_rms_desc* d, const void* out, const void* in, int64_t ld) {
+    return out == nullptr || out != in || d->rows == 1 || ld == d->cols;
+}
 // ... and those of a matrix with scales in `mode`
 static loka_status validate_rms_mode(const loka_rms_desc* d, int mode) {
     if (!rms_mode_ok(mode)) return LOKA_ERR_UNSUPPORTED;
@@ -546,6 +550,7 @@ loka_status loka_add_rmsnorm(const loka_rms_desc* desc, const void* x_bf16, cons
     if (!aligned16(x_bf16) || !aligned16(residual_bf16) || !aligned16(gamma_bf16) || !aligned16(h_out_bf16) || !aligned16(y_out) ||
         !aligned16(hq) || !aligned_to(y_scales, 4) || !aligned_to(hs, 4) || !aligned_to(rstd, 4))
         return LOKA_ERR_ALIGN;
+    if (!rms_in_place_ok(desc, h_out_bf16, x_bf16, desc->ld_x) || !rms_in_place_ok(desc, h_out_bf16, residual_bf16, desc->ld_r)) return LOKA_ERR_SHAPE;
     return add_rmsnorm_launch(desc, x_bf16, residual_bf16, gamma_bf16, h_out_bf16, y_out, y_scales, hq, hs, rstd,
                               static_cast<hipStream_t>(hip_stream));
 }
@@ -566,6 +571,7 @@ loka_status loka_rmsnorm_backward(const loka_rms_desc* desc, const void* dy_bf16
     if (!aligned16(dy_bf16) || !aligned16(hq) || !aligned16(gamma_bf16) || !aligned16(dh_bf16) || !aligned16(dx_bf16) ||
         !aligned_to(hs, 4) || !aligned_to(rstd, 4) || !aligned_to(dgamma, 4))
         return LOKA_ERR_ALIGN;
+    if (!rms_in_place_ok(desc, dx_bf16, dy_bf16, desc->ld_x) || !rms_in_place_ok(desc, dx_bf16, dh_bf16, desc->ld_r)) return LOKA_ERR_SHAPE;
     if (dgamma) {
         if (!workspace || ws_bytes < rmsnorm_backward_workspace_bytes(desc->rows, desc->cols)) return LOKA_ERR_WORKSPACE;
         if (!aligned16(workspace)) return LOKA_ERR_ALIGN;

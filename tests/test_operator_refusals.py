@@ -22,7 +22,7 @@ def test_quantize_and_dequantize():
     assert d(None, FAKE, 8, 8, FAKE, 8, None) == d(FAKE, None, 8, 8, FAKE, 8, None) == d(FAKE, FAKE, 8, 8, None, 8, None) == B.LOKA_ERR_NULL
     assert d(FAKE, FAKE, 0, 8, FAKE, 8, None) == d(FAKE, FAKE, 8, 8, FAKE, 7, None) == B.LOKA_ERR_SHAPE
     assert d(ODD, FAKE, 8, 8, FAKE, 8, None) == d(FAKE, FAKE, 8, 8, ODD, 8, None) == B.LOKA_ERR_ALIGN
-    assert [B.loka_mxfp4_padded(k) for k in (-1, 0, 1, 128, 129)] == [-1, -1, 128, 128, 256]
+    assert [B.loka_mxfp4_padded(k) for k in (-1, 0, 1, 128, 129, (1 << 63) - 1)] == [-1, -1, 128, 128, 256, -1]
 
 
 def _gemm(d, xq=FAKE, sx=FAKE, wq=FAKE, sw=FAKE, out=FAKE, y=None, ws=None, nws=0):
@@ -96,6 +96,9 @@ def test_residual_norm():
         assert _back(desc(), **{name: None}) == B.LOKA_ERR_NULL, name
     for name in ("dy", "hq", "hs", "rstd", "dx", "gamma", "dh", "dg"):
         assert _back(desc(), **{name: ODD}) == B.LOKA_ERR_ALIGN, name
+    OTHER = ctypes.c_void_p(0x2000)        # an output over an input that has another row stride
+    assert _rms(desc(ld_x=264), h=FAKE) == _rms(desc(ld_r=264), x=OTHER, res=FAKE, h=FAKE) == B.LOKA_ERR_SHAPE
+    assert _back(desc(ld_x=264)) == _back(desc(ld_r=264), dy=OTHER, dh=FAKE) == B.LOKA_ERR_SHAPE
     assert _back(desc(), dg=FAKE) == _back(desc(), dg=FAKE, ws=FAKE, nws=16) == B.LOKA_ERR_WORKSPACE
     need = B.lib().loka_rmsnorm_backward_workspace(ctypes.byref(desc()))
     assert need >= 256 * 4 and _back(desc(), dg=FAKE, ws=ctypes.c_void_p(0x1008), nws=need) == B.LOKA_ERR_ALIGN
