@@ -1,12 +1,14 @@
-// Products of MXFP4 operands (include/loka.h, loka_mxfp4_gemm / loka_mxfp4_linear) on v_mfma_scale_f32_16x16x128_f8f6f4.
+// Products of MXFP4 operands (include/loka.h, loka_mxfp4_gemm / loka_mxfp4_linear) on the scaled matrix instructions.
 //
-// The instruction takes 16 x 128 codes of each operand: lane l holds row l % 16, codes 32 (l / 16) .. + 31 in 16 bytes and that
-// group's scale byte, so a lane's operand IS one stored group and its scale.  The weights are the first operand: a lane then
-// holds four consecutive columns n of one row m of the result, which leave as one packed store.
+// With 4-bit operands a lane of v_mfma_scale_f32_16x16x128_f8f6f4 holds row l % 16 and codes 32 (l / 16) .. + 31, and of the
+// 32x32x64 form row l % 32 and codes 32 (l / 32) .. + 31, in 16 bytes, with one scale byte: a lane's operand IS one stored group and its
+// scale.  The weights are the first operand, so that a lane holds neighbouring columns n of one row m of the result.
 //
-// Which 32-groups of a row meet in one instruction is free as long as both operands agree: the four instructions of 512
-// consecutive elements take groups 4 g + s (g: lane / 16, s: instruction), so a lane reads 64 consecutive bytes of codes and
-// one word with the four scale bytes, which the instruction picks by its byte selector.
+// Which 32-groups of a row meet in one instruction is free as long as both operands agree: the four instructions of 512 (256)
+// consecutive elements take groups 4 g + s (g: lane / 16 or lane / 32, s: instruction), so a lane's four scale bytes are one word,
+// from which the instruction picks by its byte selector.
+//
+// Two kernels: few rows stream the weights from memory into registers (16 x 16 x 128), many rows work on tiles in LDS (32 x 32 x 64).
 #include "gemm_common.h"
 #include "mxfp4.h"
 
@@ -34,15 +36,13 @@ struct MxArgs {
     int tiles_m, tiles_n, splits, k_per_split, total;
     float* part;                       // [splits][batch][M][N]
     bool wide;                         // rows of whole 16-byte runs, a tile's within 32-bit offsets
-    // every XCD starts on consecutive tiles, which share operands
-    __device__ __forceinline__ int first_of(int block, int grid) const { return xcd_contiguous(block, grid); }
 };
 
-template <int SA, int SB>
+template <int S>
 __device__ __forceinline__ v4f mx_mfma(const u32x4 a, const u32x4 b, v4f c, uint32_t sa, uint32_t sb) {
     const v8i A = {static_cast<int>(a.x), static_cast<int>(a.y), static_cast<int>(a.z), static_cast<int>(a.w), 0, 0, 0, 0};
     const v8i B = {static_cast<int>(b.x), static_cast<int>(b.y), static_cast<int>(b.z), static_cast<int>(b.w), 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, SA, static_cast<int>(sa), SB, static_cast<int>(sb));
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, c, 4, 4, S, static_cast<int>(sa), S, static_cast<int>(sb));
 }
 
 template <int S>
@@ -147,7 +147,8 @@ __device__ __forceinline__ void in_order() {
 }
 
 // ---------------------------------------------------------------------------------
-// Few rows: bound by the weights' traffic.  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
+// Few rows: bound by the weights' traffic (16 x 4096 x 16384, rows x K x columns, 9.5 us with the quantization of x: 3.8 TB/s of codes;
+// 16 x 8192 x 28672 35 us).  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
 // take 512-element pieces of the contraction in turn, straight from memory into registers, and add their partial sums in LDS
 // in wave order.
 // QUANT 0: stored X.  1, 2, 16: bf16 X of up to 16 rows (MT = 1): by groups, by rows (up to 2, 16).
@@ -201,10 +202,10 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                acc[i][j] = mx_mfma<0, 0>(w[j].c[0], x[i].c[0], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<1, 1>(w[j].c[1], x[i].c[1], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<2, 2>(w[j].c[2], x[i].c[2], acc[i][j], w[j].s, x[i].s);
-                acc[i][j] = mx_mfma<3, 3>(w[j].c[3], x[i].c[3], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<0>(w[j].c[0], x[i].c[0], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<1>(w[j].c[1], x[i].c[1], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<2>(w[j].c[2], x[i].c[2], acc[i][j], w[j].s, x[i].s);
+                acc[i][j] = mx_mfma<3>(w[j].c[3], x[i].c[3], acc[i][j], w[j].s, x[i].s);
             }
     }
     if (QUANT) __syncthreads();        // (the partial sums take the place of other waves' rows)
@@ -308,7 +309,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
     };
 
     // ---- the stream of K tiles: `ld` is the next one to request
-    int ld_tile = a.first_of(blockIdx.x, gridDim.x), ld_k = 0;
+    int ld_tile = xcd_contiguous(blockIdx.x, gridDim.x), ld_k = 0;      // (every XCD starts on consecutive tiles, which share operands)
     if (ld_tile >= total) return;
     Place ld = locate(ld_tile);
     __amdgpu_buffer_rsrc_t xr, wr, sxr, swr;

@@ -415,6 +415,7 @@ loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void
 }
 
 // Workgroups of the backward pass: two a CU, which keep enough loads in flight, so that the partial sums stay small beside the rows
+// (32768 x 4096: 169 us, with three 185, with four 197; 5013 x 1008 10.8, 12.7, 12.7)
 static int64_t backward_groups(int64_t rows, int cols) {
     const int rpw = cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1;
     const int64_t most = (rows + rpw - 1) / rpw;

@@ -124,7 +124,9 @@ def _check(y, xq, sx, wq, sw, K, out=None):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 128), (2, 17, 33), (1, 4096, 4096), (3, 1000, 1111), (13, 64, 8192), (16, 520, 512), (16, 48, 640), (17, 40, 200),
             (33, 65, 1030), (64, 256, 256), (100, 100, 100), (129, 257, 384), (127, 255, 4096), (256, 256, 512), (300, 720, 1008),
-            (513, 1030, 640), (260, 516, 16384), (64, 100, 70000), (1024, 768, 256), (5, 3, 100000), (2500, 130, 64)]
+            (513, 1030, 640), (260, 516, 16384), (64, 100, 70000), (1024, 768, 256), (5, 3, 100000), (2500, 130, 64),
+            # several result tiles a workgroup, in each form of the tile kernel
+            (6000, 6000, 2000), (6001, 6003, 2000), (8200, 8200, 300), (4104, 4104, 4160), (20000, 72, 130)]
 
 
 @pytest.mark.parametrize("M,N,K", PRODUCTS)
@@ -187,16 +189,43 @@ def test_grouped(M, N, K, G, shared):
         r, c = slice(g * M, g * M + M), slice(0, N) if shared else slice(g * N, g * N + N)
         _check(y[r], xq[r], sx[r], wq[c], sw[c], K, out[r])
     # problems apart from each other, and one X for all
-    d = B.make_mxfp4_desc(M, N, K, G, shared_w=shared)
-    d.strideO = M * N + 8
-    far = torch.full((G * d.strideO,), 3.0, device=DEV)
-    d.strideX = 0
-    B.loka_mxfp4_gemm(d, xq, sx, wq, sw, want_out=False, y=far)
-    for g in range(G):
-        c = slice(0, N) if shared else slice(g * N, g * N + N)
-        part = far[g * d.strideO:(g + 1) * d.strideO]
-        _check(part[:M * N].view(M, N), xq[:M], sx[:M], wq[c], sw[c], K)
-        assert bool((part[M * N:] == 3).all())
+    for gap in (8, 3):
+        d = B.make_mxfp4_desc(M, N, K, G, shared_w=shared)
+        d.strideO = M * N + gap
+        far = torch.full((G * d.strideO,), 3.0, device=DEV)
+        d.strideX = 0
+        B.loka_mxfp4_gemm(d, xq, sx, wq, sw, want_out=False, y=far)
+        for g in range(G):
+            c = slice(0, N) if shared else slice(g * N, g * N + N)
+            part = far[g * d.strideO:(g + 1) * d.strideO]
+            _check(part[:M * N].view(M, N), xq[:M], sx[:M], wq[c], sw[c], K)
+            assert bool((part[M * N:] == 3).all())
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 9, 16, 17, 70])
+@pytest.mark.parametrize("K,ld,offset", [(1000, 1008, 8), (1000, 1007, 0), (1000, 1000, 1), (999, 1000, 0), (4736, 5000, 16)])
+def test_layer_on_rows_of_a_larger_matrix(M, K, ld, offset):
+    N = 80
+    buf = torch.randn((M + 1) * ld + 64, device=DEV, generator=_gen(M)).bfloat16()
+    x = buf.as_strided((M, K), (ld, 1), offset)
+    _, wq, sw = _operand(N, K, 8, K ** -0.5)
+    out, y = B.loka_mxfp4_linear(B.make_mxfp4_desc(M, N, K), x, wq, sw, want_y=True)
+    _check(y, *P.mx_quantize(x.contiguous()), wq, sw, K, out)
+
+
+def test_two_streams_at_once():
+    shapes = [(16, 2048, 4096), (300, 1024, 2048), (64, 512, 512), (2000, 512, 1024)]
+    work = [(B.make_mxfp4_desc(M, N, K), torch.randn(M, K, device=DEV, generator=_gen(M)).bfloat16(), *_operand(N, K, N)[1:]) for M, N, K in shapes]
+    want = [B.loka_mxfp4_linear(*w)[0] for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(5):
+        for i, w in enumerate(work):
+            with torch.cuda.stream(streams[i % 2]):
+                got.append((i, B.loka_mxfp4_linear(*w)[0]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[i]) for i, o in got)
 
 
 @pytest.mark.parametrize("M,K,N", [(50, 33, 70), (700, 256, 320), (5013, 128, 96)])
