@@ -69,9 +69,12 @@ __device__ __forceinline__ uint32_t quad_bytes(uint32_t byte) {
 }
 
 // Eight consecutive elements of a row from column c on, zeros from `cols` on; `row` is 16-byte aligned where ALIGNED.
-template <bool ALIGNED>
+template <bool ALIGNED, bool STREAMED = false>
 __device__ __forceinline__ u32x4 mx_load8(const uint16_t* row, int64_t c, int64_t cols) {
-    if (ALIGNED && c + 8 <= cols) return *reinterpret_cast<const u32x4*>(row + c);
+    if (ALIGNED && c + 8 <= cols) {
+        if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + c));      // past the caches
+        return *reinterpret_cast<const u32x4*>(row + c);
+    }
     uint32_t e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : 0u;

@@ -11,7 +11,7 @@ namespace loka {
 // Groups along the row.  16 lanes take one stored block of 128 elements (8 each: one 16-byte load, one word of codes); four
 // lanes share a group; the 16 lanes' four scale bytes leave as one word.  A workgroup takes 16 * U consecutive blocks of the
 // matrix, so that short rows fill it too; U loads of a lane are in flight together.
-template <bool ALIGNED, int U>
+template <bool ALIGNED, int U, bool STREAMED>
 __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
                                                             int64_t ld, uint32_t* __restrict__ q, uint32_t* __restrict__ scales) {
     const int t = static_cast<int>(threadIdx.x), l16 = t & 15;
@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __re
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (row < rows) v[u] = mx_load8<ALIGNED>(x + row * ld, b * kMxPad + l16 * 8, cols);
+        if (row < rows) v[u] = mx_load8<ALIGNED, STREAMED>(x + row * ld, b * kMxPad + l16 * 8, cols);
         row += step_row;
         b += step_b;
         if (b >= nb) { b -= nb; ++row; }
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __re
 // columns of rows 32 w ..: a whole group each, so its maximum needs no exchange.  The codes turn in LDS and leave as up to
 // 128 consecutive bytes of an output row.
 constexpr int kTurnRows = 256, kTurnCols = 128, kTurnPitch = kTurnRows / 2 + 16;      // (pitch: 16 bytes more, so that columns start on other banks)
-template <bool ALIGNED>
+template <bool ALIGNED, bool STREAMED>
 __global__ __launch_bounds__(512) void mx_quant_turned_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
                                                               int64_t ld, uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     __shared__ __align__(16) uint8_t codes[kTurnCols * kTurnPitch];
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(512) void mx_quant_turned_kernel(const uint16_t* __
         w[r] = 0u;
         const uint16_t* p = x + (r0 + r) * ld + c;
         if (r0 + r < rows) {
-            if (ALIGNED && c + 1 < cols) w[r] = *reinterpret_cast<const uint32_t*>(p);
+            if (ALIGNED && c + 1 < cols) w[r] = STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
             else {
                 if (c < cols) w[r] = p[0];
                 if (c + 1 < cols) w[r] |= static_cast<uint32_t>(p[1]) << 16;
@@ -200,20 +200,25 @@ static bool wide_rows(const void* p, int64_t ld) { return aligned16(p) && ld % 8
 loka_status mxfp4_quantize_launch(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                   uint8_t* scales, hipStream_t stream) {
     const uint16_t* x = static_cast<const uint16_t*>(x_bf16);
+    // An input that the 256 MB of last-level cache cannot hold is read past it: 32768 x 4096 62 -> 58 us, turned 72 -> 65. A smaller one may
+    // lie there already, and loses: 16384 x 4096 27.8 -> 31.8 us when its values were read just before, and 31.3 -> 31.4 when not.
+    const bool streamed = rows * cols >= INT64_C(1) << 27;
     if (transpose_out) {
         const int64_t grid = ((rows + kTurnRows - 1) / kTurnRows) * ((cols + kTurnCols - 1) / kTurnCols);
         if (grid >= kMaxThreads / 512) return LOKA_ERR_SHAPE;
         const bool pairs = (reinterpret_cast<uintptr_t>(x_bf16) & 3u) == 0 && ld % 2 == 0;
-        if (pairs) mx_quant_turned_kernel<true><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
-        else mx_quant_turned_kernel<false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
+        if (pairs && streamed) mx_quant_turned_kernel<true, true><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
+        else if (pairs) mx_quant_turned_kernel<true, false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
+        else mx_quant_turned_kernel<false, false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
     } else {
         constexpr int U = 4;
         const int64_t grid = (rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U);
         if (grid >= kMaxThreads / 256) return LOKA_ERR_SHAPE;
         uint32_t* qw = reinterpret_cast<uint32_t*>(q);
         uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
-        if (wide_rows(x_bf16, ld)) mx_quant_rows_kernel<true, U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
-        else mx_quant_rows_kernel<false, U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        if (wide_rows(x_bf16, ld) && streamed) mx_quant_rows_kernel<true, U, true><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        else if (wide_rows(x_bf16, ld)) mx_quant_rows_kernel<true, U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        else mx_quant_rows_kernel<false, U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
     }
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;

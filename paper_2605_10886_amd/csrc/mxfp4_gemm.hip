@@ -36,6 +36,7 @@ struct MxArgs {
     int tiles_m, tiles_n, splits, k_per_split, total;
     float* part;                       // [splits][batch][M][N]
     bool wide;                         // rows of whole 16-byte runs, a tile's within 32-bit offsets
+    bool streamed;                     // bf16 values past the caches
 };
 
 template <int S>
@@ -505,7 +506,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
             const int N = static_cast<int>(a.N), n_lane = at.n0 + n_wave + eh * 8, o_lane = (m_wave + er) * N + n_lane;
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
             // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
-            auto store = [&](const __amdgpu_buffer_rsrc_t& o, u32x4 first, u32x4 second, int i, int n, int size) __attribute__((always_inline)) {
+            auto store = [&](bool streamed, const __amdgpu_buffer_rsrc_t& o, u32x4 first, u32x4 second, int i, int n, int size) __attribute__((always_inline)) {
                 const bool in = n_lane + n < N;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -514,8 +515,16 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
                     second[e] = t.y;
                 }
                 const int off = (o_lane + i * 32 * N + n) * size;
-                __builtin_amdgcn_raw_buffer_store_b128(first, o, in ? off : 0x7FFFFFFF, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(second, o, in ? off + 16 * N * size : 0x7FFFFFFF, 0, 0);
+                const int first_at = in ? off : 0x7FFFFFFF, second_at = in ? off + 16 * N * size : 0x7FFFFFFF;
+                if (streamed) {        // (how a store meets the caches is in its instruction; the lines keep the two from being joined)
+                    __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 2);
+                    __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 2);
+                    asm volatile("; past the caches");
+                } else {
+                    __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 0);
+                    asm volatile("; into the caches");
+                }
             };
             if (out) {
                 const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000);
@@ -524,7 +533,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const v16f v = acc[i][j];
-                        store(o, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])},
+                        store(a.streamed, o, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])},
                               u32x4{pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15])}, i, j * 32 + es * 16, 2);
                     }
             }
@@ -536,7 +545,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
                     for (int j = 0; j < 2 * TN; ++j) {
                         const v16f v = acc[i][j >> 1];
                         auto word = [&](int e) __attribute__((always_inline)) { return __float_as_uint(v[(j & 1) * 8 + e]); };
-                        store(o, u32x4{word(0), word(1), word(2), word(3)}, u32x4{word(4), word(5), word(6), word(7)}, i, j * 16 + es * 4, 4);
+                        store(false, o, u32x4{word(0), word(1), word(2), word(3)}, u32x4{word(4), word(5), word(6), word(7)}, i, j * 16 + es * 4, 4);
                     }
             }
             late = out && !y ? C::R - 1 : 0;
@@ -703,6 +712,10 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     a.k_per_split = p.k_per_split;
     a.total = static_cast<int>(p.total);
     a.part = static_cast<float*>(ws);
+    // A bf16 result that the 256 MB of last-level cache would not hold leaves that cache to the operands (rows x columns x K:
+    // 32768 x 4096 x 4096 333 -> 303 us, 40000 x 4096 x 1000 161 -> 127, 65536 x 2048 x 1024 112 -> 103); smaller ones gain little or lose
+    // (24576 x 4096 x 4096 240 -> 230, 49152 x 2048 x 2048 114 -> 119, 4096 x 4096 x 4096 42.9 -> 43.8), and the next kernel may read them there.
+    a.streamed = a.M * a.N * d->batch >= INT64_C(1) << 27;
     a.wide = a.N % 8 == 0 && a.N < (INT64_C(1) << 21) && (d->batch == 1 || d->strideO % 8 == 0);
     using Large = MxTile<2, 4, 4, 2, 1, 2>;
     using Halves = MxTile<2, 2, 2, 2, 2, 3>;

@@ -240,6 +240,36 @@ def test_training_step(M, K, N):
         _check(y, *a, *b, ml, out)
 
 
+def test_values_that_pass_the_caches_by():
+    # inputs and results of 2^27 elements and more: codes against those of the halves, small whole numbers against exact products
+    M, K = 32768 + 131, 4104
+    x = _wide(1, M * K, seed=3).view(M, K)
+    q, s = B.loka_mxfp4_quantize(x)
+    qt, st = B.loka_mxfp4_quantize(x, True)
+    for a, b in ((0, 16384), (16384, M)):
+        hq, hs = B.loka_mxfp4_quantize(x[a:b])
+        _same(q[a:b], hq)
+        _same(s[a:b], hs)
+        hq, hs = B.loka_mxfp4_quantize(x[a:b], True)
+        _same(qt[:, a // 2: a // 2 + hq.shape[1]], hq)
+        _same(st[:, a // 32: a // 32 + hs.shape[1]], hs)
+    del x, q, s, qt, st
+    K, N = 160, 4104
+    codes = torch.tensor([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6], device=DEV)
+    x, w = (codes[torch.randint(0, 15, s, device=DEV, generator=_gen(s[0]))].bfloat16() for s in ((M, K), (N, K)))
+    x[:, ::32], w[:, ::32] = 6, 6      # (every group's scale is 1)
+    a, b = B.loka_mxfp4_quantize(x), B.loka_mxfp4_quantize(w)
+    want = (x.float() @ w.float().t()).bfloat16()      # multiples of 1/4 up to 5760: exact in fp32
+    d = B.make_mxfp4_desc(M, N, K)
+    out, _ = B.loka_mxfp4_gemm(d, *a, *b)
+    _same(out, want)
+    out, _ = B.loka_mxfp4_linear(d, x, *b)
+    _same(out, want)
+    out, y = B.loka_mxfp4_gemm(d, *a, *b, want_y=True)
+    _same(out, want)
+    _same(y.bfloat16(), want)
+
+
 def test_rows_past_4_gb():
     # stored codes beyond 2^32 bytes: the last rows of a tall operand, against the same rows alone
     M, K, N = (1 << 21) + 37, 4096, 32
