@@ -36,6 +36,17 @@ __device__ __forceinline__ float most(float a, float b) {  // of magnitudes, a N
     return __uint_as_float(__float_as_uint(a) > __float_as_uint(b) ? __float_as_uint(a) : __float_as_uint(b));
 }
 
+// A row's inputs and results, STREAMED past the caches
+template <bool STREAMED>
+__device__ __forceinline__ u32x4 load16(const uint16_t* p) {
+    return STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p);
+}
+template <bool STREAMED>
+__device__ __forceinline__ void store16(uint16_t* p, u32x4 v) {
+    if (STREAMED) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = v;
+}
+
 __device__ __forceinline__ void unpack8(const u32x4 w, float (&f)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
@@ -59,7 +70,7 @@ __device__ __forceinline__ void e4m3_group(bool pow2, float am, float rstd, floa
 // ---------------------------------------------------------------------------------
 // T threads take a row (T = 16, 32, 64: several rows a wave or one; 256, 1024: a workgroup per row), CPL chunks of 8
 // consecutive elements each, chunk j of thread t at 8 (t + j T): a group of 128 elements is 16 neighbouring lanes, one of 32 a quad.
-template <int T, int CPL>
+template <int T, int CPL, bool STREAMED>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const RmsArgs a) {
     constexpr int WG = T < 256 ? 256 : T;
     __shared__ float red[3][WG / 64];
@@ -75,8 +86,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
         u32x4 xv = u32x4{0u, 0u, 0u, 0u}, rv = u32x4{0u, 0u, 0u, 0u};
         g[j] = u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
         if (live && c < chunks) {
-            xv = *reinterpret_cast<const u32x4*>(a.x + row * a.ld_x + c * 8);
-            if (a.res) rv = *reinterpret_cast<const u32x4*>(a.res + row * a.ld_r + c * 8);
+            xv = load16<STREAMED>(a.x + row * a.ld_x + c * 8);
+            if (a.res) rv = load16<STREAMED>(a.res + row * a.ld_r + c * 8);
             if (a.gamma) g[j] = *reinterpret_cast<const u32x4*>(a.gamma + c * 8);
         }
         unpack8(xv, h[j]);
@@ -90,7 +101,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
             u32x4 o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(h[j][2 * i], h[j][2 * i + 1]);
-            *reinterpret_cast<u32x4*>(a.h_out + row * a.cols + c * 8) = o;
+            store16<STREAMED>(a.h_out + row * a.cols + c * 8, o);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[j][i], h[j][i], sum);
@@ -168,7 +179,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
             u32x4 o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(v[2 * i] * rstd, v[2 * i + 1] * rstd);
-            if (c < chunks) *reinterpret_cast<u32x4*>(a.y_bf16 + at * 8) = o;
+            if (c < chunks) store16<false>(a.y_bf16 + at * 8, o);
         } else if (a.out == LOKA_RMS_OUT_E4M3) {
             if (!row_y) {
                 float m = 0.f;
@@ -222,7 +233,7 @@ __device__ __forceinline__ void e4m3_values(const u32x2 w, float (&f)[8]) {
 // leaves one row of partial sums.  A row stays in its loaded form (11 registers a chunk, 16 as fp32) between its two
 // uses, so that the next row's loads are in flight while this one is reduced (PREFETCH; not in 1024 threads, which have half
 // the registers).
-template <int T, int CPL, bool PREFETCH>
+template <int T, int CPL, bool PREFETCH, bool STREAMED>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(const RmsBackArgs a) {
     constexpr int WG = T < 256 ? 256 : T, RPW = WG / T;
     __shared__ float red[2][WG / 64];
@@ -239,10 +250,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(con
             v.q[j] = u32x2{0u, 0u};
             v.s[j] = 0.f;
             if (row < a.rows && c < chunks) {
-                v.dy[j] = *reinterpret_cast<const u32x4*>(a.dy + row * a.ld_dy + c * 8);
+                v.dy[j] = load16<STREAMED>(a.dy + row * a.ld_dy + c * 8);
                 v.q[j] = *reinterpret_cast<const u32x2*>(a.hq + (row * chunks + c) * 8);
                 v.s[j] = a.ckpt_mode == kModeRow ? a.hs[row] : a.hs[row * (a.cols >> 7) + (c >> 4)];
-                if (PREFETCH && a.dh) v.dh[j] = *reinterpret_cast<const u32x4*>(a.dh + row * a.ld_dh + c * 8);
+                if (PREFETCH && a.dh) v.dh[j] = load16<STREAMED>(a.dh + row * a.ld_dh + c * 8);
             }
         }
         return v;
@@ -299,14 +310,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(con
                 unpack8(v.dy[j], d);
                 e4m3_values(v.q[j], n);
                 unpack8(KEEP ? g[KEEP ? j : 0] : gamma_of(j), gf);
-                if (!PREFETCH && a.dh) v.dh[j] = *reinterpret_cast<const u32x4*>(a.dh + row * a.ld_dh + c * 8);
+                if (!PREFETCH && a.dh) v.dh[j] = load16<STREAMED>(a.dh + row * a.ld_dh + c * 8);
                 unpack8(v.dh[j], e);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[i] = __builtin_fmaf(v.rstd, __builtin_fmaf(-mean, n[i] * v.s[j], d[i] * gf[i]), e[i]);
                 u32x4 o;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(e[2 * i], e[2 * i + 1]);
-                *reinterpret_cast<u32x4*>(a.dx + row * a.cols + c * 8) = o;
+                store16<STREAMED>(a.dx + row * a.cols + c * 8, o);
             }
         }
         if (PREFETCH) v = next;
@@ -369,12 +380,18 @@ static int kernel_mode(int mode) {
     return mode == LOKA_SCALE_ROW ? kModeRow : mode == LOKA_SCALE_BLOCK_1x128 ? kModeBlock : kModePow2;
 }
 
+// From here on the 256 MB of last-level cache cannot hold what a call moves (5 to 8 bytes an element), and rows that pass it by are
+// faster (8192 x 8192: forward 87 -> 76 us, with the checkpoint 100 -> 87, backward 93 -> 84); below they lose (8192 x 4096: 36 -> 41,
+// 43 -> 47, 39 -> 42).  y stays in the caches, at no cost: the next product reads it.
+static bool streamed(int64_t rows, int64_t cols) { return rows * cols >= INT64_C(1) << 26; }
+
 template <int T, int CPL>
 static loka_status forward_launch(const RmsArgs& a, hipStream_t stream) {
     constexpr int WG = T < 256 ? 256 : T;
     const int64_t grid = (a.rows + WG / T - 1) / (WG / T);
     if (grid >= kMaxThreads / WG) return LOKA_ERR_SHAPE;
-    add_rmsnorm_kernel<T, CPL><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(a);
+    if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(a);
+    else add_rmsnorm_kernel<T, CPL, false><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(a);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }
@@ -401,7 +418,7 @@ loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void
     a.ckpt_mode = hq ? kernel_mode(d->ckpt_mode) : kModeNone;
     a.eps = d->eps;
     // One or two chunks a lane wherever lanes suffice: more rows than registers hold at once stay in flight (a wave a row, 8 chunks a
-    // lane: 32768 x 4096 with the checkpoint 217 us, here 193; 4096 x 2048 15.1 and 12.9).
+    // lane: 32768 x 4096 with the checkpoint 217 us, here 193, both through the caches; 4096 x 2048 15.1 and 12.9).
     const int chunks = a.cols / 8;
     if (chunks <= 16) return forward_launch<16, 1>(a, stream);
     if (chunks <= 32) return forward_launch<32, 1>(a, stream);
@@ -415,7 +432,7 @@ loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void
 }
 
 // Workgroups of the backward pass: two a CU, which keep enough loads in flight, so that the partial sums stay small beside the rows
-// (32768 x 4096: 169 us, with three 185, with four 197; 5013 x 1008 10.8, 12.7, 12.7)
+// (32768 x 4096 through the caches: 169 us, with three 185, with four 197; 5013 x 1008 10.8, 12.7, 12.7)
 static int64_t backward_groups(int64_t rows, int cols) {
     const int rpw = cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1;
     const int64_t most = (rows + rpw - 1) / rpw;
@@ -428,7 +445,9 @@ size_t rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols) {
 
 template <int T, int CPL, bool PREFETCH = true>
 static void backward_launch(const RmsBackArgs& a, int64_t groups, hipStream_t stream) {
-    rmsnorm_backward_kernel<T, CPL, PREFETCH><<<static_cast<uint32_t>(groups), T < 256 ? 256 : T, 0, stream>>>(a);
+    constexpr int WG = T < 256 ? 256 : T;
+    if (streamed(a.rows, a.cols)) rmsnorm_backward_kernel<T, CPL, PREFETCH, true><<<static_cast<uint32_t>(groups), WG, 0, stream>>>(a);
+    else rmsnorm_backward_kernel<T, CPL, PREFETCH, false><<<static_cast<uint32_t>(groups), WG, 0, stream>>>(a);
 }
 
 loka_status rmsnorm_backward_launch(const loka_rms_desc* d, const void* dy, const uint8_t* hq, const float* hs, const float* rstd,

@@ -235,6 +235,32 @@ def test_gradient_against_differences():
     assert abs(float((dg.double() * u).sum() - dgd)) <= 1e-5 * float((dg.double() * u).abs().sum())
 
 
+@pytest.mark.parametrize("cols", [128, 256, 496, 1008, 2048, 4096, 8192, 16384, 32768])
+def test_rows_that_pass_the_caches_by(cols):
+    # a call of 2^26 elements and more, against its halves
+    rows = (1 << 26) // cols + 3
+    x, r, w = _inputs(rows, cols, cols)
+    blk = B.SCALE_BLOCK_1x128 if cols % 128 == 0 else B.SCALE_ROW
+    parts = slice(0, rows // 2), slice(rows // 2, rows)
+    for out in (B.RMS_OUT_BF16, B.RMS_OUT_MXFP4):
+        kw = dict(out=out, ckpt_mode=blk)
+        f, halves = B.loka_add_rmsnorm(x, r, w, **kw), [B.loka_add_rmsnorm(x[p], r[p], w, **kw) for p in parts]
+        for k in ("h", "y", "hq", "hs", "rstd") + (("scales",) if out != B.RMS_OUT_BF16 else ()):
+            for p, h in zip(parts, halves):
+                assert torch.equal(getattr(f, k)[p], getattr(h, k)), k
+    dx, dg = B.loka_rmsnorm_backward(r, f.hq, f.hs, f.rstd, w, x, ckpt_mode=blk)
+    sums = 0
+    for p, h in zip(parts, halves):
+        part, part_dg = B.loka_rmsnorm_backward(r[p], h.hq, h.hs, h.rstd, w, x[p], ckpt_mode=blk)
+        assert torch.equal(dx[p], part)
+        sums = sums + part_dg.double()
+    # a column's terms in chains of rows / 512, 16 rows of a workgroup, 16 and 32 partial sums; two such sums, each term with 3 roundings
+    values = P.e4m3_values(f.hq).view(rows, cols).abs()
+    scale = f.hs.double().view(rows, -1, 1) * f.rstd.double().view(rows, 1, 1)
+    size = ((values.view(rows, f.hs.numel() // rows, -1) * scale).view(rows, cols) * r.double().abs()).sum(0)
+    assert bool(((dg.double() - sums).abs() <= 2 * (rows / 512 + 1 + 64 + 3) * P.F32 * size).all())
+
+
 def test_rows_past_4_gb():
     rows, cols = (1 << 20) + 19, 4224                 # codes and bf16 rows beyond 2^32 bytes
     x = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
