@@ -167,9 +167,17 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
                 e4m3_group(a.ckpt_mode == kModePow2, m, 1.0f, sh, ih);
                 if ((t & 15) == 0 && c < chunks) a.hs[row * (a.cols >> 7) + (c >> 4)] = sh;
             }
-            if (c < chunks)
-                *reinterpret_cast<u32x2*>(a.hq + at * 2) = u32x2{e4m3x4(h[j][0] * ih, h[j][1] * ih, h[j][2] * ih, h[j][3] * ih),
-                                                                  e4m3x4(h[j][4] * ih, h[j][5] * ih, h[j][6] * ih, h[j][7] * ih)};
+            // (past the caches too where y is bf16, 32768 x 4096 217 -> 187 us; beside codes it costs: e4m3 172 -> 176, MXFP4 158 -> 168)
+            const u32x2 o = u32x2{e4m3x4(h[j][0] * ih, h[j][1] * ih, h[j][2] * ih, h[j][3] * ih), e4m3x4(h[j][4] * ih, h[j][5] * ih, h[j][6] * ih, h[j][7] * ih)};
+            if (c < chunks) {
+                if (STREAMED && a.out == LOKA_RMS_OUT_BF16) {
+                    asm volatile("; past the caches");         // (or the two stores become one through the caches)
+                    __builtin_nontemporal_store(o, reinterpret_cast<u32x2*>(a.hq + at * 2));
+                    asm volatile("; past the caches");
+                } else {
+                    *reinterpret_cast<u32x2*>(a.hq + at * 2) = o;
+                }
+            }
         }
         float gf[8], v[8];
         unpack8(g[j], gf);
@@ -382,7 +390,8 @@ static int kernel_mode(int mode) {
 
 // From here on the 256 MB of last-level cache cannot hold what a call moves (5 to 8 bytes an element), and rows that pass it by are
 // faster (8192 x 8192: forward 87 -> 76 us, with the checkpoint 100 -> 87, backward 93 -> 84); below they lose (8192 x 4096: 36 -> 41,
-// 43 -> 47, 39 -> 42).  y stays in the caches, at no cost: the next product reads it.
+// 43 -> 47, 39 -> 42).  y goes through
+// the caches: the next product reads it, and the call itself is faster (32768 x 4096: codes past them too 148 -> 160 us, bf16 158 -> 184).
 static bool streamed(int64_t rows, int64_t cols) { return rows * cols >= INT64_C(1) << 26; }
 
 template <int T, int CPL>
