@@ -316,7 +316,7 @@ loka_status loka_fp8_linear_norm_xq(const loka_gemm_desc* desc, const void* x_bf
  * A group with a NaN or an infinity gets byte 255 and zero codes: all of its values are NaN, and so is every product sum
  * that it enters.  Bit-exact with this recipe.
  *
- *   x_bf16  [rows, ld] bf16, ld >= cols, aligned to 2 bytes (rows that start on multiples of 16 bytes are read in wide loads)
+ *   x_bf16  [rows, ld] bf16, ld >= cols, aligned to 2 bytes (rows that start on multiples of 4 bytes are read fastest)
  *   transpose_out != 0: the operand is the transpose, [cols, rows], whose groups run along the ROWS of x: codes
  *   [cols, rowsp / 2], scales [cols, rowsp / 32], rowsp = rows up to a multiple of 128.  What weights [K, N] take for the
  *   forward product, and X and dY for dW = X^T dY.
@@ -337,7 +337,7 @@ loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64
  *           problem g start at byte g * strideX / 32)
  *   wq, sw  likewise [N, K] with strideW
  *   out_bf16 [batch][M, N] bf16 and / or y_fp32 [batch][M, N] fp32, strideO elements apart; at least one is not NULL.
- *           16-byte aligned; rows are N elements apart, whatever N (with N and strideO multiples of 8, stores are 16 bytes wide).
+ *           16-byte aligned; rows are N elements apart, whatever N (an odd N makes bf16 results that start inside a word, and slower).
  * Workspace: loka_mxfp4_gemm_workspace(desc) bytes (partial sums, where a long contraction is split over workgroups
  * because there are few output tiles; added in a fixed order: results do not change from call to call).  NULL / less: the
  * product runs unsplit, adding in another order.  16-byte aligned, not shared with a call still running. */

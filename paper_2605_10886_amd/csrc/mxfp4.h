@@ -68,12 +68,18 @@ __device__ __forceinline__ uint32_t quad_bytes(uint32_t byte) {
     return w;
 }
 
-// Eight consecutive elements of a row from column c on, zeros from `cols` on; `row` is 16-byte aligned where ALIGNED.
-template <bool ALIGNED, bool STREAMED = false>
+// Wide accesses that need no more than their elements' alignment: rows start anywhere (by elements, us: codes of 8191 x 4095 36.9, here
+// 17.6; transposed 22.8 and 19.6; values 22.1 and 14.5)
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
+
+// Eight consecutive elements of a row from column c on, zeros from `cols` on; STREAMED past the caches.
+template <bool STREAMED = false>
 __device__ __forceinline__ u32x4 mx_load8(const uint16_t* row, int64_t c, int64_t cols) {
-    if (ALIGNED && c + 8 <= cols) {
-        if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + c));      // past the caches
-        return *reinterpret_cast<const u32x4*>(row + c);
+    if (c + 8 <= cols) {
+        if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + c));
+        return *reinterpret_cast<const u32x4_any*>(row + c);
     }
     uint32_t e[8];
 #pragma unroll

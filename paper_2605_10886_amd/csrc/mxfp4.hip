@@ -11,7 +11,7 @@ namespace loka {
 // Groups along the row.  16 lanes take one stored block of 128 elements (8 each: one 16-byte load, one word of codes); four
 // lanes share a group; the 16 lanes' four scale bytes leave as one word.  A workgroup takes 16 * U consecutive blocks of the
 // matrix, so that short rows fill it too; U loads of a lane are in flight together.
-template <bool ALIGNED, int U, bool STREAMED>
+template <int U, bool STREAMED>
 __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
                                                             int64_t ld, uint32_t* __restrict__ q, uint32_t* __restrict__ scales) {
     const int t = static_cast<int>(threadIdx.x), l16 = t & 15;
@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __re
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (row < rows) v[u] = mx_load8<ALIGNED, STREAMED>(x + row * ld, b * kMxPad + l16 * 8, cols);
+        if (row < rows) v[u] = mx_load8<STREAMED>(x + row * ld, b * kMxPad + l16 * 8, cols);
         row += step_row;
         b += step_b;
         if (b >= nb) { b -= nb; ++row; }
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __re
 // columns of rows 32 w ..: a whole group each, so its maximum needs no exchange.  The codes turn in LDS and leave as up to
 // 128 consecutive bytes of an output row.
 constexpr int kTurnRows = 256, kTurnCols = 128, kTurnPitch = kTurnRows / 2 + 16;      // (pitch: 16 bytes more, so that columns start on other banks)
-template <bool ALIGNED, bool STREAMED>
+template <bool STREAMED>
 __global__ __launch_bounds__(512) void mx_quant_turned_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
                                                               int64_t ld, uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     __shared__ __align__(16) uint8_t codes[kTurnCols * kTurnPitch];
@@ -64,11 +64,8 @@ __global__ __launch_bounds__(512) void mx_quant_turned_kernel(const uint16_t* __
         w[r] = 0u;
         const uint16_t* p = x + (r0 + r) * ld + c;
         if (r0 + r < rows) {
-            if (ALIGNED && c + 1 < cols) w[r] = STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
-            else {
-                if (c < cols) w[r] = p[0];
-                if (c + 1 < cols) w[r] |= static_cast<uint32_t>(p[1]) << 16;
-            }
+            if (c + 1 < cols) w[r] = STREAMED ? __builtin_nontemporal_load(reinterpret_cast<const u32_any*>(p)) : *reinterpret_cast<const u32_any*>(p);
+            else if (c < cols) w[r] = p[0];
         }
     }
     uint32_t a = 0u;
@@ -123,7 +120,7 @@ __device__ __forceinline__ u32x4 mx_values8(uint32_t codes, uint32_t byte) {
 }
 
 // The values of stored codes: a lane turns one word (8 codes) into 16 bytes.
-template <bool ALIGNED, int U>
+template <int U>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint32_t* __restrict__ q, const uint8_t* __restrict__ scales, int64_t rows,
                                                          int64_t cols, uint16_t* __restrict__ out, int64_t ld) {
     const int t = static_cast<int>(threadIdx.x), l16 = t & 15;
@@ -144,7 +141,7 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint32_t* __restr
         if (row < rows && c < cols) {
             u32x4 o = mx_values8(v[u], s[u]);
             uint16_t* p = out + row * ld + c;
-            if (ALIGNED && c + 8 <= cols) *reinterpret_cast<u32x4*>(p) = o;
+            if (c + 8 <= cols) *reinterpret_cast<u32x4_any*>(p) = o;
             else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -157,45 +154,8 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint32_t* __restr
     }
 }
 
-// The same for contiguous rows of any length (rows that start anywhere): a lane writes 16 aligned bytes, whose eight elements begin
-// inside a word of codes and may lie in two groups; where they lie in two rows it takes them one by one.  1008 x 5013
-// (5013 columns) 11 us by single elements -> 6.7 us.
-__global__ __launch_bounds__(256) void mx_dequant_dense_kernel(const uint32_t* __restrict__ q, const uint8_t* __restrict__ scales, int64_t rows,
-                                                               int64_t cols, double per_col, uint16_t* __restrict__ out) {
-    const int64_t first = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8, total = rows * cols;
-    if (first >= total) return;
-    const int64_t nb = (cols + kMxPad - 1) / kMxPad;
-    int64_t row = static_cast<int64_t>(static_cast<double>(first) * per_col), c = first - row * cols;      // (off by at most one row)
-    if (c < 0) { c += cols; --row; }
-    if (c >= cols) { c -= cols; ++row; }
-    if (c + 8 <= cols) {
-        const uint32_t* w = q + row * nb * 16 + (c >> 3);
-        const int at = static_cast<int>(c & 7), split = 32 - static_cast<int>(c & 31);           // elements from `split` on: the next group
-        const uint32_t codes = __builtin_amdgcn_alignbit(w[at ? 1 : 0], w[0], at * 4);
-        const uint8_t* s = scales + row * nb * 4;
-        u32x4 o = mx_values8(codes, s[c >> 5]);
-        if (split < 8) {
-            const u32x4 n = mx_values8(codes, s[(c + 7) >> 5]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = 2 * i < split ? o[i] : n[i], hi = 2 * i + 1 < split ? o[i] : n[i];
-                o[i] = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
-            }
-        }
-        *reinterpret_cast<u32x4*>(out + first) = o;
-    } else {
-        for (int i = 0; i < 8 && first + i < total; ++i) {
-            const uint32_t word = q[row * nb * 16 + (c >> 3)];
-            const u32x4 o = mx_values8(word >> ((c & 7) * 4), scales[row * nb * 4 + (c >> 5)]);
-            out[first + i] = static_cast<uint16_t>(o.x);
-            if (++c == cols) { c = 0; ++row; }
-        }
-    }
-}
-
 // ---------------------------------------------------------------------------------
 constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
-static bool wide_rows(const void* p, int64_t ld) { return aligned16(p) && ld % 8 == 0; }
 
 loka_status mxfp4_quantize_launch(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                   uint8_t* scales, hipStream_t stream) {
@@ -206,19 +166,16 @@ loka_status mxfp4_quantize_launch(const void* x_bf16, int64_t rows, int64_t cols
     if (transpose_out) {
         const int64_t grid = ((rows + kTurnRows - 1) / kTurnRows) * ((cols + kTurnCols - 1) / kTurnCols);
         if (grid >= kMaxThreads / 512) return LOKA_ERR_SHAPE;
-        const bool pairs = (reinterpret_cast<uintptr_t>(x_bf16) & 3u) == 0 && ld % 2 == 0;
-        if (pairs && streamed) mx_quant_turned_kernel<true, true><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
-        else if (pairs) mx_quant_turned_kernel<true, false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
-        else mx_quant_turned_kernel<false, false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
+        if (streamed) mx_quant_turned_kernel<true><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
+        else mx_quant_turned_kernel<false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
     } else {
         constexpr int U = 4;
         const int64_t grid = (rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U);
         if (grid >= kMaxThreads / 256) return LOKA_ERR_SHAPE;
         uint32_t* qw = reinterpret_cast<uint32_t*>(q);
         uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
-        if (wide_rows(x_bf16, ld) && streamed) mx_quant_rows_kernel<true, U, true><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
-        else if (wide_rows(x_bf16, ld)) mx_quant_rows_kernel<true, U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
-        else mx_quant_rows_kernel<false, U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        if (streamed) mx_quant_rows_kernel<U, true><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        else mx_quant_rows_kernel<U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
     }
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
@@ -231,11 +188,7 @@ loka_status mxfp4_dequantize_launch(const uint8_t* q, const uint8_t* scales, int
     if (grid >= kMaxThreads / 256) return LOKA_ERR_SHAPE;
     const uint32_t* qw = reinterpret_cast<const uint32_t*>(q);
     uint16_t* out = static_cast<uint16_t*>(out_bf16);
-    const int64_t dense = (rows * cols + 2047) / 2048;
-    if (wide_rows(out_bf16, ld)) mx_dequant_kernel<true, U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(qw, scales, rows, cols, out, ld);
-    else if (aligned16(out_bf16) && ld == cols && dense < kMaxThreads / 256)
-        mx_dequant_dense_kernel<<<static_cast<uint32_t>(dense), 256, 0, stream>>>(qw, scales, rows, cols, 1.0 / static_cast<double>(cols), out);
-    else mx_dequant_kernel<false, U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(qw, scales, rows, cols, out, ld);
+    mx_dequant_kernel<U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(qw, scales, rows, cols, out, ld);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }

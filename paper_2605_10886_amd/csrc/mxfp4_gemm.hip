@@ -88,7 +88,7 @@ __device__ __forceinline__ MxPiece mx_quantize_rows(const uint16_t* x, int64_t l
         if (whole) {                   // no run of 8 is cut by the row's end
             const u32x4 w = *reinterpret_cast<const u32x4*>(x + i * ldx + (c < K ? c : 0));
             v[i] = c < K ? w : u32x4{0u, 0u, 0u, 0u};
-        } else v[i] = mx_load8<false>(x + i * ldx, c, K);
+        } else v[i] = mx_load8(x + i * ldx, c, K);
     }
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -225,9 +225,9 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
         const int64_t m = m0 + (tile / NT) * 16 + (l & 15), n = n0 + (tile % NT) * 16 + (l >> 4) * 4;
         if (m >= a.M) continue;
         const int64_t o = prob * a.strideO + m * a.N + n;
-        if (n + 4 <= a.N && ((a.N | a.strideO) & 3) == 0) {
-            if (a.out) *reinterpret_cast<u32x2*>(a.out + o) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
-            if (a.y) *reinterpret_cast<v4f*>(a.y + o) = s;
+        if (n + 4 <= a.N) {
+            if (a.out) *reinterpret_cast<u32x2_any*>(a.out + o) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
+            if (a.y) *reinterpret_cast<u32x4_any*>(a.y + o) = __builtin_bit_cast(u32x4, s);
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -501,71 +501,91 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
         float* const y = SPLIT ? a.part + (static_cast<int64_t>(at.split) * a.batch + at.prob) * a.M * a.N : a.y ? a.y + at.prob * a.strideO : nullptr;
         uint16_t* const out = SPLIT || !a.out ? nullptr : a.out + at.prob * a.strideO;
         const int el = lane_id(), er = el & 15, es = (el >> 4) & 1, eh = el >> 5;       // (not kept through the loop, nor what follows from them)
+        // (where a run of a row lies in one lane: `first` of row er, `second` of row er + 16, both from column n on)
+        auto turn = [&](u32x4& first, u32x4& second) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const u32_pair t = __builtin_amdgcn_permlane16_swap(first[e], second[e], false, false);
+                first[e] = t.x;
+                second[e] = t.y;
+            }
+        };
+        // every run of the wave's tiles: bf16 in runs of 8 columns, fp32 in runs of 4
+        auto bf16_runs = [&](auto store) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const v16f v = acc[i][j];
+                    u32x4 first{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                    u32x4 second{pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15])};
+                    turn(first, second);
+                    store(first, second, i, j * 32 + es * 16);
+                }
+        };
+        auto fp32_runs = [&](auto store) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int j = 0; j < 2 * TN; ++j) {
+                    const v16f v = acc[i][j >> 1];
+                    auto word = [&](int e) __attribute__((always_inline)) { return __float_as_uint(v[(j & 1) * 8 + e]); };
+                    u32x4 first{word(0), word(1), word(2), word(3)}, second{word(4), word(5), word(6), word(7)};
+                    turn(first, second);
+                    store(first, second, i, j * 16 + es * 4);
+                }
+        };
         if (a.wide) {                  // whole runs of 8 columns, 32-bit offsets in a tile's rows; what is past the result is dropped
             const int64_t rows = a.M - at.m0 < C::BM ? a.M - at.m0 : C::BM;
             const int N = static_cast<int>(a.N), n_lane = at.n0 + n_wave + eh * 8, o_lane = (m_wave + er) * N + n_lane;
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
             // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
-            auto store = [&](bool streamed, const __amdgpu_buffer_rsrc_t& o, u32x4 first, u32x4 second, int i, int n, int size) __attribute__((always_inline)) {
-                const bool in = n_lane + n < N;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const u32_pair t = __builtin_amdgcn_permlane16_swap(first[e], second[e], false, false);
-                    first[e] = t.x;
-                    second[e] = t.y;
-                }
-                const int off = (o_lane + i * 32 * N + n) * size;
-                const int first_at = in ? off : 0x7FFFFFFF, second_at = in ? off + 16 * N * size : 0x7FFFFFFF;
-                if (streamed) {        // (how a store meets the caches is in its instruction; the lines keep the two from being joined)
-                    __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 2);
-                    __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 2);
-                    asm volatile("; past the caches");
-                } else {
-                    __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 0);
-                    asm volatile("; into the caches");
-                }
+            auto into = [&](const __amdgpu_buffer_rsrc_t& o, int size, bool streamed) __attribute__((always_inline)) {
+                return [=](u32x4 first, u32x4 second, int i, int n) __attribute__((always_inline)) {
+                    const bool in = n_lane + n < N;
+                    const int off = (o_lane + i * 32 * N + n) * size;
+                    const int first_at = in ? off : 0x7FFFFFFF, second_at = in ? off + 16 * N * size : 0x7FFFFFFF;
+                    if (streamed) {    // (how a store meets the caches is in its instruction; the lines keep the two from being joined)
+                        __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 2);
+                        __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 2);
+                        asm volatile("; past the caches");
+                    } else {
+                        __builtin_amdgcn_raw_buffer_store_b128(first, o, first_at, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(second, o, second_at, 0, 0);
+                        asm volatile("; into the caches");
+                    }
+                };
             };
-            if (out) {
-                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000);
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        const v16f v = acc[i][j];
-                        store(a.streamed, o, u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])},
-                              u32x4{pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15])}, i, j * 32 + es * 16, 2);
-                    }
-            }
-            if (y) {
-                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(y + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 4), 0x00020000);
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                    for (int j = 0; j < 2 * TN; ++j) {
-                        const v16f v = acc[i][j >> 1];
-                        auto word = [&](int e) __attribute__((always_inline)) { return __float_as_uint(v[(j & 1) * 8 + e]); };
-                        store(false, o, u32x4{word(0), word(1), word(2), word(3)}, u32x4{word(4), word(5), word(6), word(7)}, i, j * 16 + es * 4, 4);
-                    }
-            }
+            if (out) bf16_runs(into(__builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000), 2, a.streamed));
+            if (y) fp32_runs(into(__builtin_amdgcn_make_buffer_rsrc(y + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 4), 0x00020000), 4, false));
             late = out && !y ? C::R - 1 : 0;
-        } else {
+        } else {                       // rows that start anywhere (by elements, rows x columns x K: 16384 x 4098 x 1024 238 us, here 65; 16384 x 4097 x 1024 250
+                                       // and 107, inside words; whole runs in buffers 4096 columns 57)
             late = 0;
-            const int64_t n_lane = at.n0 + n_wave + eh * 8;
+            const int64_t n_lane = at.n0 + n_wave + eh * 8, m_lane = at.m0 + m_wave + er;
+            const int cols = a.N - n_lane > 256 ? 256 : static_cast<int>(a.N - n_lane), rows = a.M - m_lane > 256 ? 256 : static_cast<int>(a.M - m_lane);
+            auto into = [&](auto* base) __attribute__((always_inline)) {
+                using T = std::remove_pointer_t<decltype(base)>;
+                constexpr int PER = 16 / sizeof(T);
+                return [=](u32x4 first, u32x4 second, int i, int n) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                const int64_t m = at.m0 + m_wave + i * 32 + es * 16 + er;
+                    for (int k = 0; k < 2; ++k) {
+                        const u32x4 v = k ? second : first;
+                        T* const p = base + (m_lane + i * 32 + k * 16) * a.N + n_lane + n;
+                        if (i * 32 + k * 16 >= rows) continue;
+                        if (n + PER <= cols) *reinterpret_cast<u32x4_any*>(p) = v;
+                        else
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int64_t n = n_lane + j * 32 + (e >> 3) * 16 + (e & 7), o = m * a.N + n;
-                        if (m < a.M && n < a.N) {
-                            if (out) out[o] = static_cast<uint16_t>(f32_to_bf16_rne(acc[i][j][e]));
-                            if (y) y[o] = acc[i][j][e];
-                        }
+                            for (int e = 0; e < PER; ++e)
+                                if (n + e < cols) {
+                                    if constexpr (sizeof(T) == 2) p[e] = static_cast<uint16_t>(v[e >> 1] >> ((e & 1) * 16));
+                                    else p[e] = __uint_as_float(v[e]);
+                                }
                     }
-            }
+                };
+            };
+            if (out) bf16_runs(into(out));
+            if (y) fp32_runs(into(y));
         }
         if (tile + static_cast<int>(gridDim.x) < total) at = locate(tile + gridDim.x);
     }

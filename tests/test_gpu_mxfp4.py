@@ -240,9 +240,10 @@ def test_training_step(M, K, N):
         _check(y, *a, *b, ml, out)
 
 
-def test_values_that_pass_the_caches_by():
+@pytest.mark.parametrize("K", [4104, 4103])
+def test_values_that_pass_the_caches_by(K):
     # inputs and results of 2^27 elements and more: codes against those of the halves, small whole numbers against exact products
-    M, K = 32768 + 131, 4104
+    M = 32768 + 131
     x = _wide(1, M * K, seed=3).view(M, K)
     q, s = B.loka_mxfp4_quantize(x)
     qt, st = B.loka_mxfp4_quantize(x, True)
@@ -254,7 +255,7 @@ def test_values_that_pass_the_caches_by():
         _same(qt[:, a // 2: a // 2 + hq.shape[1]], hq)
         _same(st[:, a // 32: a // 32 + hs.shape[1]], hs)
     del x, q, s, qt, st
-    K, N = 160, 4104
+    K, N = 160, K
     codes = torch.tensor([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6], device=DEV)
     x, w = (codes[torch.randint(0, 15, s, device=DEV, generator=_gen(s[0]))].bfloat16() for s in ((M, K), (N, K)))
     x[:, ::32], w[:, ::32] = 6, 6      # (every group's scale is 1)
@@ -268,6 +269,27 @@ def test_values_that_pass_the_caches_by():
     out, y = B.loka_mxfp4_gemm(d, *a, *b, want_y=True)
     _same(out, want)
     _same(y.bfloat16(), want)
+
+
+@pytest.mark.parametrize("N", [1, 7, 13, 250, 257, 1001, 4098])
+@pytest.mark.parametrize("M", [17, 300, 1025])
+@pytest.mark.parametrize("batch", [1, 3])
+def test_results_whose_rows_start_anywhere(batch, M, N):
+    # small whole numbers: exact sums; results side by side, so that a value written past its row or problem shows
+    K = 100
+    codes = torch.tensor([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6], device=DEV)
+    x, w = (codes[torch.randint(0, 15, s, device=DEV, generator=_gen(s[1]))].bfloat16() for s in ((batch * M, K), (batch * N, K)))
+    x[:, ::32], w[:, ::32] = 6, 6
+    d = B.make_mxfp4_desc(M, N, K, batch)
+    d.strideO = M * N + 5              # (the values between the problems stay)
+    span = (batch - 1) * d.strideO + M * N
+    out, y = torch.full((span,), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((span,), 7.0, device=DEV)
+    B.loka_mxfp4_gemm(d, *B.loka_mxfp4_quantize(x), *B.loka_mxfp4_quantize(w), out=out, y=y)
+    want = torch.full((span,), 7.0, device=DEV)
+    for b in range(batch):
+        want[b * d.strideO: b * d.strideO + M * N] = (x[b * M: (b + 1) * M].float() @ w[b * N: (b + 1) * N].float().t()).flatten()
+    _same(y, want)
+    _same(out, want.bfloat16())
 
 
 def test_rows_past_4_gb():
