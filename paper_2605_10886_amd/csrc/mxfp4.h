@@ -74,13 +74,25 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef uint32_t u32_any __attribute__((aligned(2)));
 
-// Eight consecutive elements of a row from column c on, zeros from `cols` on; STREAMED past the caches.
+// The eight elements from `s` on of v and zeros behind it (s >= 0), without a branch
+__device__ __forceinline__ u32x4 mx_from(u32x4 v, int64_t s) {
+    const bool four = s & 4, two = s & 2, one = s & 1, none = s >= 8;
+    v = four ? u32x4{v.z, v.w, 0u, 0u} : v;
+    v = two ? u32x4{v.y, v.z, v.w, 0u} : v;
+    v = one ? u32x4{__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16), __builtin_amdgcn_alignbit(v.w, v.z, 16), v.w >> 16} : v;
+    return none ? u32x4{0u, 0u, 0u, 0u} : v;
+}
+
+// Eight consecutive elements of a row from column c on, zeros from `cols` on; STREAMED past the caches.  A run that the row's end
+// cuts comes from the row's last eight.
 template <bool STREAMED = false>
 __device__ __forceinline__ u32x4 mx_load8(const uint16_t* row, int64_t c, int64_t cols) {
     if (c + 8 <= cols) {
         if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + c));
         return *reinterpret_cast<const u32x4_any*>(row + c);
     }
+    if (c >= cols) return u32x4{0u, 0u, 0u, 0u};
+    if (cols >= 8) return mx_from(*reinterpret_cast<const u32x4_any*>(row + cols - 8), c + 8 - cols);
     uint32_t e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : 0u;

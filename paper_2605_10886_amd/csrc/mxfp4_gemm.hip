@@ -73,13 +73,13 @@ __device__ __forceinline__ MxPiece mx_read_piece(const uint8_t* q, const uint8_t
     p.s = in ? s : 0x7F7F7F7Fu;
     return p;
 }
-// The same from bf16 rows, two ways.  Few rows (ROWS, 2 or 16): the wave quantizes 512 elements of a row at a time, 8 a lane as
+// The same from bf16 rows, two ways.  One or two rows: the wave quantizes 512 elements of a row at a time, 8 a lane as
 // they lie in memory, and turns the codes in its part of LDS (a lane that read its own row's groups would make every
 // 16-byte load a cache line of its own).
 constexpr int kTurn = 256 + 16;        // bytes of a row there: codes, scales
-template <int ROWS>
 __device__ __forceinline__ MxPiece mx_quantize_rows(const uint16_t* x, int64_t ldx, int rows, int64_t first, int64_t K, bool whole, uint8_t* turn,
                                                     int lane) {
+    constexpr int ROWS = 2;
     u32x4 v[ROWS];
     const int64_t c = first + lane * 8;
 #pragma unroll
@@ -117,6 +117,26 @@ __device__ __forceinline__ void mx_request_rows(const uint16_t* x, int64_t ldx, 
         __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(raw + i * 1024), 16, static_cast<int>(first) * 2 + (lane ^ i) * 16, 0, 0, 0);
     }
 }
+// ... rows that start or end anywhere through registers (16 x 14000 x 3001, rows x columns x K, 9.5 us; quantized by rows, 4 lanes a group, 24.4)
+__device__ __forceinline__ void mx_load_rows(const uint16_t* x, int64_t ldx, int rows, int64_t first, int64_t K, int lane, u32x4 (&v)[16]) {
+    const int64_t c = first + lane * 8;
+    if (K >= 8) {
+        const int64_t at = c + 8 <= K ? c : K - 8;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const u32x4_any*>(x + (i < rows ? i : 0) * ldx + at);
+    } else {
+        for (int i = 0; i < 16; ++i) v[i] = mx_load8(x + (i < rows ? i : 0) * ldx, c, K);
+    }
+}
+__device__ __forceinline__ void mx_put_rows(u32x4 (&v)[16], int64_t first, int64_t K, uint8_t* raw, int lane) {
+    const int64_t c = first + lane * 8;
+    if (K >= 8 && first + 512 > K) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = mx_from(v[i], c + 8 <= K ? 0 : c + 8 - K);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) *reinterpret_cast<u32x4*>(raw + i * 1024 + (lane ^ i) * 16) = v[i];
+}
 __device__ __forceinline__ MxPiece mx_quantize_groups(const uint8_t* raw, int lane) {
     const int r = lane & 15, g = lane >> 4;
     MxPiece p;
@@ -152,12 +172,12 @@ __device__ __forceinline__ void in_order() {
 // 16 x 8192 x 28672 35 us).  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
 // take 512-element pieces of the contraction in turn, straight from memory into registers, and add their partial sums in LDS
 // in wave order.
-// QUANT 0: stored X.  1, 2, 16: bf16 X of up to 16 rows (MT = 1): by groups, by rows (up to 2, 16).
+// QUANT 0: stored X.  1, 2, 3: bf16 X of up to 16 rows (MT = 1): by groups; by rows (up to 2); by groups, rows that start or end anywhere.
 template <int MT, int NT, int NW, int QUANT>
 __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];       // partial sums [NW][MT * NT][64]; before them, the waves' rows of x
     v4f* const part = reinterpret_cast<v4f*>(smem);
-    uint8_t* const own = smem + (threadIdx.x >> 6) * (QUANT == 1 ? kRaw : 16 * kTurn);
+    uint8_t* const own = smem + (threadIdx.x >> 6) * (QUANT == 2 ? 16 * kTurn : kRaw);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
     int64_t id = blockIdx.x;
     const int64_t nt = id % a.n_tiles;
@@ -186,6 +206,11 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
             mx_request_rows(a.x, a.ldx, static_cast<int>(a.M), p << 9, a.K, own, lane);
             in_order();
         }
+        u32x4 v[QUANT == 3 ? 16 : 1];
+        if constexpr (QUANT == 3) {
+            mx_load_rows(a.x, a.ldx, static_cast<int>(a.M), p << 9, a.K, lane, v);
+            in_order();
+        }
 #pragma unroll
         for (int j = 0; j < NT; ++j) w[j] = mx_read_piece(wq, sw, wrow[j], a.Kp, group);
         if constexpr (QUANT == 0) {
@@ -196,8 +221,11 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
             wait_vmcnt<5 * NT>();      // the rows, which were requested before the weights' five loads a tile
             in_order();
             x[0] = mx_quantize_groups(own, lane);
+        } else if constexpr (QUANT == 3) {
+            mx_put_rows(v, p << 9, a.K, own, lane);
+            x[0] = mx_quantize_groups(own, lane);
         } else {
-            x[0] = mx_quantize_rows<QUANT>(a.x, a.ldx, static_cast<int>(a.M), p << 9, a.K, a.x_whole, own, lane);
+            x[0] = mx_quantize_rows(a.x, a.ldx, static_cast<int>(a.M), p << 9, a.K, a.x_whole, own, lane);
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -612,7 +640,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* __restrict__ 
 
 template <int MT, int NT, int QUANT>
 static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
-    constexpr int NW = 8, SUMS = NW * MT * NT * 1024, OWN = QUANT == 0 ? 0 : NW * (QUANT == 1 ? kRaw : 16 * kTurn), LDS = SUMS > OWN ? SUMS : OWN;
+    constexpr int NW = 8, SUMS = NW * MT * NT * 1024, OWN = QUANT == 0 ? 0 : NW * (QUANT == 2 ? 16 * kTurn : kRaw), LDS = SUMS > OWN ? SUMS : OWN;
     a.n_tiles = (a.N + 16 * NT - 1) / (16 * NT);
     a.m_tiles = (a.M + 16 * MT - 1) / (16 * MT);
     if (a.m_tiles > kMaxThreads || a.n_tiles * a.m_tiles >= kMaxThreads / (64 * NW) / batch) return LOKA_ERR_SHAPE;
@@ -622,14 +650,25 @@ static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
     return LOKA_OK;
 }
 
-// Columns of a workgroup: as many as leave a workgroup for every CU, since each reads (and, fused, quantizes) all of x.
+// Columns of a workgroup.  Quantizing groups of x takes all of a CU's LDS, and x anew in every workgroup: as few columns as need no
+// second round (16 rows, us by 16 / 32 / 64 columns: 4112 columns x K 4096 8.6 / 6.6 / 8.6, 4096 5.5 / 6.5 / 8.4, 12000 13.9 / 11.7 / 9.0).
+// Elsewhere several workgroups share a CU, and more columns in one pay only where there are many and K is not long (two
+// rows quantized by rows: 12000 x 4096 7.6 / 8.6 / 8.4, 16384 x 4096 10.1 / 8.9 / 9.0, 8192 x 16384 16.1 / 21.5 / 23.8, rows that start anywhere,
+// which take longer, 14000 x 3001 8.8 / 7.3; 16 stored ones 32768 x 1024 7.4 / 6.6 / 6.0, 8192 x 16384 20 / 41 / 28).
 template <int MT, int QUANT>
 static loka_status stream_columns(const MxArgs& a, int64_t batch, hipStream_t stream) {
     const int64_t runs = (a.N + 15) / 16 * batch;          // of 16 columns
-    if constexpr (MT == 1) {
-        if (runs >= 1024) return stream_launch<MT, 4, QUANT>(a, batch, stream);
+    if constexpr (QUANT == 1 || QUANT == 3) {
+        if (runs <= 256) return stream_launch<MT, 1, QUANT>(a, batch, stream);
+        if (runs <= 512) return stream_launch<MT, 2, QUANT>(a, batch, stream);
+        return stream_launch<MT, 4, QUANT>(a, batch, stream);
+    } else if constexpr (QUANT == 2) {
+        if (runs >= (a.x_whole ? 1024 : 512) && a.Kp <= 8192) return stream_launch<MT, 2, QUANT>(a, batch, stream);
+    } else if constexpr (MT == 1) {
+        if (runs >= 1024 && a.Kp <= 2048) return stream_launch<MT, 4, QUANT>(a, batch, stream);
+    } else {
+        if (runs >= 512) return stream_launch<MT, 2, QUANT>(a, batch, stream);
     }
-    if (runs >= 512) return stream_launch<MT, 2, QUANT>(a, batch, stream);
     return stream_launch<MT, 1, QUANT>(a, batch, stream);
 }
 
@@ -649,28 +688,27 @@ static MxArgs args_of(const loka_gemm_desc* d, const uint8_t* wq, const uint8_t*
     return a;
 }
 
-// What runs a product: up to 16 rows the stream kernel, else the form expected to be fastest, and in how many ranges of K
-// tiles.  The estimates are microseconds fitted to measured launches (rows x columns x K, measured / estimated): a result tile
+// What runs a product: the form expected to be fastest, and in how many ranges of K tiles.  The estimates are microseconds fitted to measured launches (rows x columns x K, measured / estimated): a result tile
 // costs its form a fixed part and a part per K tile, times the rounds in which the chip takes them; the stream kernel costs by
 // 512-element pieces of 16 columns, times the row tiles.
 //   256 x 256            8192 x 8192 x 8192 295 / 294, 4096 x 4096 x 4096 43.5 / 43, 16384 x 4096 x 1024 60 / 60
 //   128 x 128, K halves  8192 x 8192 x 8192 417 / 415, 4096 x 4096 x 4096 59 / 59, 1024 x 4096 x 16384 53.5 / 53, 2048^3 11.8 / 11.9
 //   128 x 128, 4 waves   16384 x 4096 x 1024 68 / 67, 4096 x 4096 x 4096 53 / 55, 2048^3 11.5 / 11.5, 5013 x 720 x 1008 8.0 / 8.0, 2048 x 768 x 256 6.0 / 5.4
-//   stream               32 x 4096 x 4096 5.8 / 6.0, 32 x 16384 x 4096 13.1 / 13.3, 64 x 4096 x 4096 8.3 / 8.0, 128 x 4096 x 4096 14.2 / 12.5,
+//   stream               16 x 4096 x 4096 4.6 / 5.5, 16 x 8192 x 16384 20 / 20, 32 x 4096 x 4096 5.8 / 6.0, 32 x 16384 x 4096 13.1 / 13.3, 64 x 4096 x 4096 8.3 / 8.0, 128 x 4096 x 4096 14.2 / 12.5,
 //                        256 x 4096 x 4096 25 / 22, 256 x 768 x 2048 5.5 / 5.2
 enum { MX_STREAM = 0, MX_LARGE = 1, MX_HALVES = 2, MX_SMALL = 3 };
 struct MxPlan { int kind, tiles_m, tiles_n, splits, k_per_split; int64_t total; };
 static MxPlan plan_of(const loka_gemm_desc* d) {
     MxPlan p{MX_STREAM, 0, 0, 1, 0, 0};
     const int64_t Kp = mx_padded(d->K), k = (Kp + 255) / 256;
-    if (d->M <= 16 || Kp >= (INT64_C(1) << 23)) return p;              // (a tile's rows within 32-bit offsets)
+    if (Kp >= (INT64_C(1) << 23)) return p;                            // (a tile's rows within 32-bit offsets)
     auto tiles = [&](int64_t b) { return static_cast<double>((d->M + b - 1) / b) * static_cast<double>((d->N + b - 1) / b) * static_cast<double>(d->batch); };
     auto rounds = [](double t, double slots) { return std::ceil(t / slots); };
     const double t256 = tiles(256), t128 = tiles(128), bytes = static_cast<double>(d->M) * static_cast<double>(d->N) * static_cast<double>(d->batch) * 8.0;
     if (t128 > 1e9) return p;
-    const double rows = d->M <= 32 ? 32.0 : 64.0;
+    const double rows = d->M <= 16 ? 16.0 : d->M <= 32 ? 32.0 : 64.0, piece = d->M <= 16 ? 0.0010 : d->M <= 32 ? 0.0012 : 0.0022;
     double best = 3.5 + std::ceil(static_cast<double>(d->M) / rows) * std::ceil(static_cast<double>(d->N) / 16.0) * static_cast<double>(d->batch) *
-                            static_cast<double>((Kp + 511) / 512) * (rows == 32.0 ? 0.0012 : 0.0022);
+                            static_cast<double>((Kp + 511) / 512) * piece;
     auto take = [&](double us, int kind, int splits) {
         if (us >= best) return;
         best = us;
@@ -763,7 +801,7 @@ loka_status mxfp4_linear_fused_launch(const loka_gemm_desc* d, const void* x_bf1
     // (by rows / by groups, us: 1 x 4096 x 4096 4.0 / 4.5, 2 rows 4.2 / 4.5, 3 rows 4.5 / 4.5, 4 rows 4.8 / 4.4, 1 x 4096 x 16384 9.2 / 10.7)
     if (a.M <= 2) return stream_columns<1, 2>(a, 1, stream);
     if (a.x_whole && a.K < (INT64_C(1) << 30)) return stream_columns<1, 1>(a, 1, stream);
-    return stream_launch<1, 1, 16>(a, 1, stream);
+    return stream_columns<1, 3>(a, 1, stream);
 }
 
 }  // namespace loka

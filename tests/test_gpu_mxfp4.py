@@ -213,6 +213,18 @@ def test_layer_on_rows_of_a_larger_matrix(M, K, ld, offset):
     _check(y, *P.mx_quantize(x.contiguous()), wq, sw, K, out)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3, 11, 16])
+@pytest.mark.parametrize("K,N", [(5, 4100), (7, 33), (8, 4100), (9, 20), (515, 4100), (513, 8200), (1031, 16400), (1024, 4112), (1024, 8208), (2056, 16400)])
+def test_layer_on_few_rows_of_many_columns(M, K, N):
+    x = _wide(1, M * K, seed=K).view(M, K)
+    _, wq, sw = _operand(N, K, 8, K ** -0.5)
+    out, y = B.loka_mxfp4_linear(B.make_mxfp4_desc(M, N, K), x, wq, sw, want_y=True)
+    stored = P.mx_quantize(x)
+    _check(y, *stored, wq, sw, K, out)
+    out, y = B.loka_mxfp4_gemm(B.make_mxfp4_desc(M, N, K), *stored, wq, sw, want_y=True)
+    _check(y, *stored, wq, sw, K, out)
+
+
 def test_two_streams_at_once():
     shapes = [(16, 2048, 4096), (300, 1024, 2048), (64, 512, 512), (2000, 512, 1024)]
     work = [(B.make_mxfp4_desc(M, N, K), torch.randn(M, K, device=DEV, generator=_gen(M)).bfloat16(), *_operand(N, K, N)[1:]) for M, N, K in shapes]
