@@ -284,8 +284,9 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 // (The barrier costs some 800 cycles of a K tile's 3800: K tiles of 128 elements, with four in the ring, took 8192 x 8192 x
 // 8192 from 300 to 388 us.)  Workgroups are persistent, and the ring does not stop between result tiles: the next tile's first
 // K tiles arrive while this one's values are stored, and nothing waits for the stores where their number is known (see `late`).
-template <int TM_, int TN_, int WM_, int WN_, int WK_, int R_>
+template <int TM_, int TN_, int WM_, int WN_, int WK_, int R_, bool WORDS_ = false>
 struct MxTile {
+    static constexpr bool WORDS = WORDS_;                           // bf16 rows that start inside a word leave in whole words (below)
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, WK = WK_, R = R_, NW = WM * WN * WK, BM = WM * TM * 32, BN = WN * TN * 32;
     static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 8, STAGE = OFF_SW + BN * 8;
     static constexpr int XCH = WM * WN * 64 * 64;                   // WK = 2: one 32 x 32 tile of every wave
@@ -548,7 +549,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
                     u32x4 first{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
                     u32x4 second{pack_bf16x2(v[8], v[9]), pack_bf16x2(v[10], v[11]), pack_bf16x2(v[12], v[13]), pack_bf16x2(v[14], v[15])};
                     turn(first, second);
-                    store(first, second, i, j * 32 + es * 16);
+                    store(first, second, i, j * 32 + es * 16, j);
                 }
         };
         auto fp32_runs = [&](auto store) __attribute__((always_inline)) {
@@ -560,7 +561,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
                     auto word = [&](int e) __attribute__((always_inline)) { return __float_as_uint(v[(j & 1) * 8 + e]); };
                     u32x4 first{word(0), word(1), word(2), word(3)}, second{word(4), word(5), word(6), word(7)};
                     turn(first, second);
-                    store(first, second, i, j * 16 + es * 4);
+                    store(first, second, i, j * 16 + es * 4, j);
                 }
         };
         if (a.wide) {                  // whole runs of 8 columns, 32-bit offsets in a tile's rows; what is past the result is dropped
@@ -569,7 +570,7 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
             // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
             auto into = [&](const __amdgpu_buffer_rsrc_t& o, int size, bool streamed) __attribute__((always_inline)) {
-                return [=](u32x4 first, u32x4 second, int i, int n) __attribute__((always_inline)) {
+                return [=](u32x4 first, u32x4 second, int i, int n, int) __attribute__((always_inline)) {
                     const bool in = n_lane + n < N;
                     const int off = (o_lane + i * 32 * N + n) * size;
                     const int first_at = in ? off : 0x7FFFFFFF, second_at = in ? off + 16 * N * size : 0x7FFFFFFF;
@@ -587,33 +588,58 @@ __device__ __forceinline__ void mx_tiles(const MxArgs& a, uint8_t* smem) {
             if (out) bf16_runs(into(__builtin_amdgcn_make_buffer_rsrc(out + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 2), 0x00020000), 2, a.streamed));
             if (y) fp32_runs(into(__builtin_amdgcn_make_buffer_rsrc(y + at.m0 * a.N, 0, static_cast<int>(rows * a.N * 4), 0x00020000), 4, false));
             late = out && !y ? C::R - 1 : 0;
-        } else {                       // rows that start anywhere (by elements, rows x columns x K: 16384 x 4098 x 1024 238 us, here 65; 16384 x 4097 x 1024 250
-                                       // and 107, inside words; whole runs in buffers 4096 columns 57)
+        } else {                       // rows that start anywhere (by elements, rows x columns x K: 16384 x 4098 x 1024 238 us, here 65; 4096 columns 57.  Past the
+                                       // caches they lose: 65536 x 4098 x 512 264 -> 500)
             late = 0;
             const int64_t n_lane = at.n0 + n_wave + eh * 8, m_lane = at.m0 + m_wave + er;
             const int cols = a.N - n_lane > 256 ? 256 : static_cast<int>(a.N - n_lane), rows = a.M - m_lane > 256 ? 256 : static_cast<int>(a.M - m_lane);
-            auto into = [&](auto* base) __attribute__((always_inline)) {
+            // elements first .. of v, a run of the row whose first column is n + n_lane, as far as the row goes
+            auto put = [=](auto* base, u32x4 v, int row, int n, int first) __attribute__((always_inline)) {
                 using T = std::remove_pointer_t<decltype(base)>;
                 constexpr int PER = 16 / sizeof(T);
-                return [=](u32x4 first, u32x4 second, int i, int n) __attribute__((always_inline)) {
+                T* const p = base + (m_lane + row) * a.N + n_lane + n;
+                if (row >= rows) return;
+                if (first == 0 && n + PER <= cols) *reinterpret_cast<u32x4_any*>(p) = v;
+                else
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (e >= first && n + e < cols) {
+                            if constexpr (sizeof(T) == 2) p[e] = static_cast<uint16_t>(v[e >> 1] >> ((e & 1) * 16));
+                            else p[e] = __uint_as_float(v[e]);
+                        }
+            };
+            const bool inside = C::WORDS && ((a.N | static_cast<int64_t>(reinterpret_cast<uintptr_t>(out) >> 1)) & 1);
+            if (out && inside) {
+                // Rows that start inside a word (all of a lane's rows, or none: they lie 16 apart) are stored one column to the left, in whole words: a
+                // run's last element goes with the next run, the lane before it in the order (es, eh), or its own
+                // value of the tile before.  (Inside words 16384 x 4097 x 1024 took 107 us, here 76.)
+                const bool odd = (reinterpret_cast<uintptr_t>(out + m_lane * a.N) >> 1) & 1, first_run = es == 0 && eh == 0, last_run = es == 1 && eh == 1;
+                const int from = (er + (eh ? es * 16 : 32 + (es ^ 1) * 16)) * 4;         // that lane
+                uint32_t before[2] = {0u, 0u};
+                bf16_runs([&](u32x4 first, u32x4 second, int i, int n, int j) __attribute__((always_inline)) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const u32x4 v = k ? second : first;
-                        T* const p = base + (m_lane + i * 32 + k * 16) * a.N + n_lane + n;
-                        if (i * 32 + k * 16 >= rows) continue;
-                        if (n + PER <= cols) *reinterpret_cast<u32x4_any*>(p) = v;
-                        else
-#pragma unroll
-                            for (int e = 0; e < PER; ++e)
-                                if (n + e < cols) {
-                                    if constexpr (sizeof(T) == 2) p[e] = static_cast<uint16_t>(v[e >> 1] >> ((e & 1) * 16));
-                                    else p[e] = __uint_as_float(v[e]);
-                                }
+                        const uint32_t last = v[3], left = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(last_run ? before[k] : last)));
+                        before[k] = last;
+                        const u32x4 w{__builtin_amdgcn_alignbit(v[0], left, 16), __builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16),
+                                      __builtin_amdgcn_alignbit(v[3], v[2], 16)};
+                        const int row = i * 32 + k * 16;
+                        put(out, odd ? w : v, row, odd ? n - 1 : n, odd && first_run && j == 0 ? 1 : 0);
+                        if (odd && last_run && j == TN - 1 && row < rows && n + 7 < cols) out[(m_lane + row) * a.N + n_lane + n + 7] = static_cast<uint16_t>(last >> 16);
                     }
-                };
-            };
-            if (out) bf16_runs(into(out));
-            if (y) fp32_runs(into(y));
+                });
+            } else if (out) {
+                bf16_runs([&](u32x4 first, u32x4 second, int i, int n, int) __attribute__((always_inline)) {
+                    put(out, first, i * 32, n, 0);
+                    put(out, second, i * 32 + 16, n, 0);
+                });
+            }
+            if (y)
+                fp32_runs([&](u32x4 first, u32x4 second, int i, int n, int) __attribute__((always_inline)) {
+                    put(y, first, i * 32, n, 0);
+                    put(y, second, i * 32 + 16, n, 0);
+                });
         }
         if (tile + static_cast<int>(gridDim.x) < total) at = locate(tile + gridDim.x);
     }
@@ -775,10 +801,15 @@ loka_status mxfp4_gemm_launch(const loka_gemm_desc* d, const uint8_t* xq, const 
     // (24576 x 4096 x 4096 240 -> 230, 49152 x 2048 x 2048 114 -> 119, 4096 x 4096 x 4096 42.9 -> 43.8), and the next kernel may read them there.
     a.streamed = a.M * a.N * d->batch >= INT64_C(1) << 27;
     a.wide = a.N % 8 == 0 && a.N < (INT64_C(1) << 21) && (d->batch == 1 || d->strideO % 8 == 0);
-    using Large = MxTile<2, 4, 4, 2, 1, 2>;
+    using Large = MxTile<2, 4, 4, 2, 1, 2, true>;
     using Halves = MxTile<2, 2, 2, 2, 2, 3>;
     using Small = MxTile<2, 2, 2, 2, 1, 2>;
+    using SmallWords = MxTile<2, 2, 2, 2, 1, 2, true>;
     if (p.kind == MX_LARGE) return tile_launch<Large, false>(a, stream);
+    // (stores bound several rounds of small tiles: 65536 x 1025 x 256 71 -> 52 us by words; one round loses, 5013 x 721 x 1008 8.3 -> 8.5, and the longer
+    // kernel by itself costs 5013 x 720 x 1008 3 %)
+    const bool odd = a.out && ((a.N & 1) || (d->batch > 1 && (d->strideO & 1)));
+    if (p.kind == MX_SMALL && odd && a.total > 256 * Small::PER_CU) return tile_launch<SmallWords, false>(a, stream);
     if (p.kind == MX_SMALL) return tile_launch<Small, false>(a, stream);
     if (p.splits == 1) return tile_launch<Halves, false>(a, stream);
     const loka_status st = tile_launch<Halves, true>(a, stream);

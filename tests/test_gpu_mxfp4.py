@@ -283,12 +283,10 @@ def test_values_that_pass_the_caches_by(K):
     _same(y.bfloat16(), want)
 
 
-@pytest.mark.parametrize("N", [1, 7, 13, 250, 257, 1001, 4098])
-@pytest.mark.parametrize("M", [17, 300, 1025])
-@pytest.mark.parametrize("batch", [1, 3])
-def test_results_whose_rows_start_anywhere(batch, M, N):
+@pytest.mark.parametrize("batch,M,N,K", [(b, M, N, 100) for b in (1, 3) for M in (17, 300, 1025) for N in (1, 7, 13, 250, 257, 1001, 4098)] +
+                         [(1, 20000, 515, 100), (9, 3000, 258, 70), (1, 4096, 4095, 512), (1, 4200, 4098, 512), (3, 2111, 4033, 300), (2, 70001, 129, 100)])
+def test_results_whose_rows_start_anywhere(batch, M, N, K):
     # small whole numbers: exact sums; results side by side, so that a value written past its row or problem shows
-    K = 100
     codes = torch.tensor([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6], device=DEV)
     x, w = (codes[torch.randint(0, 15, s, device=DEV, generator=_gen(s[1]))].bfloat16() for s in ((batch * M, K), (batch * N, K)))
     x[:, ::32], w[:, ::32] = 6, 6
