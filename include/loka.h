@@ -320,7 +320,7 @@ loka_status loka_fp8_linear_norm_xq(const loka_gemm_desc* desc, const void* x_bf
  *   transpose_out != 0: the operand is the transpose, [cols, rows], whose groups run along the ROWS of x: codes
  *   [cols, rowsp / 2], scales [cols, rowsp / 32], rowsp = rows up to a multiple of 128.  What weights [K, N] take for the
  *   forward product, and X and dY for dW = X^T dY.
- * Any rows >= 1 and cols >= 1 (each at most 2^31 - 1; the stored form may exceed 4 GB).  q 16-byte, scales 4-byte aligned. */
+ * Any rows >= 1 and cols >= 1 (each at most 2^31 - 1, 2^48 elements in all; the stored form may exceed 4 GB).  q 16-byte, scales 4-byte aligned. */
 int64_t loka_mxfp4_padded(int64_t cols);          /* cols up to a multiple of 128; -1 for cols <= 0 or where that is no int64.  Host only. */
 loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                 uint8_t* scales, void* hip_stream);
@@ -331,7 +331,8 @@ loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64
 
 /* Y[m,n] = sum_k x[m,k] w[n,k] over MXFP4 operands, fp32 accumulation on the scaled matrix instruction, for `batch`
  * problems of one shape.  Of `desc` M, N, K, batch, the strides and norm, act and variant are read; norm must be
- * LOKA_NORM_NONE, act LOKA_ACT_NONE, variant -1 (LOKA_ERR_UNSUPPORTED otherwise).  Any M, N, K >= 1.
+ * LOKA_NORM_NONE, act LOKA_ACT_NONE, variant -1 (LOKA_ERR_UNSUPPORTED otherwise).  Any M, N, K >= 1 (each
+ * and batch at most 2^31 - 1, 2^48 elements of an operand or of all results).
  *   xq, sx  [batch] stored operands [M, K]; strideX = elements between problems in the stored form, at least
  *           M * loka_mxfp4_padded(K) and a multiple of 128, or 0 = shared (the scales of
  *           problem g start at byte g * strideX / 32)

@@ -436,12 +436,16 @@ loka_status loka_tracker_update(const void* x_bf16, int64_t B, int64_t K, int64_
 // ---- MXFP4
 int64_t loka_mxfp4_padded(int64_t cols) { return cols <= 0 || cols > INT64_MAX - 127 ? -1 : (cols + 127) / 128 * 128; }
 
+// More elements than any memory holds: refused before sizes are multiplied further.
+static bool too_many(int64_t batch, int64_t rows, int64_t cols) {
+    return static_cast<double>(batch) * static_cast<double>(rows) * static_cast<double>(cols) > 281474976710656.0;      // 2^48
+}
 static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                 uint8_t* scales, void* hip_stream) {
     if (!x_bf16 || !q || !scales) return LOKA_ERR_NULL;
-    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX || too_many(1, rows, cols)) return LOKA_ERR_SHAPE;
     if (!aligned_to(x_bf16, 2) || !aligned16(q) || !aligned_to(scales, 4)) return LOKA_ERR_ALIGN;
     return mxfp4_quantize_launch(x_bf16, rows, cols, ld, transpose_out, q, scales, static_cast<hipStream_t>(hip_stream));
 }
@@ -449,7 +453,7 @@ loka_status loka_mxfp4_quantize(const void* x_bf16, int64_t rows, int64_t cols, 
 loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, void* out_bf16, int64_t ld,
                                   void* hip_stream) {
     if (!q || !scales || !out_bf16) return LOKA_ERR_NULL;
-    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (rows <= 0 || cols <= 0 || ld < cols || rows > INT32_MAX || cols > INT32_MAX || too_many(1, rows, cols)) return LOKA_ERR_SHAPE;
     if (!aligned_to(out_bf16, 2) || !aligned16(q) || !aligned_to(scales, 4)) return LOKA_ERR_ALIGN;
     return mxfp4_dequantize_launch(q, scales, rows, cols, out_bf16, ld, static_cast<hipStream_t>(hip_stream));
 }
@@ -459,6 +463,7 @@ static loka_status validate_mxfp4(const loka_gemm_desc* d, bool linear) {
     if (!d) return LOKA_ERR_NULL;
     if (d->M <= 0 || d->N <= 0 || d->K <= 0 || d->batch <= 0) return LOKA_ERR_SHAPE;
     if (d->M > INT32_MAX || d->N > INT32_MAX || d->K > INT32_MAX || d->batch > INT32_MAX) return LOKA_ERR_SHAPE;
+    if (too_many(1, d->M, d->K) || too_many(1, d->N, d->K) || too_many(d->batch, d->M, d->N)) return LOKA_ERR_SHAPE;
     if (d->norm != LOKA_NORM_NONE || d->act != LOKA_ACT_NONE || d->variant != -1) return LOKA_ERR_UNSUPPORTED;
     if (linear) return d->batch == 1 ? LOKA_OK : LOKA_ERR_UNSUPPORTED;
     if (d->batch > 1) {

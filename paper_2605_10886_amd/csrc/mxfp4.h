@@ -9,6 +9,17 @@ constexpr int kMxGroup = 32;           // elements that share a scale
 constexpr int kMxPad = 128;            // a stored row is a whole number of matrix instructions' K
 constexpr int kMxNaN = 255;            // scale byte of a group with a NaN or an infinity
 
+// A launch has fewer than 2^32 threads: workgroups 0 .. groups - 1 of `threads` threads in as many launches as that takes, each told its first
+template <class F>
+static inline loka_status in_launches(int64_t groups, int threads, F&& launch) {
+    const int64_t most = (INT64_C(1) << 32) / threads - 1;
+    for (int64_t from = 0; from < groups; from += most) {
+        launch(from, static_cast<uint32_t>(groups - from < most ? groups - from : most));
+        LOKA_HIP_TRY(hipGetLastError());
+    }
+    return LOKA_OK;
+}
+
 static inline int64_t mx_padded(int64_t cols) { return (cols + kMxPad - 1) / kMxPad * kMxPad; }
 
 // Scale byte of a group from the bits of its largest magnitude as binary32 (a bf16's bits shifted up): the exponent field is

@@ -13,10 +13,10 @@ namespace loka {
 // matrix, so that short rows fill it too; U loads of a lane are in flight together.
 template <int U, bool STREAMED>
 __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
-                                                            int64_t ld, uint32_t* __restrict__ q, uint32_t* __restrict__ scales) {
+                                                            int64_t ld, uint32_t* __restrict__ q, uint32_t* __restrict__ scales, int64_t first_wg) {
     const int t = static_cast<int>(threadIdx.x), l16 = t & 15;
     const int64_t nb = (cols + kMxPad - 1) / kMxPad, total = rows * nb;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * (16 * U) + (t >> 4);
+    const int64_t first = (first_wg + blockIdx.x) * (16 * U) + (t >> 4);
     int64_t row = first / nb, b = first - row * nb;
     const int64_t step_row = 16 / nb, step_b = 16 - step_row * nb;
     u32x4 v[U];
@@ -50,13 +50,13 @@ __global__ __launch_bounds__(256) void mx_quant_rows_kernel(const uint16_t* __re
 constexpr int kTurnRows = 256, kTurnCols = 128, kTurnPitch = kTurnRows / 2 + 16;      // (pitch: 16 bytes more, so that columns start on other banks)
 template <bool STREAMED>
 __global__ __launch_bounds__(512) void mx_quant_turned_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t cols,
-                                                              int64_t ld, uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+                                                              int64_t ld, uint8_t* __restrict__ q, uint8_t* __restrict__ scales, int64_t first_wg) {
     __shared__ __align__(16) uint8_t codes[kTurnCols * kTurnPitch];
     __shared__ __align__(8) uint8_t bytes[kTurnCols * 8];
     const int t = static_cast<int>(threadIdx.x), lane = t & 63, wave = t >> 6;
     const int64_t rowsp = (rows + kMxPad - 1) / kMxPad * kMxPad;
     const int64_t nct = (cols + kTurnCols - 1) / kTurnCols;
-    const int64_t rt = blockIdx.x / nct, ct = blockIdx.x - rt * nct;
+    const int64_t rt = (first_wg + blockIdx.x) / nct, ct = first_wg + blockIdx.x - rt * nct;
     const int64_t r0 = rt * kTurnRows + wave * kMxGroup, c = ct * kTurnCols + lane * 2;
     uint32_t w[kMxGroup];              // (element of column c, of column c + 1) of each row
 #pragma unroll
@@ -122,10 +122,10 @@ __device__ __forceinline__ u32x4 mx_values8(uint32_t codes, uint32_t byte) {
 // The values of stored codes: a lane turns one word (8 codes) into 16 bytes.
 template <int U>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint32_t* __restrict__ q, const uint8_t* __restrict__ scales, int64_t rows,
-                                                         int64_t cols, uint16_t* __restrict__ out, int64_t ld) {
+                                                         int64_t cols, uint16_t* __restrict__ out, int64_t ld, int64_t first_wg) {
     const int t = static_cast<int>(threadIdx.x), l16 = t & 15;
     const int64_t nb = (cols + kMxPad - 1) / kMxPad, total = rows * nb;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * (16 * U) + (t >> 4);
+    const int64_t first = (first_wg + blockIdx.x) * (16 * U) + (t >> 4);
     int64_t row = first / nb, b = first - row * nb;
     const int64_t step_row = 16 / nb, step_b = 16 - step_row * nb;
     uint32_t v[U], s[U];
@@ -155,8 +155,6 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint32_t* __restr
 }
 
 // ---------------------------------------------------------------------------------
-constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
-
 loka_status mxfp4_quantize_launch(const void* x_bf16, int64_t rows, int64_t cols, int64_t ld, int transpose_out, uint8_t* q,
                                   uint8_t* scales, hipStream_t stream) {
     const uint16_t* x = static_cast<const uint16_t*>(x_bf16);
@@ -164,33 +162,29 @@ loka_status mxfp4_quantize_launch(const void* x_bf16, int64_t rows, int64_t cols
     // lie there already, and loses: 16384 x 4096 27.8 -> 31.8 us when its values were read just before, and 31.3 -> 31.4 when not.
     const bool streamed = rows * cols >= INT64_C(1) << 27;
     if (transpose_out) {
-        const int64_t grid = ((rows + kTurnRows - 1) / kTurnRows) * ((cols + kTurnCols - 1) / kTurnCols);
-        if (grid >= kMaxThreads / 512) return LOKA_ERR_SHAPE;
-        if (streamed) mx_quant_turned_kernel<true><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
-        else mx_quant_turned_kernel<false><<<static_cast<uint32_t>(grid), 512, 0, stream>>>(x, rows, cols, ld, q, scales);
-    } else {
-        constexpr int U = 4;
-        const int64_t grid = (rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U);
-        if (grid >= kMaxThreads / 256) return LOKA_ERR_SHAPE;
-        uint32_t* qw = reinterpret_cast<uint32_t*>(q);
-        uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
-        if (streamed) mx_quant_rows_kernel<U, true><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
-        else mx_quant_rows_kernel<U, false><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(x, rows, cols, ld, qw, sw);
+        const int64_t groups = ((rows + kTurnRows - 1) / kTurnRows) * ((cols + kTurnCols - 1) / kTurnCols);
+        return in_launches(groups, 512, [&](int64_t from, uint32_t grid) {
+            if (streamed) mx_quant_turned_kernel<true><<<grid, 512, 0, stream>>>(x, rows, cols, ld, q, scales, from);
+            else mx_quant_turned_kernel<false><<<grid, 512, 0, stream>>>(x, rows, cols, ld, q, scales, from);
+        });
     }
-    LOKA_HIP_TRY(hipGetLastError());
-    return LOKA_OK;
+    constexpr int U = 4;
+    uint32_t* qw = reinterpret_cast<uint32_t*>(q);
+    uint32_t* sw = reinterpret_cast<uint32_t*>(scales);
+    return in_launches((rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U), 256, [&](int64_t from, uint32_t grid) {
+        if (streamed) mx_quant_rows_kernel<U, true><<<grid, 256, 0, stream>>>(x, rows, cols, ld, qw, sw, from);
+        else mx_quant_rows_kernel<U, false><<<grid, 256, 0, stream>>>(x, rows, cols, ld, qw, sw, from);
+    });
 }
 
 loka_status mxfp4_dequantize_launch(const uint8_t* q, const uint8_t* scales, int64_t rows, int64_t cols, void* out_bf16, int64_t ld,
                                     hipStream_t stream) {
     constexpr int U = 4;
-    const int64_t grid = (rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U);
-    if (grid >= kMaxThreads / 256) return LOKA_ERR_SHAPE;
     const uint32_t* qw = reinterpret_cast<const uint32_t*>(q);
     uint16_t* out = static_cast<uint16_t*>(out_bf16);
-    mx_dequant_kernel<U><<<static_cast<uint32_t>(grid), 256, 0, stream>>>(qw, scales, rows, cols, out, ld);
-    LOKA_HIP_TRY(hipGetLastError());
-    return LOKA_OK;
+    return in_launches((rows * (mx_padded(cols) / kMxPad) + 16 * U - 1) / (16 * U), 256, [&](int64_t from, uint32_t grid) {
+        mx_dequant_kernel<U><<<grid, 256, 0, stream>>>(qw, scales, rows, cols, out, ld, from);
+    });
 }
 
 }  // namespace loka

@@ -17,8 +17,6 @@
 
 namespace loka {
 
-constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
-
 typedef float v16f __attribute__((ext_vector_type(16)));
 
 struct MxArgs {
@@ -29,7 +27,7 @@ struct MxArgs {
     int64_t M, N, K, Kp;               // Kp: stored row length in elements
     int64_t ldx;
     int64_t strideX, strideW, strideO; // elements between problems
-    int64_t n_tiles, m_tiles;          // stream kernel
+    int64_t n_tiles, m_tiles, first_wg; // stream kernel
     bool x_whole;                      // rows of x start on multiples of 16 bytes, and are a whole number of 16-byte runs
     // tile kernel: result tiles of a problem, K ranges and their length in K tiles, all tiles
     int64_t batch;
@@ -179,7 +177,7 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
     v4f* const part = reinterpret_cast<v4f*>(smem);
     uint8_t* const own = smem + (threadIdx.x >> 6) * (QUANT == 2 ? 16 * kTurn : kRaw);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    int64_t id = blockIdx.x;
+    int64_t id = a.first_wg + blockIdx.x;
     const int64_t nt = id % a.n_tiles;
     id /= a.n_tiles;
     const int64_t mt = id % a.m_tiles, prob = id / a.m_tiles;
@@ -669,11 +667,11 @@ static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
     constexpr int NW = 8, SUMS = NW * MT * NT * 1024, OWN = QUANT == 0 ? 0 : NW * (QUANT == 2 ? 16 * kTurn : kRaw), LDS = SUMS > OWN ? SUMS : OWN;
     a.n_tiles = (a.N + 16 * NT - 1) / (16 * NT);
     a.m_tiles = (a.M + 16 * MT - 1) / (16 * MT);
-    if (a.m_tiles > kMaxThreads || a.n_tiles * a.m_tiles >= kMaxThreads / (64 * NW) / batch) return LOKA_ERR_SHAPE;
     if (LDS > 65536) LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&mx_stream_kernel<MT, NT, NW, QUANT>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
-    mx_stream_kernel<MT, NT, NW, QUANT><<<static_cast<uint32_t>(a.n_tiles * a.m_tiles * batch), 64 * NW, LDS, stream>>>(a);
-    LOKA_HIP_TRY(hipGetLastError());
-    return LOKA_OK;
+    return in_launches(a.n_tiles * a.m_tiles * batch, 64 * NW, [&](int64_t from, uint32_t grid) {
+        a.first_wg = from;
+        mx_stream_kernel<MT, NT, NW, QUANT><<<grid, 64 * NW, LDS, stream>>>(a);
+    });
 }
 
 // Columns of a workgroup.  Quantizing groups of x takes all of a CU's LDS, and x anew in every workgroup: as few columns as need no

@@ -5,7 +5,6 @@
 
 namespace loka {
 
-constexpr int64_t kMaxThreads = INT64_C(1) << 32;       // of one launch
 constexpr int kModeRow = 0, kModeBlock = 1, kModePow2 = 2, kModeNone = 3;      // of scales, as the kernels see them
 
 struct RmsArgs {
@@ -15,7 +14,7 @@ struct RmsArgs {
     float* y_scales;                   // (MXFP4: bytes)
     uint32_t* hq;
     float *hs, *rstd;
-    int64_t rows, ld_x, ld_r;
+    int64_t rows, ld_x, ld_r, first_wg;
     int cols;
     int out, out_mode, ckpt_mode;
     float eps;
@@ -75,7 +74,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
     constexpr int WG = T < 256 ? 256 : T;
     __shared__ float red[3][WG / 64];
     const int tid = static_cast<int>(threadIdx.x), t = tid % T;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * (WG / T) + tid / T;
+    const int64_t row = (a.first_wg + blockIdx.x) * (WG / T) + tid / T;
     const bool live = row < a.rows;
     const int chunks = a.cols >> 3;
     float h[CPL][8], sum = 0.f, am_y = 0.f, am_h = 0.f;
@@ -395,14 +394,13 @@ static int kernel_mode(int mode) {
 static bool streamed(int64_t rows, int64_t cols) { return rows * cols >= INT64_C(1) << 26; }
 
 template <int T, int CPL>
-static loka_status forward_launch(const RmsArgs& a, hipStream_t stream) {
+static loka_status forward_launch(RmsArgs a, hipStream_t stream) {
     constexpr int WG = T < 256 ? 256 : T;
-    const int64_t grid = (a.rows + WG / T - 1) / (WG / T);
-    if (grid >= kMaxThreads / WG) return LOKA_ERR_SHAPE;
-    if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(a);
-    else add_rmsnorm_kernel<T, CPL, false><<<static_cast<uint32_t>(grid), WG, 0, stream>>>(a);
-    LOKA_HIP_TRY(hipGetLastError());
-    return LOKA_OK;
+    return in_launches((a.rows + WG / T - 1) / (WG / T), WG, [&](int64_t from, uint32_t grid) {
+        a.first_wg = from;
+        if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true><<<grid, WG, 0, stream>>>(a);
+        else add_rmsnorm_kernel<T, CPL, false><<<grid, WG, 0, stream>>>(a);
+    });
 }
 
 loka_status add_rmsnorm_launch(const loka_rms_desc* d, const void* x, const void* residual, const void* gamma, void* h_out, void* y_out,
