@@ -335,7 +335,7 @@ loka_status loka_mxfp4_dequantize(const uint8_t* q, const uint8_t* scales, int64
  * and batch at most 2^31 - 1, 2^48 elements of an operand or of all results).
  *   xq, sx  [batch] stored operands [M, K]; strideX = elements between problems in the stored form, at least
  *           M * loka_mxfp4_padded(K) and a multiple of 128, or 0 = shared (the scales of
- *           problem g start at byte g * strideX / 32)
+ *           problem g start at byte g * strideX / 32); no stride is read where batch is 1
  *   wq, sw  likewise [N, K] with strideW
  *   out_bf16 [batch][M, N] bf16 and / or y_fp32 [batch][M, N] fp32, strideO elements apart; at least one is not NULL.
  *           16-byte aligned; rows are N elements apart, whatever N (an odd N makes bf16 results that start inside a word, and slower).

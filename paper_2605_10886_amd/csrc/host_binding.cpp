@@ -394,10 +394,12 @@ bool product_outputs(PyObject* want_out, PyObject* want_y, PyObject* out_o, PyOb
 int64_t span(int64_t batch, int64_t stride, int64_t each) { return (batch - 1) * stride + each; }
 constexpr int64_t kMost = INT64_C(1) << 31, kMostElements = INT64_C(1) << 46;      // of a size; of a whole operand
 bool sizes_ok(const loka_gemm_desc& d) {
-    return d.M > 0 && d.N > 0 && d.K > 0 && d.batch > 0 && d.M < kMost && d.N < kMost && d.K < kMost && d.batch < kMost &&
-           d.strideX >= 0 && d.strideW >= 0 && d.strideO >= 0 && d.strideX < kMostElements && d.strideW < kMostElements &&
-           d.strideO < kMostElements && d.batch * (d.strideO / 1024 + 1) < kMostElements / 1024 &&
-           d.batch * (d.strideX / 1024 + 1) < kMostElements / 1024 && d.batch * (d.strideW / 1024 + 1) < kMostElements / 1024;
+    return d.M > 0 && d.N > 0 && d.K > 0 && d.batch > 0 && d.M < kMost && d.N < kMost && d.K < kMost && d.batch < kMost;
+}
+// (read where there are several problems)
+bool strides_ok(const loka_gemm_desc& d) {
+    auto ok = [&](int64_t stride) { return stride >= 0 && stride < kMostElements && d.batch * (stride / 1024 + 1) < kMostElements / 1024; };
+    return d.batch == 1 || (ok(d.strideX) && ok(d.strideW) && ok(d.strideO));
 }
 
 // mxfp4_gemm(desc, xq, sx, wq, sw, want_out, want_y, out, y, workspace) -> (out or None, y or None)
@@ -406,7 +408,7 @@ PyObject* mxfp4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!need_args(n, 10)) return nullptr;
     const loka_gemm_desc d = desc_of(a[0]);
     const at::Tensor &xq = tensor(a[1]), &sx = tensor(a[2]), &wq = tensor(a[3]), &sw = tensor(a[4]);
-    if (!sizes_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_gemm");
+    if (!sizes_ok(d) || !strides_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_mxfp4_gemm");
     const int64_t kp = loka_mxfp4_padded(d.K);
     const int64_t nx = span(d.batch, d.strideX, d.M * kp), nw = span(d.batch, d.strideW, d.N * kp);
     if (!holds(xq, at::kByte, nx / 2) || !holds(sx, at::kByte, nx / 32) || !holds(wq, at::kByte, nw / 2) || !holds(sw, at::kByte, nw / 32))
