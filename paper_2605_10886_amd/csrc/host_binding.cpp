@@ -314,6 +314,8 @@ bool on_gpu(const at::Device& dev, std::initializer_list<const at::Tensor*> ts) 
     return true;
 }
 at::Tensor given(PyObject* o) { return o == Py_None ? at::Tensor() : tensor(o); }
+// a workspace that may be written for its nbytes() from its address on
+bool is_run(const at::Tensor& ws) { return !ws.defined() || ws.is_contiguous(); }
 template <class T>
 T* at_or_null(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.data_ptr()) : nullptr; }
 void* stream_of(const at::Device& dev) { return c10::hip::getCurrentHIPStream(dev.index()).stream(); }
@@ -415,6 +417,7 @@ PyObject* mxfp4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return refuse("xq, sx, wq, sw: stored operands [batch, M, K] and [batch, N, K], contiguous uint8");
     const at::Device dev = xq.device();
     at::Tensor ws = given(a[9]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
     if (!on_gpu(dev, {&sx, &wq, &sw, &ws})) return refuse("tensors on one GPU");
     const c10::DeviceGuard guard(dev);
     at::Tensor out, y;
@@ -442,6 +445,7 @@ PyObject* mxfp4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!is_stored(wq, sw, d.N, d.K)) return refuse("wq, sw: a stored operand [N, K], contiguous uint8");
     const at::Device dev = x.device();
     at::Tensor ws = given(a[8]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
     if (!on_gpu(dev, {&wq, &sw, &ws})) return refuse("tensors on one GPU");
     const c10::DeviceGuard guard(dev);
     at::Tensor out, y;
@@ -540,6 +544,7 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (gamma.defined() && !(holds(gamma, at::kBFloat16, d.cols) && gamma.numel() == d.cols)) return refuse("gamma: contiguous bf16 [cols]");
     const at::Device dev = dy.device();
     at::Tensor dx = given(a[8]), ws = given(a[9]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
     if (!on_gpu(dev, {&hq, &hs, &rstd, &gamma, &dh, &dx, &ws})) return refuse("tensors on one GPU");
     const c10::DeviceGuard guard(dev);
     if (!dx.defined()) dx = empty({d.rows, d.cols}, at::kBFloat16, dev);

@@ -45,3 +45,15 @@ def test_one_problem_reads_no_strides():
         with pytest.raises(B.LokaError) as e:
             B.loka_mxfp4_gemm(d, q, s, q, s)
         assert e.value.status == B.LOKA_ERR_SHAPE
+
+
+def test_a_workspace_is_one_run_of_memory():
+    # bytes of an expanded or strided tensor are not its own: writing them would run past it or between its elements
+    x, q, s = torch.zeros(64, 64, dtype=torch.bfloat16), torch.zeros(64, 64, dtype=torch.uint8), torch.zeros(64, 4, dtype=torch.uint8)
+    hq, hs, rstd = torch.zeros(64, 64, dtype=torch.uint8), torch.zeros(64), torch.zeros(64)
+    d = B.make_mxfp4_desc(64, 64, 64)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2]):
+        for call in (lambda: B.loka_mxfp4_gemm(d, q, s, q, s, workspace=ws), lambda: B.loka_mxfp4_linear(d, x, q, s, workspace=ws),
+                     lambda: B.loka_rmsnorm_backward(x, hq, hs, rstd, ckpt_mode=B.SCALE_ROW, workspace=ws)):
+            with pytest.raises(AssertionError, match="workspace"):
+                call()
