@@ -51,7 +51,7 @@ __device__ __forceinline__ void unpack8(const u32x4 w, float (&f)[8]) {
     for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
 }
 
-// Scale and factor of an e4m3 group of y = v * rstd whose largest |v| is `am` (rstd = 1: of v itself).  Away from the floor
+// Scale and factor of an e4m3 group of y = v * rstd whose largest |v| is `am` (rstd = 1, or a power of two: of v itself, in its unit).  Away from the floor
 // amax / 448 and 448 / amax: rstd cancels in the factor, so a code has one rounding fewer than v * rstd, then * 448 / amax.
 // A group with an infinite or NaN value gets a NaN scale.
 __device__ __forceinline__ void e4m3_group(bool pow2, float am, float rstd, float& scale, float& inv) {
@@ -66,10 +66,15 @@ __device__ __forceinline__ void e4m3_group(bool pow2, float am, float rstd, floa
     if (__float_as_uint(top) >= 0x7F800000u) scale = __uint_as_float(0x7FC00000u);
 }
 
+// A sum of squares from here on has fp32's precision (each of up to 32768 terms below 2^-126 is off by at most 2^-150), and beside an eps from
+// here on a smaller sum's errors do not matter.  For a smaller eps another instance of the kernel looks at every sum: its branch, and
+// what is not moved over it, cost rows that do not need it 0.1 us a launch and up to 5 % (5984 x 1280 11.9 -> 12.3 us).
+constexpr float kLeast = 0x1p-90f;
+
 // ---------------------------------------------------------------------------------
 // T threads take a row (T = 16, 32, 64: several rows a wave or one; 256, 1024: a workgroup per row), CPL chunks of 8
 // consecutive elements each, chunk j of thread t at 8 (t + j T): a group of 128 elements is 16 neighbouring lanes, one of 32 a quad.
-template <int T, int CPL, bool STREAMED>
+template <int T, int CPL, bool STREAMED, bool RANGE>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const RmsArgs a) {
     constexpr int WG = T < 256 ? 256 : T;
     __shared__ float red[3][WG / 64];
@@ -105,44 +110,67 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[j][i], h[j][i], sum);
     }
-    // the row's largest magnitudes, where a scale is per row
+    // the row's sum of squares, and its largest magnitudes where a scale is per row
     const bool row_y = a.out == LOKA_RMS_OUT_E4M3 && a.out_mode == kModeRow, row_h = a.ckpt_mode == kModeRow;
-    if (row_y) {
+    auto over_row = [&]() __attribute__((always_inline)) {
+        if (row_y) {
+            am_y = 0.f;
 #pragma unroll
-        for (int j = 0; j < CPL; ++j) {
-            float gf[8];
-            unpack8(g[j], gf);
+            for (int j = 0; j < CPL; ++j) {
+                float gf[8];
+                unpack8(g[j], gf);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) am_y = most(am_y, fabsf(h[j][i] * gf[i]));
+                for (int i = 0; i < 8; ++i) am_y = most(am_y, fabsf(h[j][i] * gf[i]));
+            }
+            am_y = lanes_most<T>(am_y);
         }
-        am_y = lanes_most<T>(am_y);
-    }
-    if (row_h) {
+        if (row_h) {
+            am_h = 0.f;
+#pragma unroll
+            for (int j = 0; j < CPL; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) am_h = most(am_h, fabsf(h[j][i]));
+            am_h = lanes_most<T>(am_h);
+        }
+        sum = lanes_sum<T>(sum);
+        if (T > 64) {
+            if ((tid & 63) == 0) {
+                red[0][tid >> 6] = sum;
+                red[1][tid >> 6] = am_y;
+                red[2][tid >> 6] = am_h;
+            }
+            __syncthreads();
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WG / 64; ++w) {
+                sum += red[0][w];
+                am_y = most(am_y, red[1][w]);
+                am_h = most(am_h, red[2][w]);
+            }
+        }
+    };
+    over_row();
+    // RANGE: a row whose squares fp32 does not hold (all of its lanes see the same sum) is taken up or down by a power of two, which is
+    // exact; from here on h and 1 / rstd are in that unit.
+    float up = 1.0f, down = 1.0f;
+    if (RANGE && !(sum < 0x1p100f && sum >= kLeast)) {
+        const bool small = sum < 1.0f;
+        up = small ? 0x1p96f : 0x1p-72f;
+        down = small ? 0x1p-96f : 0x1p72f;
+        sum = 0.f;
 #pragma unroll
         for (int j = 0; j < CPL; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) am_h = most(am_h, fabsf(h[j][i]));
-        am_h = lanes_most<T>(am_h);
-    }
-    sum = lanes_sum<T>(sum);
-    if (T > 64) {
-        if ((tid & 63) == 0) {
-            red[0][tid >> 6] = sum;
-            red[1][tid >> 6] = am_y;
-            red[2][tid >> 6] = am_h;
-        }
-        __syncthreads();
-        sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < WG / 64; ++w) {
-            sum += red[0][w];
-            am_y = most(am_y, red[1][w]);
-            am_h = most(am_h, red[2][w]);
-        }
+            for (int i = 0; i < 8; ++i) {
+                h[j][i] *= up;
+                sum = __builtin_fmaf(h[j][i], h[j][i], sum);
+            }
+        if (T > 64) __syncthreads();   // (everyone has read the first sums)
+        over_row();
     }
     if (!live) return;
-    const float rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps);
-    if (a.rstd && t == 0) a.rstd[row] = rstd;
+    const float rstd = 1.0f / sqrtf(sum / static_cast<float>(a.cols) + a.eps * up * up);
+    if (a.rstd && t == 0) a.rstd[row] = rstd * up;
 
     float sy = 0.f, iy = 0.f, sh = 0.f, ih = 0.f;
     if (row_y) {
@@ -150,7 +178,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
         if (t == 0) a.y_scales[row] = sy;
     }
     if (row_h) {
-        e4m3_group(false, am_h, 1.0f, sh, ih);
+        e4m3_group(false, am_h, down, sh, ih);
         if (t == 0) a.hs[row] = sh;
     }
 #pragma unroll
@@ -163,7 +191,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = most(m, fabsf(h[j][i]));
                 m = lanes_most<16>(m);
-                e4m3_group(a.ckpt_mode == kModePow2, m, 1.0f, sh, ih);
+                e4m3_group(a.ckpt_mode == kModePow2, m, down, sh, ih);
                 if ((t & 15) == 0 && c < chunks) a.hs[row * (a.cols >> 7) + (c >> 4)] = sh;
             }
             // (past the caches too where y is bf16, 32768 x 4096 217 -> 187 us; beside codes it costs: e4m3 172 -> 176, MXFP4 158 -> 168)
@@ -398,8 +426,9 @@ static loka_status forward_launch(RmsArgs a, hipStream_t stream) {
     constexpr int WG = T < 256 ? 256 : T;
     return in_launches((a.rows + WG / T - 1) / (WG / T), WG, [&](int64_t from, uint32_t grid) {
         a.first_wg = from;
-        if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true><<<grid, WG, 0, stream>>>(a);
-        else add_rmsnorm_kernel<T, CPL, false><<<grid, WG, 0, stream>>>(a);
+        if (a.eps < kLeast) add_rmsnorm_kernel<T, CPL, false, true><<<grid, WG, 0, stream>>>(a);
+        else if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true, false><<<grid, WG, 0, stream>>>(a);
+        else add_rmsnorm_kernel<T, CPL, false, false><<<grid, WG, 0, stream>>>(a);
     });
 }
 
