@@ -346,6 +346,10 @@ size_t loka_mxfp4_gemm_workspace(const loka_gemm_desc* desc);
 loka_status loka_mxfp4_gemm(const loka_gemm_desc* desc, const uint8_t* xq, const uint8_t* sx, const uint8_t* wq,
                             const uint8_t* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
                             void* hip_stream);
+/* Test aid, host only: the kernel that loka_mxfp4_gemm runs for desc.  0: weights streamed into registers; 1: tiles of 256 x 256;
+ * 2: tiles of 128 x 128 in two halves of K (split over workgroups where loka_mxfp4_gemm_workspace is not 0); 3: tiles of 128 x 128;
+ * -1: refused. */
+int loka_test_mxfp4_form(const loka_gemm_desc* desc);
 
 /* A layer with kept 4-bit weights on bf16 activations, for any number of rows: loka_mxfp4_quantize(x) and loka_mxfp4_gemm
  * in one call, with the same codes.  At most 16 rows (single tokens, small serving batches) are one launch that quantizes

@@ -113,6 +113,7 @@ _SIGNATURES = [
     ("loka_mxfp4_padded", c_int64, [c_int64]),
     ("loka_mxfp4_quantize", c_int, [c_void_p, c_int64, c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
     ("loka_mxfp4_dequantize", c_int, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_void_p]),
+    ("loka_test_mxfp4_form", c_int, [POINTER(GemmDesc)]),
     ("loka_mxfp4_gemm_workspace", c_size_t, [POINTER(GemmDesc)]),
     ("loka_mxfp4_gemm", c_int, [POINTER(GemmDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                 c_size_t, c_void_p]),

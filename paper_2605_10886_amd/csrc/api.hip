@@ -51,6 +51,7 @@ loka_status tracker_update_launch(const void*, int64_t, int64_t, int64_t, int64_
 loka_status mxfp4_quantize_launch(const void*, int64_t, int64_t, int64_t, int, uint8_t*, uint8_t*, hipStream_t);
 loka_status mxfp4_dequantize_launch(const uint8_t*, const uint8_t*, int64_t, int64_t, void*, int64_t, hipStream_t);
 // mxfp4_gemm.hip
+int mxfp4_gemm_form(const loka_gemm_desc*);
 size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc*);
 loka_status mxfp4_gemm_launch(const loka_gemm_desc*, const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, void*, float*, void*,
                               size_t, hipStream_t);
@@ -474,6 +475,8 @@ static loka_status validate_mxfp4(const loka_gemm_desc* d, bool linear) {
     }
     return LOKA_OK;
 }
+
+int loka_test_mxfp4_form(const loka_gemm_desc* desc) { return validate_mxfp4(desc, false) != LOKA_OK ? -1 : mxfp4_gemm_form(desc); }
 
 size_t loka_mxfp4_gemm_workspace(const loka_gemm_desc* desc) {
     return validate_mxfp4(desc, false) != LOKA_OK ? 0 : mxfp4_gemm_workspace_bytes(desc);

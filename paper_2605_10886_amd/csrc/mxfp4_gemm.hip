@@ -756,6 +756,8 @@ static MxPlan plan_of(const loka_gemm_desc* d) {
     return p;
 }
 
+int mxfp4_gemm_form(const loka_gemm_desc* d) { return plan_of(d).kind; }
+
 size_t mxfp4_gemm_workspace_bytes(const loka_gemm_desc* d) {
     const MxPlan p = plan_of(d);
     return p.splits > 1 ? static_cast<size_t>(p.splits) * d->batch * d->M * d->N * 4 : 0;
