@@ -220,3 +220,22 @@ def test_columns_quantized_past_4_gb():
     assert not bool(q[:, 32: first // 2].any()) and not bool(s[:, 2: first // 32].any())
     end = -(-M // 32)
     assert not bool(q[:, end * 16:].any()) and not bool(s[:, end:].any())
+
+
+def test_every_scale_byte():
+    # values of all codes under all bytes (those beyond bf16's range are infinite, 255 is NaN), and the product of every pair of scales
+    byte = torch.arange(256, device=DEV, dtype=torch.uint8)
+    q = torch.zeros(256, 64, dtype=torch.uint8, device=DEV)
+    q[:, :8] = torch.tensor([0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE], dtype=torch.uint8, device=DEV)
+    s = byte[:, None].repeat(1, 4).contiguous()
+    got, want = B.loka_mxfp4_dequantize(q, s, 16).double(), P.mx_values(q, s)[:, :16].float().bfloat16().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+    for M, N, form in ((255, 255, S.STREAM), (4080, 4080, S.SMALL)):
+        d = B.make_mxfp4_desc(M, N, 128)
+        assert B.lib().loka_test_mxfp4_form(ctypes.byref(d)) == form
+        (xq, sx), (wq, sw) = ((torch.zeros(r, 64, dtype=torch.uint8, device=DEV), torch.zeros(r, 4, dtype=torch.uint8, device=DEV)) for r in (M, N))
+        xq[:, 0], wq[:, 0] = 2, 2
+        sx[:, 0], sw[:, 0] = byte[torch.arange(M, device=DEV) % 255], byte[torch.arange(N, device=DEV) % 255]
+        _, y = B.loka_mxfp4_gemm(d, xq, sx, wq, sw, want_y=True)
+        # a power of two: exact down to the last subnormal, 0 below, infinite from 2^128 on
+        assert torch.equal(y, (P.mx_values(xq, sx)[:, :1] * P.mx_values(wq, sw)[:, :1].t()).float())
