@@ -115,7 +115,7 @@ __device__ __forceinline__ void mx_request_rows(const uint16_t* x, int64_t ldx, 
         __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void*)(raw + i * 1024), 16, static_cast<int>(first) * 2 + (lane ^ i) * 16, 0, 0, 0);
     }
 }
-// ... rows that start or end anywhere through registers (16 x 14000 x 3001, rows x columns x K, 9.5 us; quantized by rows, 4 lanes a group, 24.4)
+// ... rows that start or end anywhere through registers (rows x columns x K: 16 x 14000 x 3001 9.5 us; quantized by rows, 4 lanes a group, 24.4)
 __device__ __forceinline__ void mx_load_rows(const uint16_t* x, int64_t ldx, int rows, int64_t first, int64_t K, int lane, u32x4 (&v)[16]) {
     const int64_t c = first + lane * 8;
     if (K >= 8) {
@@ -166,8 +166,8 @@ __device__ __forceinline__ void in_order() {
 }
 
 // ---------------------------------------------------------------------------------
-// Few rows: bound by the weights' traffic (16 x 4096 x 16384, rows x K x columns, 9.5 us with the quantization of x: 3.8 TB/s of codes;
-// 16 x 8192 x 28672 35 us).  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
+// Few rows: bound by the weights' traffic (rows x columns x K here and below: 16 x 16384 x 4096 9.5 us with the quantization of x, 3.8 TB/s of
+// codes; 16 x 28672 x 8192 35 us).  A workgroup of NW waves owns 16 NT columns x 16 MT rows of the result; the waves
 // take 512-element pieces of the contraction in turn, straight from memory into registers, and add their partial sums in LDS
 // in wave order.
 // QUANT 0: stored X.  1, 2, 3: bf16 X of up to 16 rows (MT = 1): by groups; by rows (up to 2); by groups, rows that start or end anywhere.
@@ -272,8 +272,8 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 //
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds row r = l % 32, one group of 32 elements (of the two: h = l / 32) and its scale
 // byte.  The four instructions of a K tile (quarters s) take groups 4 h + s, so a lane's four scale bytes are one word.
-// From registers, on changing operands, this form sustains 6.6 PFLOP/s on 4-bit codes and the 16 x 16 x 128 form 5.8, which
-// the 16-byte encoding holds at 24 cycles an instruction.  WK = 1: a wave multiplies all quarters; WK = 2: two of them, and
+// From registers, on changing operands, this form sustains 6.0 - 6.3 PFLOP/s on 4-bit codes and the 16 x 16 x 128 form 6.4 - 6.8; here
+// half as many instructions, and longer runs to store, win: 32768 x 4096 x 4096 358 -> 344 us, 8192 x 8192 x 8192 the same.  WK = 1: a wave multiplies all quarters; WK = 2: two of them, and
 // two waves add up at the end (two waves on a SIMD where the tile gives only four).
 // W's rows are dealt to the instruction's so that a lane's values are two runs of 8 columns.
 //
@@ -675,10 +675,11 @@ static loka_status stream_launch(MxArgs a, int64_t batch, hipStream_t stream) {
 }
 
 // Columns of a workgroup.  Quantizing groups of x takes all of a CU's LDS, and x anew in every workgroup: as few columns as need no
-// second round (16 rows, us by 16 / 32 / 64 columns: 4112 columns x K 4096 8.6 / 6.6 / 8.6, 4096 5.5 / 6.5 / 8.4, 12000 13.9 / 11.7 / 9.0).
-// Elsewhere several workgroups share a CU, and more columns in one pay only where there are many and K is not long (two
-// rows quantized by rows: 12000 x 4096 7.6 / 8.6 / 8.4, 16384 x 4096 10.1 / 8.9 / 9.0, 8192 x 16384 16.1 / 21.5 / 23.8, rows that start anywhere,
-// which take longer, 14000 x 3001 8.8 / 7.3; 16 stored ones 32768 x 1024 7.4 / 6.6 / 6.0, 8192 x 16384 20 / 41 / 28).
+// second round (us by 16 / 32 / 64 columns a workgroup: 16 x 4112 x 4096 8.6 / 6.6 / 8.6, 16 x 4096 x 4096 5.5 / 6.5 / 8.4, 16 x 12000 x 4096
+// 13.9 / 11.7 / 9.0).
+// Elsewhere several workgroups share a CU, and more columns in one pay only where there are many and K is not long (quantized
+// by rows: 2 x 12000 x 4096 7.6 / 8.6 / 8.4, 2 x 16384 x 4096 10.1 / 8.9 / 9.0, 2 x 8192 x 16384 16.1 / 21.5 / 23.8, rows that start anywhere,
+// which take longer, 2 x 14000 x 3001 8.8 / 7.3; stored X: 16 x 32768 x 1024 7.4 / 6.6 / 6.0, 16 x 8192 x 16384 20 / 41 / 28).
 template <int MT, int QUANT>
 static loka_status stream_columns(const MxArgs& a, int64_t batch, hipStream_t stream) {
     const int64_t runs = (a.N + 15) / 16 * batch;          // of 16 columns
@@ -829,7 +830,8 @@ loka_status mxfp4_linear_fused_launch(const loka_gemm_desc* d, const void* x_bf1
     a.x = static_cast<const uint16_t*>(x_bf16);
     a.ldx = ld;
     a.x_whole = aligned16(x_bf16) && ld % 8 == 0 && a.K % 8 == 0;
-    // (by rows / by groups, us: 1 x 4096 x 4096 4.0 / 4.5, 2 rows 4.2 / 4.5, 3 rows 4.5 / 4.5, 4 rows 4.8 / 4.4, 1 x 4096 x 16384 9.2 / 10.7)
+    // (rows x columns x K, us by rows / by groups: 1 x 4096 x 4096 4.0 / 4.5, 2 x 4096 x 4096 4.2 / 4.5, 3 x 4096 x 4096 4.5 / 4.5, 4 x 4096 x 4096
+    // 4.8 / 4.4, 1 x 4096 x 16384 9.2 / 10.7)
     if (a.M <= 2) return stream_columns<1, 2>(a, 1, stream);
     if (a.x_whole && a.K < (INT64_C(1) << 30)) return stream_columns<1, 1>(a, 1, stream);
     return stream_columns<1, 3>(a, 1, stream);

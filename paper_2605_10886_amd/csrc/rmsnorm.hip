@@ -52,7 +52,8 @@ __device__ __forceinline__ void unpack8(const u32x4 w, float (&f)[8]) {
 }
 
 // Scale and factor of an e4m3 group of y = v * rstd whose largest |v| is `am` (rstd = 1, or a power of two: of v itself, in its unit).  Away from the floor
-// amax / 448 and 448 / amax: rstd cancels in the factor, so a code has one rounding fewer than v * rstd, then * 448 / amax.
+// amax / 448 and 448 / amax: rstd cancels in the factor, so a code has one rounding fewer than v * rstd, then * 448 / amax
+// (32768 x 4096, row scales: 122 codes are not the 64-bit formula's, where torch's fp32 operations leave 176).
 // A group with an infinite or NaN value gets a NaN scale.
 __device__ __forceinline__ void e4m3_group(bool pow2, float am, float rstd, float& scale, float& inv) {
     const float top = am * rstd;
@@ -266,8 +267,8 @@ __device__ __forceinline__ void e4m3_values(const u32x2 w, float (&f)[8]) {
 
 // Layout of rows and chunks as above; a workgroup walks over rows, adding dgamma's terms of its columns in registers, and
 // leaves one row of partial sums.  A row stays in its loaded form (11 registers a chunk, 16 as fp32) between its two
-// uses, so that the next row's loads are in flight while this one is reduced (PREFETCH; not in 1024 threads, which have half
-// the registers).
+// uses, so that the next row's loads are in flight while this one is reduced (PREFETCH; not beyond 16384 elements, whose 1024 threads
+// hold four chunks each in half the registers).
 template <int T, int CPL, bool PREFETCH, bool STREAMED>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(const RmsBackArgs a) {
     constexpr int WG = T < 256 ? 256 : T, RPW = WG / T;
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rmsnorm_backward_kernel(con
         if (a.gamma && t + j * T < chunks) return *reinterpret_cast<const u32x4*>(a.gamma + (t + j * T) * 8);
         return u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
     };
-    constexpr bool KEEP = T < 1024;    // gamma in registers
+    constexpr bool KEEP = T < 1024;    // gamma in registers (1024 threads have half as many: read again for each row)
     float dg[CPL][8];
     u32x4 g[KEEP ? CPL : 1];
 #pragma unroll
