@@ -376,7 +376,7 @@ loka_status loka_mxfp4_linear(const loka_gemm_desc* desc, const void* x_bf16, in
  * A row with a NaN or an infinity: bf16 and MXFP4 values that are NaN by the formula are NaN, and an e4m3 scale group that
  * holds such a value has a NaN scale.  The sum of squares is held in fp32: it has to stay below 3.4e38.  Where eps is below
  * 8e-28 (0 among them) neither that nor a sum too small for fp32 is a limit: such a row is scaled by a power of two, and every
- * finite h gives its y (rstd itself is fp32: infinite where eps is 0 and the root of the mean square below 2.9e-39).
+ * finite row gives its y (rstd itself is fp32: infinite where eps is 0 and the root of the mean square below 2.9e-39).
  * cols % 16 == 0 and at most 32768; cols % 128 == 0 for the block modes.  ld_x, ld_r (row strides of x and residual, in
  * elements) multiples of 8 and at least cols; outputs are contiguous.  Pointers 16-byte aligned (scales and rstd: 4).
  * h_out may be x or residual itself, with a row stride of cols (LOKA_ERR_SHAPE otherwise); no other outputs may overlap inputs. */

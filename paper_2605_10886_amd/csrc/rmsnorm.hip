@@ -69,7 +69,7 @@ __device__ __forceinline__ void e4m3_group(bool pow2, float am, float rstd, floa
 
 // A sum of squares from here on has fp32's precision (each of up to 32768 terms below 2^-126 is off by at most 2^-150), and beside an eps from
 // here on a smaller sum's errors do not matter.  For a smaller eps another instance of the kernel looks at every sum: its branch, and
-// what is not moved over it, cost rows that do not need it 0.1 us a launch and up to 5 % (5984 x 1280 11.9 -> 12.3 us).
+// what is not moved over it, cost rows that do not need it 0.1 us a launch and up to 3 % (5984 x 1280 12.6 -> 12.9 us, 32768 x 4096 the same).
 constexpr float kLeast = 0x1p-90f;
 
 // ---------------------------------------------------------------------------------
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
     // RANGE: a row whose squares fp32 does not hold (all of its lanes see the same sum) is taken up or down by a power of two, which is
     // exact; from here on h and 1 / rstd are in that unit.
     float up = 1.0f, down = 1.0f;
-    if (RANGE && !(sum < 0x1p100f && sum >= kLeast)) {
+    if (RANGE && __builtin_expect(!(sum < 0x1p126f && sum >= kLeast), 0)) {
         const bool small = sum < 1.0f;
         up = small ? 0x1p96f : 0x1p-72f;
         down = small ? 0x1p-96f : 0x1p72f;
@@ -166,6 +166,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void add_rmsnorm_kernel(const Rm
                 h[j][i] *= up;
                 sum = __builtin_fmaf(h[j][i], h[j][i], sum);
             }
+#pragma unroll
+        for (int j = 0; j < CPL; ++j) asm volatile("" : "+v"(g[j]));       // (or gamma is unpacked once for both paths, and held: 72 registers for 62)
         if (T > 64) __syncthreads();   // (everyone has read the first sums)
         over_row();
     }
@@ -427,9 +429,14 @@ static loka_status forward_launch(RmsArgs a, hipStream_t stream) {
     constexpr int WG = T < 256 ? 256 : T;
     return in_launches((a.rows + WG / T - 1) / (WG / T), WG, [&](int64_t from, uint32_t grid) {
         a.first_wg = from;
-        if (a.eps < kLeast) add_rmsnorm_kernel<T, CPL, false, true><<<grid, WG, 0, stream>>>(a);
-        else if (streamed(a.rows, a.cols)) add_rmsnorm_kernel<T, CPL, true, false><<<grid, WG, 0, stream>>>(a);
-        else add_rmsnorm_kernel<T, CPL, false, false><<<grid, WG, 0, stream>>>(a);
+        const bool past = streamed(a.rows, a.cols);
+        if (a.eps < kLeast) {
+            if (past) add_rmsnorm_kernel<T, CPL, true, true><<<grid, WG, 0, stream>>>(a);
+            else add_rmsnorm_kernel<T, CPL, false, true><<<grid, WG, 0, stream>>>(a);
+        } else {
+            if (past) add_rmsnorm_kernel<T, CPL, true, false><<<grid, WG, 0, stream>>>(a);
+            else add_rmsnorm_kernel<T, CPL, false, false><<<grid, WG, 0, stream>>>(a);
+        }
     });
 }
 
