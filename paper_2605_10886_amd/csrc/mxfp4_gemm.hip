@@ -273,8 +273,9 @@ __global__ __launch_bounds__(64 * NW) void mx_stream_kernel(const MxArgs a) {
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane l holds row r = l % 32, one group of 32 elements (of the two: h = l / 32) and its scale
 // byte.  The four instructions of a K tile (quarters s) take groups 4 h + s, so a lane's four scale bytes are one word.
 // From registers, on changing operands, this form sustains 6.0 - 6.3 PFLOP/s on 4-bit codes and the 16 x 16 x 128 form 6.4 - 6.8; here
-// half as many instructions, and longer runs to store, win: 32768 x 4096 x 4096 358 -> 344 us, 8192 x 8192 x 8192 the same.  WK = 1: a wave multiplies all quarters; WK = 2: two of them, and
-// two waves add up at the end (two waves on a SIMD where the tile gives only four).
+// half as many instructions, and longer runs to store, win: 32768 x 4096 x 4096 358 -> 344 us, 8192 x 8192 x 8192 the same.
+// WK = 1: a wave multiplies all quarters; WK = 2: two of them, and two waves add up at the end (two waves on a SIMD where the
+// tile gives only four).
 // W's rows are dealt to the instruction's so that a lane's values are two runs of 8 columns.
 //
 // One barrier a K tile: its last operands are in registers when the barrier is passed, so the loads of a K tile R further on
