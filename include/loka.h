@@ -406,6 +406,120 @@ loka_status loka_rmsnorm_backward(const loka_rms_desc* desc, const void* dy_bf16
                                   const float* rstd, const void* gamma_bf16, const void* dh_bf16, void* dx_bf16,
                                   float* dgamma, void* workspace, size_t ws_bytes, void* hip_stream);
 
+/* ---------------------------------------------------------------- a layer of experts
+ * A layer of `experts` (or `groups`) linear layers, of which each token takes top_k: loka_route chooses them and sorts the
+ * (token, choice) pairs by expert, loka_grouped_quantize brings operands into 8 bits, loka_grouped_gemm / _linear multiply each
+ * group of rows by its own weights, loka_grouped_wgrad gives the weights' gradients, loka_combine adds a token's results up.
+ * How many rows an expert gets is on the device only: no call synchronizes or reads it on the host.
+ *
+ * The ROUTED ORDER: all pairs, experts ascending, tokens ascending within an expert.  offsets [groups + 1] int32 (device):
+ * group g owns rows offsets[g] .. offsets[g + 1] - 1; ascending from 0, the last at most `rows`.  Groups may be empty.  Rows from
+ * offsets[groups] on belong to no group: outputs leave them as they were.
+ *
+ * loka_route: of row t of the logits the top_k greatest entries, greatest first (equal ones: the lower index first; a NaN is
+ * greater than any number).  An entry of minus infinity is never chosen: where a row has fewer others, the choices left over are
+ * none (expert and slot -1, weight 0).  Weights, all sums in fp32:
+ *   LOKA_SCORE_SOFTMAX  scale * exp(l_e) / sum over all entries, or, with renorm, over the chosen ones
+ *   LOKA_SCORE_SIGMOID  scale * sigmoid(l_e), with renorm divided by the sum of the chosen ones' sigmoids
+ * A NaN or plus infinity makes the weights NaN that the formula makes so.
+ *   logits  [tokens, ld] bf16 (desc->bf16) or fp32, aligned to an element
+ *   expert, weight, slot [tokens, top_k]: index of the choice, its weight, its row of the routed order
+ *   row     [tokens * top_k]: the token of each row of the routed order, -1 behind the last;  offsets [experts + 1]
+ * Results do not change from call to call.  Workspace: loka_route_workspace(desc) bytes, 16-byte aligned. */
+typedef enum { LOKA_SCORE_SOFTMAX = 0, LOKA_SCORE_SIGMOID = 1 } loka_score;
+typedef struct {
+    int64_t tokens;           /* 1 .. 2^25 */
+    int64_t ld;               /* row stride of the logits in elements, >= experts */
+    int32_t experts;          /* 1 .. 1024 */
+    int32_t top_k;            /* 1 .. 16, at most experts */
+    int32_t score;            /* loka_score */
+    int32_t renorm;           /* != 0: the chosen weights add up to scale */
+    int32_t bf16;             /* != 0: the logits (and their gradient) are bf16, else fp32 */
+    float scale;
+} loka_route_desc;
+size_t loka_route_workspace(const loka_route_desc* desc);
+loka_status loka_route(const loka_route_desc* desc, const void* logits, int32_t* expert, float* weight, int32_t* slot,
+                       int32_t* row, int32_t* offsets, void* workspace, size_t ws_bytes, void* hip_stream);
+/* Gradient of the logits from that of the weights, dweight fp32 [tokens, top_k] (not read where there was no choice); expert as
+ * loka_route wrote it.  dlogits [tokens, experts], contiguous, of the logits' type; every entry is written. */
+loka_status loka_route_backward(const loka_route_desc* desc, const void* logits, const int32_t* expert, const float* dweight,
+                                void* dlogits, void* hip_stream);
+
+/* 8-bit operands of grouped products: e4m3 codes with a power-of-two scale (fp32) per 128 elements of the contraction, by the rule
+ * of LOKA_SCALE_BLOCK_1x128_POW2 (scale = the least power of two s with amax / s <= 448).  A group of 128 with a NaN or an infinity
+ * has a NaN scale and zero codes: every sum that it enters is NaN.  Two stored forms of a matrix x [rows, cols]:
+ *   ALONG   contraction over cols: q [rows][colsp] codes, scales [rows][colsp / 128]; colsp = cols up to a multiple of 128, zero
+ *           codes behind cols (where cols is such a multiple, what loka_quantize and loka_add_rmsnorm write in that mode)
+ *   TURNED  contraction over rows, each group of rows by itself: a group's rows in blocks of 128 from its first row on, zero codes behind its
+ *           last; the groups' blocks follow each other.  qt [blocks][cols][128] codes, st [blocks][cols].
+ * loka_grouped_blocks(rows, groups): blocks to provide for any group sizes (blocks that no group takes are left as they were).  Host only; -1
+ * for sizes out of range.
+ * x_bf16 [x_rows, ld], any alignment of an element.  index int32 [rows] (device) or NULL: row p of the matrix is row index[p] of x
+ * (indices outside 0 .. x_rows - 1: a row of zeros); NULL: row p (x_rows is not read).  offsets NULL: `groups` groups of
+ * rows / groups rows each, which `groups` has to divide.  q and scales, and qt and st: both or neither; one pair at least.  Weights
+ * [groups, K, N] are x with rows = groups * K, cols = N: TURNED is what a product over K takes, ALONG what one over N takes. */
+typedef struct {
+    int64_t rows, cols;       /* of the matrix; rows at most 2^31 - 1, cols at most 2^20 */
+    int64_t ld;               /* row stride of x in elements, >= cols */
+    int64_t x_rows;
+    int32_t groups;           /* 1 .. 1024 */
+} loka_grouped_quantize_desc;
+int64_t loka_grouped_blocks(int64_t rows, int64_t groups);
+loka_status loka_grouped_quantize(const loka_grouped_quantize_desc* desc, const void* x_bf16, const int32_t* index, const int32_t* offsets,
+                                  uint8_t* q, float* scales, uint8_t* qt, float* st, void* hip_stream);
+
+/* Y[p, n] = sum_k x[p, k] w_g[k, n] for the rows p of each group g: FP8 operands and their scales on the scaled matrix instruction,
+ * fp32 accumulation.
+ *   xq, sx  ALONG, contraction over K: [rows] in the routed order, or, with index (int32 [rows], device), [x_rows], of which row
+ *           p of the product takes row index[p] (an index outside is read as the nearest one inside)
+ *   wq, sw  w_form LOKA_W_TURNED: [groups][Kp / 128][N][128], scales [groups][Kp / 128][N] (of weights [groups, K, N])
+ *           w_form LOKA_W_ALONG:  [groups][N][Kp], scales [groups][N][Kp / 128]             (of weights [groups, N, K]: dX = dY W^T)
+ *   out_bf16 and / or y_fp32 [rows, N], 16-byte aligned; at least one.  Any N, K (at most 2^20).  Scales have to be powers of two (their exponents are read).
+ * No workspace.  Results do not change from call to call. */
+typedef enum { LOKA_W_TURNED = 0, LOKA_W_ALONG = 1 } loka_w_form;
+typedef struct {
+    int64_t rows;             /* of the routed order, at most 2^31 - 1 */
+    int64_t x_rows;           /* rows that index may name (not read without index) */
+    int64_t N, K;
+    int32_t groups;           /* 1 .. 1024 */
+    int32_t w_form;           /* loka_w_form (loka_grouped_wgrad: not read) */
+} loka_grouped_desc;
+loka_status loka_grouped_gemm(const loka_grouped_desc* desc, const uint8_t* xq, const float* sx, const int32_t* index,
+                              const int32_t* offsets, const uint8_t* wq, const float* sw, void* out_bf16, float* y_fp32, void* hip_stream);
+
+/* The same from bf16 tokens x [x_rows (without index: rows), ld], quantized in the call: the results of loka_grouped_quantize (ALONG)
+ * and loka_grouped_gemm, for a serving loop's single tokens up to whole batches.
+ * Workspace: loka_grouped_linear_workspace(desc, with_index) bytes, 16-byte aligned (codes and scales of x). */
+size_t loka_grouped_linear_workspace(const loka_grouped_desc* desc, int with_index);
+loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf16, int64_t ld, const int32_t* index, const int32_t* offsets,
+                                const uint8_t* wq, const float* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
+                                void* hip_stream);
+
+/* Gradients of the weights: dw_g[k, n] = sum over the group's rows p of x[p, k] dy[p, n] (an empty group: zeros).
+ *   xt, sxt, dyt, sdyt  TURNED forms of x [rows, K] and dy [rows, N], of the same offsets
+ *   dw_bf16 and / or dw_fp32 [groups][K][N], 16-byte aligned; at least one
+ * Workspace: loka_grouped_wgrad_workspace(desc) bytes (partial sums where there are few results and long groups; added in a fixed order:
+ * results do not change from call to call), 16-byte aligned. */
+size_t loka_grouped_wgrad_workspace(const loka_grouped_desc* desc);
+loka_status loka_grouped_wgrad(const loka_grouped_desc* desc, const uint8_t* xt, const float* sxt, const uint8_t* dyt, const float* sdyt,
+                               const int32_t* offsets, void* dw_bf16, float* dw_fp32, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* out[t] = sum over j of weight[t, j] * y[slot[t, j]] (+ residual[t]), fp32 sums in the order of j, one rounding to bf16.  A slot outside
+ * 0 .. rows - 1 adds nothing.  y_bf16 [rows, cols]; weight fp32 [tokens, top_k] or NULL (1: the sum that dX's rows take); residual
+ * bf16 [tokens, cols] or NULL; out bf16 [tokens, cols], which may be the residual itself.  Matrices are contiguous; pointers 16-byte (slot, weight: 4-byte) aligned.
+ * Backward: dy[slot[t, j]] = weight[t, j] * dout[t] (bf16; rows that no slot names are left as they were) and dweight[t, j] =
+ * sum over the columns of dout[t] * y[slot[t, j]] (fp32, a fixed order; 0 for a slot outside).  dy or dweight may be NULL, y where dweight is.
+ * Slots name different rows, as loka_route's do. */
+typedef struct {
+    int64_t tokens, cols;     /* tokens * top_k at most 2^30, cols at most 2^20 */
+    int64_t rows;             /* of y and dy, at most 2^31 - 1 */
+    int32_t top_k;            /* 1 .. 16 */
+} loka_combine_desc;
+loka_status loka_combine(const loka_combine_desc* desc, const void* y_bf16, const int32_t* slot, const float* weight,
+                         const void* residual_bf16, void* out_bf16, void* hip_stream);
+loka_status loka_combine_backward(const loka_combine_desc* desc, const void* dout_bf16, const void* y_bf16, const int32_t* slot,
+                                  const float* weight, void* dy_bf16, float* dweight, void* hip_stream);
+
 /* ---------------------------------------------------------------- probe reference
  * Yref = X . W from the UNQUANTIZED bf16 operands with fp32 accumulation: the
  * high-precision reference the probe measures FP8 against (Section 2.3, "Error

@@ -31,6 +31,8 @@ NORM_NONE, NORM_LAYERNORM, NORM_RMSNORM, NORM_BLOCKNORM = range(4)
 NORMS = {"none": NORM_NONE, "layernorm": NORM_LAYERNORM, "rmsnorm": NORM_RMSNORM, "blocknorm": NORM_BLOCKNORM}
 ACT_NONE, ACT_HARDSWISH = 0, 1
 RMS_OUT_BF16, RMS_OUT_E4M3, RMS_OUT_MXFP4 = range(3)
+SCORE_SOFTMAX, SCORE_SIGMOID = range(2)
+W_TURNED, W_ALONG = range(2)
 
 
 class GemmDesc(Structure):
@@ -43,6 +45,23 @@ class GemmDesc(Structure):
 class RmsDesc(Structure):
     _fields_ = [("rows", c_int64), ("cols", c_int64), ("ld_x", c_int64), ("ld_r", c_int64),
                 ("out", c_int32), ("out_mode", c_int32), ("ckpt_mode", c_int32), ("eps", c_float)]
+
+
+class RouteDesc(Structure):
+    _fields_ = [("tokens", c_int64), ("ld", c_int64), ("experts", c_int32), ("top_k", c_int32), ("score", c_int32),
+                ("renorm", c_int32), ("bf16", c_int32), ("scale", c_float)]
+
+
+class GroupedQuantizeDesc(Structure):
+    _fields_ = [("rows", c_int64), ("cols", c_int64), ("ld", c_int64), ("x_rows", c_int64), ("groups", c_int32)]
+
+
+class GroupedDesc(Structure):
+    _fields_ = [("rows", c_int64), ("x_rows", c_int64), ("N", c_int64), ("K", c_int64), ("groups", c_int32), ("w_form", c_int32)]
+
+
+class CombineDesc(Structure):
+    _fields_ = [("tokens", c_int64), ("cols", c_int64), ("rows", c_int64), ("top_k", c_int32)]
 
 
 class ProbeStats(Structure):
@@ -125,6 +144,22 @@ _SIGNATURES = [
     ("loka_rmsnorm_backward_workspace", c_size_t, [POINTER(RmsDesc)]),
     ("loka_rmsnorm_backward", c_int, [POINTER(RmsDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("loka_route_workspace", c_size_t, [POINTER(RouteDesc)]),
+    ("loka_route", c_int, [POINTER(RouteDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("loka_route_backward", c_int, [POINTER(RouteDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    ("loka_grouped_blocks", c_int64, [c_int64, c_int64]),
+    ("loka_grouped_quantize", c_int, [POINTER(GroupedQuantizeDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_void_p]),
+    ("loka_grouped_gemm", c_int, [POINTER(GroupedDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                  c_void_p]),
+    ("loka_grouped_linear_workspace", c_size_t, [POINTER(GroupedDesc), c_int]),
+    ("loka_grouped_linear", c_int, [POINTER(GroupedDesc), c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                    c_void_p, c_size_t, c_void_p]),
+    ("loka_grouped_wgrad_workspace", c_size_t, [POINTER(GroupedDesc)]),
+    ("loka_grouped_wgrad", c_int, [POINTER(GroupedDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_size_t, c_void_p]),
+    ("loka_combine", c_int, [POINTER(CombineDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    ("loka_combine_backward", c_int, [POINTER(CombineDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
 ]
 EXPORTS = [s[0] for s in _SIGNATURES]
 
@@ -332,6 +367,69 @@ def loka_rmsnorm_backward(dy, hq, hs, rstd, gamma=None, dh=None, ckpt_mode: int 
     """The gradient of loka_add_rmsnorm's input from its checkpoint; dh: the gradient that reaches the sum past the norm.
     Returns (dx bf16 [rows, cols], dgamma fp32 [cols] or None)."""
     return (_native or _host()).rmsnorm_backward(dy, hq, hs, rstd, gamma, dh, ckpt_mode, want_dgamma, dx, workspace)
+
+
+RouteOut = namedtuple("RouteOut", "experts weights slots rows offsets")
+
+
+def loka_route(logits, top_k: int, score: int = SCORE_SOFTMAX, renorm: bool = True, scale: float = 1.0, workspace=None) -> RouteOut:
+    """The top_k experts of each row of logits [tokens, experts] (bf16 or fp32), their weights fp32, and the routed order: slots
+    [tokens, top_k] (row of each choice), rows [tokens * top_k] (token of each row), offsets [experts + 1]; int32, on the device."""
+    return tuple.__new__(RouteOut, (_native or _host()).route(logits, top_k, score, renorm, scale, workspace))
+
+
+def loka_route_backward(logits, experts, dweights, score: int = SCORE_SOFTMAX, renorm: bool = True, scale: float = 1.0, dlogits=None):
+    """The gradient of the logits (of their type) from that of loka_route's weights."""
+    return (_native or _host()).route_backward(logits, experts, dweights, score, renorm, scale, dlogits)
+
+
+def loka_grouped_blocks(rows: int, groups: int) -> int:
+    return int(lib().loka_grouped_blocks(int(rows), int(groups)))
+
+
+GroupedOut = namedtuple("GroupedOut", "q scales qt st")
+
+
+def loka_grouped_quantize(x, groups: int = 1, offsets=None, index=None, along: bool = True, turned: bool = False, q=None, scales=None,
+                          qt=None, st=None) -> GroupedOut:
+    """x bf16 [rows, cols], or its rows `index` in their order, as operands of grouped products.  along: codes [rows, colsp] and scales
+    [rows, colsp / 128]; turned: codes [blocks, cols, 128] and scales [blocks, cols], blocks of 128 rows of one group.  The groups are
+    those of `offsets`, or `groups` equal ones (weights [groups, K, N] as [groups * K, N]).  What is not asked for is None."""
+    return tuple.__new__(GroupedOut, (_native or _host()).grouped_quantize(x, groups, offsets, index, along, turned, q, scales, qt, st))
+
+
+def make_grouped_desc(rows, N, K, groups, turned_w: bool = True) -> GroupedDesc:
+    """rows of the routed order, each [K] times the weights [K, N] of its group.  turned_w: the weights' turned form (of [groups, K, N]), else
+    the one along their rows (of [groups, N, K])."""
+    return GroupedDesc(rows, 0, N, K, groups, W_TURNED if turned_w else W_ALONG)
+
+
+def loka_grouped_gemm(desc: GroupedDesc, xq, sx, wq, sw, offsets, index=None, want_out: bool = True, want_y: bool = False, out=None, y=None):
+    """Each group of rows times its weights, of stored operands; with index, row p is row index[p] of xq.  Returns (bf16 [rows, N] or None, fp32
+    likewise or None)."""
+    return (_native or _host()).grouped_gemm(desc, xq, sx, wq, sw, offsets, index, want_out, want_y, out, y)
+
+
+def loka_grouped_linear(desc: GroupedDesc, x, wq, sw, offsets, index=None, want_out: bool = True, want_y: bool = False, out=None, y=None,
+                        workspace=None):
+    """The same on bf16 tokens x [tokens, K], quantized in the call."""
+    return (_native or _host()).grouped_linear(desc, x, wq, sw, offsets, index, want_out, want_y, out, y, workspace)
+
+
+def loka_grouped_wgrad(desc: GroupedDesc, xt, sxt, dyt, sdyt, offsets, want_out: bool = True, want_y: bool = False, out=None, y=None,
+                       workspace=None):
+    """X^T dY of each group, of turned operands.  Returns (bf16 [groups, K, N] or None, fp32 likewise or None)."""
+    return (_native or _host()).grouped_wgrad(desc, xt, sxt, dyt, sdyt, offsets, want_out, want_y, out, y, workspace)
+
+
+def loka_combine(y, slots, weights=None, residual=None, out=None):
+    """The sum of rows `slots` of y [rows, cols] for each token, times weights [tokens, top_k], plus the residual.  bf16 [tokens, cols]."""
+    return (_native or _host()).combine(y, slots, weights, residual, out)
+
+
+def loka_combine_backward(dout, y, slots, weights=None, rows: int = 0, want_dy: bool = True, want_dweights: bool = True, dy=None):
+    """Gradients of y (rows: of y, where y is None) and of the weights.  Returns (dy bf16 [rows, cols] or None, dweights fp32 or None)."""
+    return (_native or _host()).combine_backward(dout, y, slots, weights, rows, want_dy, want_dweights, dy)
 
 
 def loka_bf16_gemm(desc: GemmDesc, x, w, yref=None, workspace=None):

@@ -21,7 +21,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libloka.so")
 HOST = os.path.join(HERE, "_host.so")
 SOURCES = ["api.hip", "quantize.hip", "gemm.hip", "gemm_panel32.hip", "gemm_wreg.hip", "gemm_strip.hip", "probe.hip", "dispatch.hip", "tracker.hip", "ceiling.hip",
-           "mxfp4.hip", "mxfp4_gemm.hip", "rmsnorm.hip"]
+           "mxfp4.hip", "mxfp4_gemm.hip", "rmsnorm.hip", "experts.hip", "grouped.hip", "grouped_gemm.hip"]
 
 # -packed-fp32-ops off: packed fp32 VALU forms are kept out of the generated code.
 # No fast-math: divisions and square roots stay correctly rounded, no FMA contraction
@@ -36,7 +36,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-cont
 # every LDS read, and the accumulators spill.  The pass is switched off for that file (its other kernels come out
 # the same, instruction for instruction, apart from a few address computations).  mxfp4_gemm.hip: the same pass moves the first
 # half of a K tile's matrix instructions behind the barrier that the second half's operands wait for.
-EXTRA_FLAGS = {"gemm_panel32.hip": ["-mllvm", "-disable-machine-sink"], "mxfp4_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
+EXTRA_FLAGS = {"gemm_panel32.hip": ["-mllvm", "-disable-machine-sink"], "mxfp4_gemm.hip": ["-mllvm", "-disable-machine-sink"],
+               "grouped_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
 
 
 def _hipcc() -> str:

@@ -1,6 +1,7 @@
 // C ABI of the library: argument validation (host only, before any HIP call) and
 // forwarding to the kernel launchers.  See include/loka.h for the contract.
 #include "common.h"
+#include "experts.h"
 
 #include <algorithm>
 #include <cstdint>
@@ -586,6 +587,165 @@ loka_status loka_rmsnorm_backward(const loka_rms_desc* desc, const void* dy_bf16
     }
     return rmsnorm_backward_launch(desc, dy_bf16, hq, hs, rstd, gamma_bf16, dh_bf16, dx_bf16, dgamma, workspace,
                                    static_cast<hipStream_t>(hip_stream));
+}
+
+// ---- a layer of experts
+static loka_status validate_route(const loka_route_desc* d) {
+    if (!d) return LOKA_ERR_NULL;
+    if (d->tokens <= 0 || d->tokens > (INT64_C(1) << 25) || d->experts <= 0 || d->experts > 1024 || d->top_k <= 0 || d->top_k > 16 || d->top_k > d->experts ||
+        d->ld < d->experts || too_many(1, d->tokens, d->ld))
+        return LOKA_ERR_SHAPE;
+    return d->score == LOKA_SCORE_SOFTMAX || d->score == LOKA_SCORE_SIGMOID ? LOKA_OK : LOKA_ERR_UNSUPPORTED;
+}
+
+size_t loka_route_workspace(const loka_route_desc* desc) { return validate_route(desc) != LOKA_OK ? 0 : route_workspace_bytes(desc); }
+
+loka_status loka_route(const loka_route_desc* desc, const void* logits, int32_t* expert, float* weight, int32_t* slot, int32_t* row,
+                       int32_t* offsets, void* workspace, size_t ws_bytes, void* hip_stream) {
+    if (!desc || !logits || !expert || !weight || !slot || !row || !offsets) return LOKA_ERR_NULL;
+    const loka_status st = validate_route(desc);
+    if (st != LOKA_OK) return st;
+    if (!aligned_to(logits, desc->bf16 ? 2 : 4) || !aligned_to(expert, 4) || !aligned_to(weight, 4) || !aligned_to(slot, 4) || !aligned_to(row, 4) ||
+        !aligned_to(offsets, 4))
+        return LOKA_ERR_ALIGN;
+    const size_t need = route_workspace_bytes(desc);
+    if (need && (!workspace || ws_bytes < need)) return LOKA_ERR_WORKSPACE;
+    if (need && !aligned16(workspace)) return LOKA_ERR_ALIGN;
+    return route_launch(desc, logits, expert, weight, slot, row, offsets, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+loka_status loka_route_backward(const loka_route_desc* desc, const void* logits, const int32_t* expert, const float* dweight, void* dlogits,
+                                void* hip_stream) {
+    if (!desc || !logits || !expert || !dweight || !dlogits) return LOKA_ERR_NULL;
+    const loka_status st = validate_route(desc);
+    if (st != LOKA_OK) return st;
+    const uintptr_t size = desc->bf16 ? 2 : 4;
+    if (!aligned_to(logits, size) || !aligned_to(dlogits, size) || !aligned_to(expert, 4) || !aligned_to(dweight, 4)) return LOKA_ERR_ALIGN;
+    return route_backward_launch(desc, logits, expert, dweight, dlogits, static_cast<hipStream_t>(hip_stream));
+}
+
+constexpr int64_t kMostWidth = INT64_C(1) << 20;       // of a layer of experts, so that a tile's rows lie within 32-bit offsets
+constexpr int32_t kMostGroups = 1024;
+
+int64_t loka_grouped_blocks(int64_t rows, int64_t groups) {
+    if (rows <= 0 || rows > INT32_MAX || groups <= 0 || groups > kMostGroups) return -1;
+    return (rows + (kGroupBlock - 1) * std::min(rows, groups)) / kGroupBlock;
+}
+
+static loka_status grouped_quantize_checked(const loka_grouped_quantize_desc* d, const void* x, const int32_t* index, const int32_t* offsets, uint8_t* q,
+                                            float* scales, uint8_t* qt, float* st, void* hip_stream) {
+    if (d->rows <= 0 || d->rows > INT32_MAX || d->cols <= 0 || d->cols > kMostWidth || d->ld < d->cols || d->groups <= 0 || d->groups > kMostGroups) return LOKA_ERR_SHAPE;
+    if (index && (d->x_rows <= 0 || d->x_rows > INT32_MAX)) return LOKA_ERR_SHAPE;
+    if (too_many(1, d->rows, d->cols) || too_many(1, index ? d->x_rows : d->rows, d->ld)) return LOKA_ERR_SHAPE;
+    if (!offsets && d->rows % d->groups) return LOKA_ERR_SHAPE;
+    if (!aligned_to(x, 2) || !aligned_to(index, 4) || !aligned_to(offsets, 4) || !aligned16(q) || !aligned16(qt) || !aligned_to(scales, 4) || !aligned_to(st, 4))
+        return LOKA_ERR_ALIGN;
+    return grouped_quantize_launch(d, x, index, offsets, q, scales, qt, st, static_cast<hipStream_t>(hip_stream));
+}
+
+loka_status loka_grouped_quantize(const loka_grouped_quantize_desc* desc, const void* x_bf16, const int32_t* index, const int32_t* offsets,
+                                  uint8_t* q, float* scales, uint8_t* qt, float* st, void* hip_stream) {
+    if (!desc || !x_bf16 || (q != nullptr) != (scales != nullptr) || (qt != nullptr) != (st != nullptr) || (!q && !qt)) return LOKA_ERR_NULL;
+    return grouped_quantize_checked(desc, x_bf16, index, offsets, q, scales, qt, st, hip_stream);
+}
+
+static loka_status validate_grouped(const loka_grouped_desc* d, bool gathered) {
+    if (!d) return LOKA_ERR_NULL;
+    if (d->rows <= 0 || d->rows > INT32_MAX || d->N <= 0 || d->N > kMostWidth || d->K <= 0 || d->K > kMostWidth || d->groups <= 0 || d->groups > kMostGroups)
+        return LOKA_ERR_SHAPE;
+    if (gathered && (d->x_rows <= 0 || d->x_rows > INT32_MAX)) return LOKA_ERR_SHAPE;
+    return LOKA_OK;
+}
+static loka_status validate_grouped_gemm(const loka_grouped_desc* d, bool gathered) {
+    const loka_status st = validate_grouped(d, gathered);
+    if (st != LOKA_OK) return st;
+    if (!grouped_gemm_fits(d)) return LOKA_ERR_SHAPE;
+    return d->w_form == LOKA_W_TURNED || d->w_form == LOKA_W_ALONG ? LOKA_OK : LOKA_ERR_UNSUPPORTED;
+}
+
+loka_status loka_grouped_gemm(const loka_grouped_desc* desc, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
+                              const uint8_t* wq, const float* sw, void* out_bf16, float* y_fp32, void* hip_stream) {
+    if (!desc || !xq || !sx || !offsets || !wq || !sw || (!out_bf16 && !y_fp32)) return LOKA_ERR_NULL;
+    const loka_status st = validate_grouped_gemm(desc, index != nullptr);
+    if (st != LOKA_OK) return st;
+    if (!aligned16(xq) || !aligned_to(sx, 4) || !aligned_to(index, 4) || !aligned_to(offsets, 4) || !aligned16(wq) || !aligned_to(sw, 4) ||
+        !aligned16(out_bf16) || !aligned16(y_fp32))
+        return LOKA_ERR_ALIGN;
+    return grouped_gemm_launch(desc, xq, sx, index, offsets, wq, sw, out_bf16, y_fp32, static_cast<hipStream_t>(hip_stream));
+}
+
+// The workspace of the layer: codes of x, then their scales.
+size_t loka_grouped_linear_workspace(const loka_grouped_desc* desc, int with_index) {
+    if (validate_grouped_gemm(desc, with_index != 0) != LOKA_OK) return 0;
+    const size_t n = static_cast<size_t>(with_index ? desc->x_rows : desc->rows) * static_cast<size_t>(group_blocks(desc->K));
+    return n * kGroupBlock + (n * 4 + 15) / 16 * 16;
+}
+
+loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf16, int64_t ld, const int32_t* index, const int32_t* offsets,
+                                const uint8_t* wq, const float* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
+                                void* hip_stream) {
+    if (!desc || !x_bf16 || !offsets || !wq || !sw || (!out_bf16 && !y_fp32)) return LOKA_ERR_NULL;
+    const loka_status st = validate_grouped_gemm(desc, index != nullptr);
+    if (st != LOKA_OK) return st;
+    if (ld < desc->K) return LOKA_ERR_SHAPE;
+    if (!aligned_to(x_bf16, 2) || !aligned_to(index, 4) || !aligned_to(offsets, 4) || !aligned16(wq) || !aligned_to(sw, 4) || !aligned16(out_bf16) ||
+        !aligned16(y_fp32))
+        return LOKA_ERR_ALIGN;
+    const size_t need = loka_grouped_linear_workspace(desc, index != nullptr);
+    if (need && (!workspace || ws_bytes < need)) return LOKA_ERR_WORKSPACE;
+    if (need && !aligned16(workspace)) return LOKA_ERR_ALIGN;
+    const int64_t rows = index ? desc->x_rows : desc->rows;
+    uint8_t* const xq = static_cast<uint8_t*>(workspace);
+    float* const sx = reinterpret_cast<float*>(xq + static_cast<size_t>(rows) * static_cast<size_t>(group_blocks(desc->K)) * kGroupBlock);
+    const loka_grouped_quantize_desc qd{rows, desc->K, ld, rows, 1};
+    const loka_status sq = grouped_quantize_checked(&qd, x_bf16, nullptr, nullptr, xq, sx, nullptr, nullptr, hip_stream);
+    if (sq != LOKA_OK) return sq;
+    return grouped_gemm_launch(desc, xq, sx, index, offsets, wq, sw, out_bf16, y_fp32, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t loka_grouped_wgrad_workspace(const loka_grouped_desc* desc) {
+    return validate_grouped(desc, false) != LOKA_OK || !grouped_wgrad_fits(desc) ? 0 : grouped_wgrad_workspace_bytes(desc);
+}
+
+loka_status loka_grouped_wgrad(const loka_grouped_desc* desc, const uint8_t* xt, const float* sxt, const uint8_t* dyt, const float* sdyt,
+                               const int32_t* offsets, void* dw_bf16, float* dw_fp32, void* workspace, size_t ws_bytes, void* hip_stream) {
+    if (!desc || !xt || !sxt || !dyt || !sdyt || !offsets || (!dw_bf16 && !dw_fp32)) return LOKA_ERR_NULL;
+    const loka_status st = validate_grouped(desc, false);
+    if (st != LOKA_OK) return st;
+    if (!grouped_wgrad_fits(desc)) return LOKA_ERR_SHAPE;
+    if (!aligned16(xt) || !aligned_to(sxt, 4) || !aligned16(dyt) || !aligned_to(sdyt, 4) || !aligned_to(offsets, 4) || !aligned16(dw_bf16) || !aligned16(dw_fp32))
+        return LOKA_ERR_ALIGN;
+    const size_t need = grouped_wgrad_workspace_bytes(desc);
+    if (need && (!workspace || ws_bytes < need)) return LOKA_ERR_WORKSPACE;
+    if (need && !aligned16(workspace)) return LOKA_ERR_ALIGN;
+    return grouped_wgrad_launch(desc, xt, sxt, dyt, sdyt, offsets, dw_bf16, dw_fp32, workspace, ws_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+static loka_status validate_combine(const loka_combine_desc* d) {
+    if (!d) return LOKA_ERR_NULL;
+    if (d->tokens <= 0 || d->top_k <= 0 || d->top_k > 16 || d->tokens > (INT64_C(1) << 30) / d->top_k || d->cols <= 0 || d->cols > kMostWidth || d->rows <= 0 ||
+        d->rows > INT32_MAX || too_many(1, d->rows, d->cols) || too_many(1, d->tokens, d->cols))
+        return LOKA_ERR_SHAPE;
+    return LOKA_OK;
+}
+
+loka_status loka_combine(const loka_combine_desc* desc, const void* y_bf16, const int32_t* slot, const float* weight,
+                         const void* residual_bf16, void* out_bf16, void* hip_stream) {
+    if (!desc || !y_bf16 || !slot || !out_bf16) return LOKA_ERR_NULL;
+    const loka_status st = validate_combine(desc);
+    if (st != LOKA_OK) return st;
+    if (!aligned16(y_bf16) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned16(residual_bf16) || !aligned16(out_bf16)) return LOKA_ERR_ALIGN;
+    return combine_launch(desc, y_bf16, slot, weight, residual_bf16, out_bf16, static_cast<hipStream_t>(hip_stream));
+}
+
+loka_status loka_combine_backward(const loka_combine_desc* desc, const void* dout_bf16, const void* y_bf16, const int32_t* slot,
+                                  const float* weight, void* dy_bf16, float* dweight, void* hip_stream) {
+    if (!desc || !dout_bf16 || !slot || (!dy_bf16 && !dweight) || (dweight && !y_bf16)) return LOKA_ERR_NULL;
+    const loka_status st = validate_combine(desc);
+    if (st != LOKA_OK) return st;
+    if (!aligned16(dout_bf16) || !aligned16(y_bf16) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned16(dy_bf16) || !aligned_to(dweight, 4))
+        return LOKA_ERR_ALIGN;
+    return combine_backward_launch(desc, dout_bf16, y_bf16, slot, weight, dy_bf16, dweight, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

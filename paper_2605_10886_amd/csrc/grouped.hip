@@ -1,0 +1,202 @@
+// 8-bit operands of grouped products in their two stored forms (include/loka.h, loka_grouped_quantize).  Bytes only: 2 read and
+// 1 + 1/32 written per element and form.
+#include "experts.h"
+
+namespace loka {
+
+struct GqArgs {
+    const uint16_t* x;
+    const int32_t *index, *offsets;
+    uint8_t *q, *qt;
+    float *scales, *st;
+    int64_t rows, cols, ld, x_rows, first_wg;
+    int64_t per_group, blocks_per_group;           // offsets == nullptr
+    int groups, col_tiles;
+};
+
+// Scale and factor of a group of 128 from the bits of its largest magnitude (a bf16's): NaN, and a factor that is not used, where it is not finite
+__device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale, float& inv) {
+    group_scale_pow2(bf16_bits_to_f32(amax), scale, inv);
+    if (amax < 0x7F80u) return true;
+    scale = __uint_as_float(0x7FC00000u);
+    return false;
+}
+__device__ __forceinline__ uint32_t max_abs8(u32x4 v) {
+    uint32_t a = max_abs_bf16x2(v.x & 0x7FFF7FFFu, v.y);
+    a = max_abs_bf16x2(max_abs_bf16x2(a, v.z), v.w);
+    return max_of_halves(a);
+}
+__device__ __forceinline__ u32x2 gq_codes8(u32x4 v, float inv, bool finite) {
+    const u32x2 c{e4m3x4_finite(bf16_lo(v.x) * inv, bf16_hi(v.x) * inv, bf16_lo(v.y) * inv, bf16_hi(v.y) * inv),
+                  e4m3x4_finite(bf16_lo(v.z) * inv, bf16_hi(v.z) * inv, bf16_lo(v.w) * inv, bf16_hi(v.w) * inv)};
+    return finite ? c : u32x2{0u, 0u};
+}
+// the source row of row p, or -1: a row of zeros
+__device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
+    if (!a.index) return p;
+    const int64_t s = a.index[p];
+    return s >= 0 && s < a.x_rows ? s : -1;
+}
+
+// ALONG: 16 lanes take 128 elements of a row, 8 each.
+template <int U>
+__global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
+    const int t = static_cast<int>(threadIdx.x), l = t & 15;
+    const int64_t nb = (a.cols + kGroupBlock - 1) / kGroupBlock;
+    int64_t rows = a.rows;
+    if (a.offsets) {
+        const int last = a.offsets[a.groups];
+        rows = last < 0 ? 0 : last < rows ? last : rows;
+    }
+    const int64_t total = rows * nb, first = (a.first_wg + blockIdx.x) * (16 * U) + (t >> 4);
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t unit = first + u * 16, row = unit / nb, c = (unit - row * nb) * kGroupBlock + l * 8;
+        v[u] = u32x4{0u, 0u, 0u, 0u};
+        if (unit < total) {
+            const int64_t s = gq_source(a, row);
+            if (s >= 0) v[u] = mx_load8(a.x + s * a.ld, c, a.cols);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t unit = first + u * 16;
+        float scale, inv;
+        const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[u])), scale, inv);
+        const u32x2 c = gq_codes8(v[u], inv, finite);
+        if (unit < total) {
+            *reinterpret_cast<u32x2*>(a.q + unit * kGroupBlock + l * 8) = c;
+            if (l == 0) a.scales[unit] = scale;
+        }
+    }
+}
+
+// TURNED, and ALONG from the same read: a workgroup takes a block of 128 rows of one group x 128 columns; a thread 8 rows x 8 columns.
+// Maxima down a column cross the wave by lane exchanges and the waves through LDS; the codes turn in LDS (runs of 8 rows of a
+// column, run r at place r ^ (column / 8)) and leave in whole lines.
+template <bool ALONG>
+__global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
+    __shared__ __align__(16) uint8_t codes[128 * 128];
+    __shared__ __align__(16) u32x4 maxima[4][16];
+    const int t = static_cast<int>(threadIdx.x), cg = t & 15, rg = t >> 4, wave = t >> 6;
+    const int64_t wg = a.first_wg + blockIdx.x, block = wg / a.col_tiles, ct = wg - block * a.col_tiles;
+    int64_t row0;
+    int count;
+    if (a.offsets) {
+        const UnitAt at = find_unit(a.offsets, a.groups, static_cast<int>(a.rows), kGroupBlock, static_cast<int>(block));
+        if (at.group < 0) return;
+        const int skip = (static_cast<int>(block) - at.before) * kGroupBlock;
+        row0 = at.first + skip;
+        count = at.count - skip;
+    } else {
+        const int64_t g = block / a.blocks_per_group, skip = (block - g * a.blocks_per_group) * kGroupBlock;
+        row0 = g * a.per_group + skip;
+        count = static_cast<int>(a.per_group - skip < kGroupBlock ? a.per_group - skip : kGroupBlock);
+    }
+    if (count > kGroupBlock) count = kGroupBlock;
+    const int64_t c = ct * 128 + cg * 8;
+    u32x4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = u32x4{0u, 0u, 0u, 0u};
+        const int r = rg * 8 + i;
+        if (r < count) {
+            const int64_t s = gq_source(a, row0 + r);
+            if (s >= 0) v[i] = mx_load8(a.x + s * a.ld, c, a.cols);
+        }
+    }
+    u32x4 m = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = max_abs_bf16x2(m[e], v[i][e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        m[e] = max_abs_bf16x2(m[e], __shfl_xor(m[e], 16, 64));
+        m[e] = max_abs_bf16x2(m[e], __shfl_xor(m[e], 32, 64));
+    }
+    if ((t & 63) < 16) maxima[wave][cg] = m;
+    if (ALONG) {
+        const int64_t kb = (a.cols + kGroupBlock - 1) / kGroupBlock;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float scale, inv;
+            const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[i])), scale, inv);
+            const int r = rg * 8 + i;
+            if (r < count) {
+                const int64_t unit = (row0 + r) * kb + ct;
+                *reinterpret_cast<u32x2*>(a.q + unit * kGroupBlock + cg * 8) = gq_codes8(v[i], inv, finite);
+                if (cg == 0) a.scales[unit] = scale;
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const u32x4 o = maxima[w][cg];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = max_abs_bf16x2(m[e], o[e]);
+    }
+    float scale[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        float inv;
+        const bool finite = gq_scale((k & 1) ? m[k >> 1] >> 16 : m[k >> 1] & 0xFFFFu, scale[k], inv);
+        auto val = [&](int i) __attribute__((always_inline)) { return ((k & 1) ? bf16_hi(v[i][k >> 1]) : bf16_lo(v[i][k >> 1])) * inv; };
+        const u32x2 o{e4m3x4_finite(val(0), val(1), val(2), val(3)), e4m3x4_finite(val(4), val(5), val(6), val(7))};
+        *reinterpret_cast<u32x2*>(codes + (cg * 8 + k) * 128 + ((rg ^ cg) * 8)) = finite ? o : u32x2{0u, 0u};
+    }
+    if (rg == 0) {
+        float* const st = a.st + block * a.cols + c;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (c + k < a.cols) st[k] = scale[k];
+    }
+    __syncthreads();
+    uint8_t* const out = a.qt + (block * a.cols + ct * 128) * 128;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int i = t + k * 256, col = i >> 3, p = i & 7, g = col >> 3;
+        if (ct * 128 + col < a.cols) {
+            const u32x2 lo = *reinterpret_cast<const u32x2*>(codes + col * 128 + ((2 * p) ^ g) * 8);
+            const u32x2 hi = *reinterpret_cast<const u32x2*>(codes + col * 128 + ((2 * p + 1) ^ g) * 8);
+            *reinterpret_cast<u32x4*>(out + col * 128 + p * 16) = u32x4{lo.x, lo.y, hi.x, hi.y};
+        }
+    }
+}
+
+loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const void* x, const int32_t* index, const int32_t* offsets, uint8_t* q,
+                                    float* scales, uint8_t* qt, float* st, hipStream_t stream) {
+    GqArgs a{};
+    a.x = static_cast<const uint16_t*>(x);
+    a.index = index;
+    a.offsets = offsets;
+    a.q = q;
+    a.scales = scales;
+    a.qt = qt;
+    a.st = st;
+    a.rows = d->rows;
+    a.cols = d->cols;
+    a.ld = d->ld;
+    a.x_rows = d->x_rows;
+    a.groups = d->groups;
+    a.col_tiles = static_cast<int>(group_blocks(d->cols));
+    a.per_group = d->rows / d->groups;
+    a.blocks_per_group = group_blocks(a.per_group);
+    if (!qt) {
+        constexpr int U = 4;
+        return in_launches((d->rows * a.col_tiles + 16 * U - 1) / (16 * U), 256, [&](int64_t from, uint32_t grid) {
+            a.first_wg = from;
+            gq_along_kernel<U><<<grid, 256, 0, stream>>>(a);
+        });
+    }
+    const int64_t blocks = offsets ? loka_grouped_blocks(d->rows, d->groups) : a.blocks_per_group * d->groups;
+    return in_launches(blocks * a.col_tiles, 256, [&](int64_t from, uint32_t grid) {
+        a.first_wg = from;
+        if (q) gq_turned_kernel<true><<<grid, 256, 0, stream>>>(a);
+        else gq_turned_kernel<false><<<grid, 256, 0, stream>>>(a);
+    });
+}
+
+}  // namespace loka

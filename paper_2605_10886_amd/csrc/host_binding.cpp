@@ -562,6 +562,315 @@ PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- a layer of experts
+template <class D>
+D bytes_of(PyObject* o, const char* what) {      // a ctypes structure: its bytes are the descriptor
+    Py_buffer b;
+    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+        PyErr_Clear();
+        throw std::invalid_argument(what);
+    }
+    D d;
+    const bool ok = b.len == static_cast<Py_ssize_t>(sizeof(d));
+    if (ok) memcpy(&d, b.buf, sizeof(d));
+    PyBuffer_Release(&b);
+    if (!ok) throw std::invalid_argument(what);
+    return d;
+}
+bool is_int32(const at::Tensor& t, int64_t n) { return holds(t, at::kInt, n) && t.numel() == n; }
+bool is_matrix(const at::Tensor& t, at::ScalarType type, int64_t rows, int64_t cols) {
+    return t.scalar_type() == type && t.is_contiguous() && t.dim() == 2 && t.size(0) == rows && t.size(1) == cols;
+}
+// the routing problem that the logits and the options describe; false with an exception set
+bool route_desc(const at::Tensor& logits, PyObject* const* a, loka_route_desc& d) {      // a: top_k, score, renorm, scale
+    const long k = PyLong_AsLong(a[0]), score = PyLong_AsLong(a[1]);
+    const int renorm = PyObject_IsTrue(a[2]);
+    const double scale = PyFloat_AsDouble(a[3]);
+    if (PyErr_Occurred()) return false;
+    const bool bf16 = logits.scalar_type() == at::kBFloat16;
+    if ((!bf16 && logits.scalar_type() != at::kFloat) || logits.dim() != 2 || (logits.size(1) > 1 && logits.stride(1) != 1)) {
+        refuse("logits: bf16 or fp32 [tokens, experts] with contiguous rows");
+        return false;
+    }
+    if (logits.size(0) <= 0 || logits.size(1) <= 0 || logits.size(1) > 1024 || k <= 0 || k > 16) {
+        fail(LOKA_ERR_SHAPE, "loka_route");
+        return false;
+    }
+    d = loka_route_desc{logits.size(0), logits.size(0) > 1 ? logits.stride(0) : logits.size(1), static_cast<int32_t>(logits.size(1)), static_cast<int32_t>(k),
+                        static_cast<int32_t>(score), renorm, bf16, static_cast<float>(scale)};
+    return true;
+}
+
+// route(logits, top_k, score, renorm, scale, workspace) -> (expert, weight, slot, row, offsets)
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 6)) return nullptr;
+    const at::Tensor& logits = tensor(a[0]);
+    loka_route_desc d;
+    if (!route_desc(logits, a + 1, d)) return nullptr;
+    const at::Device dev = logits.device();
+    at::Tensor ws = given(a[5]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
+    if (!on_gpu(dev, {&ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor expert = empty({d.tokens, d.top_k}, at::kInt, dev), weight = empty({d.tokens, d.top_k}, at::kFloat, dev), slot = empty({d.tokens, d.top_k}, at::kInt, dev),
+               row = empty({d.tokens * d.top_k}, at::kInt, dev), offsets = empty({d.experts + 1}, at::kInt, dev);
+    if (!ws.defined()) ws = scratch(loka_route_workspace(&d), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_route(&d, ptr(logits), static_cast<int32_t*>(ptr(expert)), static_cast<float*>(ptr(weight)), static_cast<int32_t*>(ptr(slot)),
+                          static_cast<int32_t*>(ptr(row)), static_cast<int32_t*>(ptr(offsets)), at_or_null<void>(ws), ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_route");
+    return pack({expert, weight, slot, row, offsets});
+    END_HANDLE_TH_ERRORS
+}
+
+// route_backward(logits, expert, dweight, score, renorm, scale, dlogits) -> dlogits
+PyObject* route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 7)) return nullptr;
+    const at::Tensor &logits = tensor(a[0]), &expert = tensor(a[1]), &dweight = tensor(a[2]);
+    if (expert.dim() != 2) return refuse("expert: contiguous int32 [tokens, top_k]");
+    PyObject* const k = PyLong_FromLongLong(expert.size(1));
+    if (!k) return nullptr;
+    PyObject* const options[4] = {k, a[3], a[4], a[5]};
+    loka_route_desc d;
+    const bool ok = route_desc(logits, options, d);
+    Py_DECREF(k);
+    if (!ok) return nullptr;
+    if (!is_matrix(expert, at::kInt, d.tokens, d.top_k) || !is_matrix(dweight, at::kFloat, d.tokens, d.top_k))
+        return refuse("expert, dweight: contiguous int32 and fp32 [tokens, top_k]");
+    const at::Device dev = logits.device();
+    at::Tensor dl = given(a[6]);
+    if (!on_gpu(dev, {&expert, &dweight, &dl})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (!dl.defined()) dl = empty({d.tokens, d.experts}, logits.scalar_type(), dev);
+    else if (!is_matrix(dl, logits.scalar_type(), d.tokens, d.experts)) return refuse("dlogits: contiguous [tokens, experts] of the logits' type");
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_route_backward(&d, ptr(logits), static_cast<int32_t*>(ptr(expert)), static_cast<float*>(ptr(dweight)), ptr(dl), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_route_backward");
+    return wrap(dl);
+    END_HANDLE_TH_ERRORS
+}
+
+// grouped_quantize(x, groups, offsets, index, along, turned, q, scales, qt, st) -> (q, scales, qt, st)
+PyObject* grouped_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 10)) return nullptr;
+    const at::Tensor& x = tensor(a[0]);
+    const long long groups = PyLong_AsLongLong(a[1]);
+    const at::Tensor offsets = given(a[2]), index = given(a[3]);
+    const int along = PyObject_IsTrue(a[4]), turned = PyObject_IsTrue(a[5]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!is_rows(x)) return refuse("x: bf16 [rows, cols] with contiguous rows");
+    if (offsets.defined() && !(holds(offsets, at::kInt, 2) && offsets.dim() == 1)) return refuse("offsets: contiguous int32 [groups + 1]");
+    if (index.defined() && !(holds(index, at::kInt, 0) && index.dim() == 1)) return refuse("index: contiguous int32 [rows]");
+    if (!along && !turned) return refuse("one of the two forms at least");
+    const int64_t g = offsets.defined() ? offsets.numel() - 1 : groups;
+    loka_grouped_quantize_desc d{index.defined() ? index.numel() : x.size(0), x.size(1), row_stride(x), x.size(0), static_cast<int32_t>(g)};
+    if (g <= 0 || g > 1024 || d.rows <= 0 || d.rows >= kMost || x.size(0) <= 0 || d.cols <= 0 || d.cols >= kMost || (!offsets.defined() && d.rows % g)) return fail(LOKA_ERR_SHAPE, "loka_grouped_quantize");
+    const int64_t kb = (d.cols + 127) / 128, blocks = offsets.defined() ? loka_grouped_blocks(d.rows, g) : (d.rows / g + 127) / 128 * g;
+    const at::Device dev = x.device();
+    at::Tensor q = given(a[6]), s = given(a[7]), qt = given(a[8]), st = given(a[9]);
+    if (!on_gpu(dev, {&offsets, &index, &q, &s, &qt, &st})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (along) {
+        if (!q.defined()) q = empty({d.rows, kb * 128}, at::kByte, dev);
+        if (!s.defined()) s = empty({d.rows, kb}, at::kFloat, dev);
+        if (!holds(q, at::kByte, d.rows * kb * 128) || !holds(s, at::kFloat, d.rows * kb)) return refuse("q, scales: contiguous uint8 [rows, padded cols] and fp32 [rows, padded cols / 128]");
+    }
+    if (turned) {
+        if (!qt.defined()) qt = empty({blocks, d.cols, 128}, at::kByte, dev);
+        if (!st.defined()) st = empty({blocks, d.cols}, at::kFloat, dev);
+        if (!holds(qt, at::kByte, blocks * d.cols * 128) || !holds(st, at::kFloat, blocks * d.cols)) return refuse("qt, st: contiguous uint8 [blocks, cols, 128] and fp32 [blocks, cols]");
+    }
+    if (!along) q = s = at::Tensor();
+    if (!turned) qt = st = at::Tensor();
+    void* st_ = stream_of(dev);
+    const loka_status status = unlocked([&] {
+        return loka_grouped_quantize(&d, ptr(x), at_or_null<int32_t>(index), at_or_null<int32_t>(offsets), at_or_null<uint8_t>(q), at_or_null<float>(s),
+                                     at_or_null<uint8_t>(qt), at_or_null<float>(st), st_);
+    });
+    if (status != LOKA_OK) return fail(status, "loka_grouped_quantize");
+    return pack({q, s, qt, st});
+    END_HANDLE_TH_ERRORS
+}
+
+// sizes of a grouped product within what the library takes, so that they can be multiplied
+bool grouped_ok(const loka_grouped_desc& d) {
+    constexpr int64_t width = INT64_C(1) << 20;
+    return d.rows > 0 && d.rows < kMost && d.N > 0 && d.N <= width && d.K > 0 && d.K <= width && d.groups > 0 && d.groups <= 1024;
+}
+bool is_weights(const at::Tensor& q, const at::Tensor& s, const loka_grouped_desc& d) {
+    const int64_t n = d.groups * ((d.K + 127) / 128) * d.N;
+    return holds(q, at::kByte, n * 128) && q.numel() == n * 128 && holds(s, at::kFloat, n) && s.numel() == n;
+}
+
+// grouped_gemm(desc, xq, sx, wq, sw, offsets, index, want_out, want_y, out, y) -> (out or None, y or None)
+PyObject* grouped_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 11)) return nullptr;
+    loka_grouped_desc d = bytes_of<loka_grouped_desc>(a[0], "expected a GroupedDesc");
+    const at::Tensor &xq = tensor(a[1]), &sx = tensor(a[2]), &wq = tensor(a[3]), &sw = tensor(a[4]), &offsets = tensor(a[5]);
+    const at::Tensor index = given(a[6]);
+    if (!grouped_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_grouped_gemm");
+    const int64_t kb = (d.K + 127) / 128;
+    if (!(holds(xq, at::kByte, 1) && xq.dim() == 2 && xq.size(1) == kb * 128) || !holds(sx, at::kFloat, xq.size(0) * kb) || (!index.defined() && xq.size(0) < d.rows))
+        return refuse("xq, sx: contiguous uint8 [rows, padded K] and fp32 [rows, padded K / 128]");
+    if (!is_weights(wq, sw, d)) return refuse("wq, sw: stored weights of every group, contiguous uint8 and fp32");
+    if (!is_int32(offsets, d.groups + 1) || (index.defined() && !is_int32(index, d.rows))) return refuse("offsets, index: contiguous int32 [groups + 1] and [rows]");
+    d.x_rows = xq.size(0);
+    const at::Device dev = xq.device();
+    if (!on_gpu(dev, {&sx, &wq, &sw, &offsets, &index})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor out, y;
+    if (!product_outputs(a[7], a[8], a[9], a[10], d.rows * d.N, d.rows, d.N, dev, out, y)) return nullptr;
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_grouped_gemm(&d, static_cast<uint8_t*>(ptr(xq)), static_cast<float*>(ptr(sx)), at_or_null<int32_t>(index), static_cast<int32_t*>(ptr(offsets)),
+                                 static_cast<uint8_t*>(ptr(wq)), static_cast<float*>(ptr(sw)), at_or_null<void>(out), at_or_null<float>(y), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_grouped_gemm");
+    return pack({out, y});
+    END_HANDLE_TH_ERRORS
+}
+
+// grouped_linear(desc, x, wq, sw, offsets, index, want_out, want_y, out, y, workspace) -> (out or None, y or None)
+PyObject* grouped_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 11)) return nullptr;
+    loka_grouped_desc d = bytes_of<loka_grouped_desc>(a[0], "expected a GroupedDesc");
+    const at::Tensor &x = tensor(a[1]), &wq = tensor(a[2]), &sw = tensor(a[3]), &offsets = tensor(a[4]);
+    const at::Tensor index = given(a[5]);
+    if (!grouped_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_grouped_linear");
+    if (!is_rows(x) || x.size(1) != d.K || x.size(0) <= 0 || x.size(0) >= kMost || (!index.defined() && x.size(0) < d.rows)) return refuse("x: bf16 [tokens, K] with contiguous rows");
+    if (!is_weights(wq, sw, d)) return refuse("wq, sw: stored weights of every group, contiguous uint8 and fp32");
+    if (!is_int32(offsets, d.groups + 1) || (index.defined() && !is_int32(index, d.rows))) return refuse("offsets, index: contiguous int32 [groups + 1] and [rows]");
+    d.x_rows = x.size(0);
+    const at::Device dev = x.device();
+    at::Tensor ws = given(a[10]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
+    if (!on_gpu(dev, {&wq, &sw, &offsets, &index, &ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor out, y;
+    if (!product_outputs(a[6], a[7], a[8], a[9], d.rows * d.N, d.rows, d.N, dev, out, y)) return nullptr;
+    if (!ws.defined()) ws = scratch(loka_grouped_linear_workspace(&d, index.defined()), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_grouped_linear(&d, ptr(x), row_stride(x), at_or_null<int32_t>(index), static_cast<int32_t*>(ptr(offsets)), static_cast<uint8_t*>(ptr(wq)),
+                                   static_cast<float*>(ptr(sw)), at_or_null<void>(out), at_or_null<float>(y), at_or_null<void>(ws), ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_grouped_linear");
+    return pack({out, y});
+    END_HANDLE_TH_ERRORS
+}
+
+// grouped_wgrad(desc, xt, sxt, dyt, sdyt, offsets, want_out, want_y, out, y, workspace) -> (dw bf16 or None, dw fp32 or None)
+PyObject* grouped_wgrad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 11)) return nullptr;
+    const loka_grouped_desc d = bytes_of<loka_grouped_desc>(a[0], "expected a GroupedDesc");
+    const at::Tensor &xt = tensor(a[1]), &sxt = tensor(a[2]), &dyt = tensor(a[3]), &sdyt = tensor(a[4]), &offsets = tensor(a[5]);
+    if (!grouped_ok(d)) return fail(LOKA_ERR_SHAPE, "loka_grouped_wgrad");
+    const int64_t blocks = loka_grouped_blocks(d.rows, d.groups);
+    if (!holds(xt, at::kByte, blocks * d.K * 128) || !holds(sxt, at::kFloat, blocks * d.K) || !holds(dyt, at::kByte, blocks * d.N * 128) || !holds(sdyt, at::kFloat, blocks * d.N))
+        return refuse("xt, sxt, dyt, sdyt: turned forms of [rows, K] and [rows, N], contiguous uint8 and fp32");
+    if (!is_int32(offsets, d.groups + 1)) return refuse("offsets: contiguous int32 [groups + 1]");
+    const at::Device dev = xt.device();
+    at::Tensor ws = given(a[10]);
+    if (!is_run(ws)) return refuse("workspace: contiguous");
+    if (!on_gpu(dev, {&sxt, &dyt, &sdyt, &offsets, &ws})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    at::Tensor out, y;
+    if (!product_outputs(a[6], a[7], a[8], a[9], d.groups * d.K * d.N, d.groups * d.K, d.N, dev, out, y)) return nullptr;
+    if (a[8] == Py_None && out.defined()) out = out.view({d.groups, d.K, d.N});
+    if (a[9] == Py_None && y.defined()) y = y.view({d.groups, d.K, d.N});
+    if (!ws.defined()) ws = scratch(loka_grouped_wgrad_workspace(&d), dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_grouped_wgrad(&d, static_cast<uint8_t*>(ptr(xt)), static_cast<float*>(ptr(sxt)), static_cast<uint8_t*>(ptr(dyt)), static_cast<float*>(ptr(sdyt)),
+                                  static_cast<int32_t*>(ptr(offsets)), at_or_null<void>(out), at_or_null<float>(y), at_or_null<void>(ws), ws.defined() ? ws.nbytes() : 0, st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_grouped_wgrad");
+    return pack({out, y});
+    END_HANDLE_TH_ERRORS
+}
+
+// the slots [tokens, top_k], their weights, and y [rows, cols] or a matrix of the tokens; false with an exception set
+bool combine_desc(const at::Tensor& slot, const at::Tensor& weight, int64_t rows, int64_t cols, loka_combine_desc& d) {
+    if (!(slot.scalar_type() == at::kInt && slot.is_contiguous() && slot.dim() == 2) || (weight.defined() && !is_matrix(weight, at::kFloat, slot.size(0), slot.size(1)))) {
+        refuse("slot, weight: contiguous int32 and fp32 [tokens, top_k]");
+        return false;
+    }
+    if (slot.size(0) <= 0 || slot.size(1) <= 0 || slot.size(1) > 16 || rows <= 0 || cols <= 0) {
+        fail(LOKA_ERR_SHAPE, "loka_combine");
+        return false;
+    }
+    d = loka_combine_desc{slot.size(0), cols, rows, static_cast<int32_t>(slot.size(1))};
+    return true;
+}
+
+// combine(y, slot, weight, residual, out) -> out
+PyObject* combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 5)) return nullptr;
+    const at::Tensor &y = tensor(a[0]), &slot = tensor(a[1]);
+    const at::Tensor weight = given(a[2]), res = given(a[3]);
+    at::Tensor out = given(a[4]);
+    if (!(y.dim() == 2 && y.scalar_type() == at::kBFloat16 && y.is_contiguous())) return refuse("y: contiguous bf16 [rows, cols]");
+    loka_combine_desc d;
+    if (!combine_desc(slot, weight, y.size(0), y.size(1), d)) return nullptr;
+    if ((res.defined() && !is_matrix(res, at::kBFloat16, d.tokens, d.cols)) || (out.defined() && !is_matrix(out, at::kBFloat16, d.tokens, d.cols)))
+        return refuse("residual, out: contiguous bf16 [tokens, cols]");
+    const at::Device dev = y.device();
+    if (!on_gpu(dev, {&slot, &weight, &res, &out})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (!out.defined()) out = empty({d.tokens, d.cols}, at::kBFloat16, dev);
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_combine(&d, ptr(y), static_cast<int32_t*>(ptr(slot)), at_or_null<float>(weight), at_or_null<void>(res), ptr(out), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_combine");
+    return wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// combine_backward(dout, y, slot, weight, rows, want_dy, want_dweight, dy) -> (dy or None, dweight or None)
+PyObject* combine_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!need_args(n, 8)) return nullptr;
+    const at::Tensor &dout = tensor(a[0]), &slot = tensor(a[2]);
+    const at::Tensor y = given(a[1]), weight = given(a[3]);
+    const long long rows_of = PyLong_AsLongLong(a[4]);
+    const int want_dy = PyObject_IsTrue(a[5]), want_dweight = PyObject_IsTrue(a[6]);
+    if (PyErr_Occurred()) return nullptr;
+    at::Tensor dy = given(a[7]);
+    if (!(dout.dim() == 2 && dout.scalar_type() == at::kBFloat16 && dout.is_contiguous())) return refuse("dout: contiguous bf16 [tokens, cols]");
+    if (want_dweight && !y.defined()) return refuse("y: what dweight is taken from");
+    if (!want_dweight && !want_dy && !dy.defined()) return refuse("one of the two gradients at least");
+    const int64_t rows = y.defined() ? y.size(0) : dy.defined() ? dy.size(0) : rows_of;
+    loka_combine_desc d;
+    if (!combine_desc(slot, weight, rows, dout.size(1), d)) return nullptr;
+    if (dout.size(0) != d.tokens || (y.defined() && !is_matrix(y, at::kBFloat16, rows, d.cols)) || (dy.defined() && !is_matrix(dy, at::kBFloat16, rows, d.cols)))
+        return refuse("dout [tokens, cols], y and dy [rows, cols]: contiguous bf16");
+    const at::Device dev = dout.device();
+    if (!on_gpu(dev, {&y, &slot, &weight, &dy})) return refuse("tensors on one GPU");
+    const c10::DeviceGuard guard(dev);
+    if (!dy.defined() && want_dy) dy = empty({rows, d.cols}, at::kBFloat16, dev);
+    at::Tensor dw = want_dweight ? empty({d.tokens, d.top_k}, at::kFloat, dev) : at::Tensor();
+    void* st_ = stream_of(dev);
+    const loka_status st = unlocked([&] {
+        return loka_combine_backward(&d, ptr(dout), at_or_null<void>(y), static_cast<int32_t*>(ptr(slot)), at_or_null<float>(weight), at_or_null<void>(dy),
+                                     at_or_null<float>(dw), st_);
+    });
+    if (st != LOKA_OK) return fail(st, "loka_combine_backward");
+    return pack({dy, dw});
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XSETREF(g_error, cls);
@@ -573,7 +882,8 @@ PyMethodDef kMethods[] = {
     LOKA_FAST(quantize), LOKA_FAST(gemm_norm), LOKA_FAST(gemm_norm_fp8out), LOKA_FAST(linear_norm), LOKA_FAST(linear_norm_xq),
     LOKA_FAST(bf16_gemm), LOKA_FAST(probe_error), LOKA_FAST(tracker_update),
     LOKA_FAST(mxfp4_quantize), LOKA_FAST(mxfp4_dequantize), LOKA_FAST(mxfp4_gemm), LOKA_FAST(mxfp4_linear), LOKA_FAST(add_rmsnorm),
-    LOKA_FAST(rmsnorm_backward),
+    LOKA_FAST(rmsnorm_backward), LOKA_FAST(route), LOKA_FAST(route_backward), LOKA_FAST(grouped_quantize), LOKA_FAST(grouped_gemm),
+    LOKA_FAST(grouped_linear), LOKA_FAST(grouped_wgrad), LOKA_FAST(combine), LOKA_FAST(combine_backward),
     {"set_error", &set_error, METH_O, "the exception class raised for a status other than LOKA_OK"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", "marshalling of the per-step calls", -1, kMethods, nullptr, nullptr, nullptr, nullptr};

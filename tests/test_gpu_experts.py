@@ -1,0 +1,514 @@
+"""A layer of experts (loka_route, loka_grouped_*, loka_combine) against plain 64-bit forms."""
+import math
+
+import pytest
+import torch
+
+import plain_experts as X
+import plain_ops as P
+from paper_2605_10886_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SCORES = {"softmax": B.SCORE_SOFTMAX, "sigmoid": B.SCORE_SIGMOID}
+BF = 2.0 ** -8          # half a step of bf16, relative
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _randn(*shape, seed):
+    return torch.randn(*shape, device=DEV, generator=_gen(seed))
+
+
+def _i32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+# ---------------------------------------------------------------- the choice
+
+def _check_route(logits, k, score, renorm, scale=1.0):
+    r = B.loka_route(logits, k, SCORES[score], renorm, scale)
+    e = X.choose(logits, k)
+    assert torch.equal(r.experts.long(), e)
+    slots, rows, offsets = X.order(e, logits.shape[1])
+    assert torch.equal(r.slots, slots) and torch.equal(r.rows, rows) and torch.equal(r.offsets, offsets)
+    w = X.weights(logits, e, score, renorm, scale)
+    assert torch.equal(torch.isnan(r.weights), torch.isnan(w))
+    # an exponential's argument is off by half a step of its size (at most `span` here), itself by 2 steps, its sums by half a step per
+    # addition (up to 16 in a lane, 6 exchanges), a quotient and the scale by half a step each, numerator and denominator alike
+    span = float(torch.where(logits.isfinite(), logits.double(), 0.0).abs().max())
+    tol = (2 * (2 * span + 4) + 24 + 6) * P.F32
+    err = (r.weights.double() - w).abs()
+    assert bool((torch.nan_to_num(err) <= tol * torch.nan_to_num(w).abs() + 2.0 ** -126).all()), float((err / w.abs()).nan_to_num().max())
+    return r
+
+
+@pytest.mark.parametrize("score,renorm", [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 64, 8), (3, 5, 5), (17, 16, 16), (64, 65, 3), (127, 128, 2), (128, 256, 8), (129, 257, 4), (300, 512, 6), (257, 1024, 16),
+                                   (1000, 60, 4), (40, 1000, 10)])
+def test_route(T, E, k, score, renorm):
+    _check_route(1.5 * _randn(T, E, seed=T + E), k, score, renorm, 2.5)
+    _check_route((1.5 * _randn(T, E, seed=T + E + 1)).bfloat16(), k, score, renorm)         # (with equal entries)
+
+
+def test_route_ties_masks_and_values_without_an_order():
+    inf, nan = math.inf, math.nan
+    x = torch.tensor([[1.0, 3.0, 3.0, 2.0, 3.0], [-inf, -inf, 0.0, -inf, -inf], [-inf] * 5, [0.0, -0.0, 0.0, -0.0, 0.0], [-3e38, 3e38, -inf, 1.0, -3.4e38],
+                      [-200.0, -201.0, -300.0, -inf, -202.0], [nan, inf, 1.0, -inf, 0.0], [inf, inf, 0.0, 0.0, 0.0], [2.0, nan, nan, inf, -inf]], device=DEV)
+    for score in SCORES:
+        for renorm in (True, False):
+            for k in (1, 3, 5):
+                r = B.loka_route(x, k, SCORES[score], renorm)
+                e = X.choose(x, k)
+                assert torch.equal(r.experts.long(), e), (score, renorm, k)
+                slots, rows, offsets = X.order(e, 5)
+                assert torch.equal(r.slots, slots) and torch.equal(r.rows, rows) and torch.equal(r.offsets, offsets)
+                w = X.weights(x, e, score, renorm)
+                for t in range(6):             # rows without a NaN or an infinity among the chosen (below 2^-126 fp32 has steps of 2^-149)
+                    assert bool(((r.weights[t].double() - w[t]).abs() <= 2.0 ** -13 * w[t] + 2.0 ** -126).all()), (t, score, renorm, k)
+                assert bool((r.weights[2] == 0).all()) and bool((r.weights[r.experts < 0] == 0).all())
+                assert bool(torch.isnan(r.weights[6, 0])) and bool(torch.isnan(r.weights[8, 0]))
+                if renorm or score == "softmax":
+                    assert bool(torch.isnan(r.weights[8][r.experts[8] >= 0]).all())
+
+
+def test_route_rows_apart_on_another_stream_and_every_call_alike():
+    wide = _randn(700, 96, seed=3)
+    x = wide[:, 5:77]
+    want = _check_route(x, 6, "softmax", True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = [B.loka_route(x, 6) for _ in range(3)]
+    s.synchronize()
+    for r in got:
+        assert all(torch.equal(a, b) for a, b in zip(r, want))
+
+
+def test_route_of_many_tokens():
+    T, E, k = 100003, 32, 4
+    x = _randn(T, E, seed=9).bfloat16()
+    r = B.loka_route(x, k)
+    v, i = torch.sort(x.float(), dim=1, descending=True, stable=True)
+    assert torch.equal(r.experts.long(), i[:, :k])
+    flat = i[:, :k].reshape(-1)
+    place = torch.sort(flat, stable=True).indices
+    assert torch.equal(r.rows.long(), place // k)
+    assert torch.equal(r.offsets[1:].long(), torch.stack([(flat <= e).sum() for e in range(E)]))
+    slots = torch.empty_like(place)
+    slots[place] = torch.arange(T * k, device=DEV)
+    assert torch.equal(r.slots.long(), slots.view(T, k))
+
+
+@pytest.mark.parametrize("score,renorm", [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)])
+@pytest.mark.parametrize("T,E,k,bf16", [(1, 64, 8, False), (3, 5, 5, False), (100, 16, 16, True), (65, 130, 3, True), (33, 256, 8, False), (17, 1000, 10, True), (5, 1, 1, False)])
+def test_route_backward(T, E, k, bf16, score, renorm):
+    x = 1.5 * _randn(T, E, seed=T * E)
+    x[torch.rand(T, E, device=DEV, generator=_gen(1)) < 0.2] = -math.inf
+    x[0] = -math.inf                    # a row that chooses nothing
+    if T > 1:
+        x[1, 0] = 0.5
+    x = x.bfloat16() if bf16 else x
+    e = X.choose(x, k)
+    g = _randn(T, k, seed=2)
+    g[e < 0] = math.nan                 # not read
+    got = B.loka_route_backward(x, e.int(), g, SCORES[score], renorm, 1.25)
+    leaf = x.double().cpu().requires_grad_(True)
+    w = X.weights(leaf, e.cpu(), score, renorm, 1.25)
+    live = (e >= 0).cpu()
+    loss = (w[live] * g.double().cpu()[live]).sum()
+    loss.backward()
+    want = torch.nan_to_num(leaf.grad)
+    assert got.dtype == x.dtype
+    # as the weights', and the terms of g (w - ...): at most 16 of them, up to `most` each
+    most = 1.25 * float(torch.nan_to_num(g).abs().max()) * 2
+    tol = (2 * (2 * 8 + 4) + 24 + 16 + 8) * P.F32 * most
+    err = (got.double().cpu() - want).abs() - (BF * want.abs() if bf16 else 0)
+    assert float(err.max()) <= tol
+    assert not bool(got[0].any())
+
+
+# ---------------------------------------------------------------- stored forms
+
+def _check_along(q, s, x):
+    c, f = X.along(x)
+    assert torch.equal(torch.nan_to_num(s.double(), nan=-1.0), torch.nan_to_num(f, nan=-1.0))
+    assert torch.equal(X.e4m3(q), c)
+
+
+SIZES = [(1, 1), (1, 130), (7, 128), (128, 64), (129, 257), (300, 1008), (1000, 40), (33, 4096)]
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_quantize_along(rows, cols):
+    x = _randn(rows, cols, seed=rows)
+    x[:, ::7] *= 300.0
+    x = x.bfloat16()
+    r = B.loka_grouped_quantize(x)
+    assert r.q.shape == (rows, -(-cols // 128) * 128) and r.qt is None and r.st is None
+    _check_along(r.q, r.scales, x)
+    if cols % 128 == 0:                 # what the block recipe writes
+        q, s = B.loka_quantize(x, B.SCALE_BLOCK_1x128_POW2)
+        assert torch.equal(q, r.q) and torch.equal(s.view_as(r.scales), r.scales)
+
+
+@pytest.mark.parametrize("cols", [1, 40, 128, 130, 1008])
+@pytest.mark.parametrize("sizes", [[1], [128], [129, 0, 1, 127], [0, 0, 300, 0], [5] * 70, [0] * 100 + [3] + [0] * 900 + [200]])
+def test_quantize_both_forms_of_gathered_rows(sizes, cols):
+    bounds = [0]
+    for n in sizes:
+        bounds.append(bounds[-1] + n)
+    rows = bounds[-1] + 37              # 37 of no group
+    wide = _randn(50, cols + 3, seed=cols).bfloat16()
+    x = wide[:, 1:1 + cols]             # rows that start anywhere
+    index = torch.randint(0, 50, (rows,), device=DEV, generator=_gen(len(sizes))).int()
+    index[0] = -1                       # outside: zeros
+    index[-38] = 50
+    off = _i32(bounds)
+    blocks = B.loka_grouped_blocks(rows, len(sizes))
+    mark = 0xA5
+    q = torch.full((rows, -(-cols // 128) * 128), mark, dtype=torch.uint8, device=DEV)
+    s, qt, st = torch.full((rows, q.shape[1] // 128), -7.0, device=DEV), torch.full((blocks, cols, 128), mark, dtype=torch.uint8, device=DEV), torch.full((blocks, cols), -7.0, device=DEV)
+    r = B.loka_grouped_quantize(x, offsets=off, index=index, turned=True, q=q, scales=s, qt=qt, st=st)
+    assert r.q.data_ptr() == q.data_ptr() and r.st.data_ptr() == st.data_ptr()
+    src = index.long()
+    v = x[src.clamp(0, 49)].clone()
+    v[(src < 0) | (src >= 50)] = 0
+    n = bounds[-1]
+    _check_along(q[:n], s[:n], v[:n])
+    assert bool((q[n:] == mark).all()) and bool((s[n:] == -7).all())
+    c, f = X.turned(v, bounds)
+    assert torch.equal(X.e4m3(qt[:len(c)]), c) and torch.equal(st[:len(c)].double(), f)
+    assert bool((qt[len(c):] == mark).all()) and bool((st[len(c):] == -7).all())
+    only = B.loka_grouped_quantize(x, offsets=off, index=index, along=False, turned=True)
+    assert only.q is None and torch.equal(only.qt[:len(c)], qt[:len(c)]) and torch.equal(only.st[:len(c)], st[:len(c)])
+    alone = B.loka_grouped_quantize(x, offsets=off, index=index)
+    assert torch.equal(alone.q[:n], q[:n]) and torch.equal(alone.scales[:n], s[:n])
+
+
+@pytest.mark.parametrize("E,K,N", [(1, 64, 64), (3, 100, 72), (5, 128, 256), (2, 300, 1000)])
+def test_quantize_weights(E, K, N):
+    w = _randn(E * K, N, seed=E).bfloat16()
+    r = B.loka_grouped_quantize(w, groups=E, turned=True)
+    _check_along(r.q, r.scales, w)
+    c, f = X.turned(w, [e * K for e in range(E + 1)])
+    assert r.qt.shape == c.shape and torch.equal(X.e4m3(r.qt), c) and torch.equal(r.st.double(), f)
+
+
+def test_quantize_values_at_the_borders():
+    tiny, big = 2.0 ** -126, float(torch.finfo(torch.bfloat16).max)
+    x = torch.zeros(256, 128, device=DEV)
+    x[0, 3], x[1, 5], x[2, 7], x[3, 9] = math.nan, math.inf, -math.inf, big
+    x[4], x[5], x[6, 0], x[7, 0] = tiny, -tiny, 448.0, 450.0
+    x[8:] = _randn(248, 128, seed=1) * torch.exp2(torch.randint(-40, 40, (248, 1), device=DEV, generator=_gen(2)).float())
+    x[130, 20] = math.nan
+    x = x.bfloat16()
+    r = B.loka_grouped_quantize(x, groups=2, turned=True)
+    _check_along(r.q, r.scales, x)
+    c, f = X.turned(x, [0, 128, 256])
+    assert torch.equal(torch.nan_to_num(r.st.double(), nan=-1.0), torch.nan_to_num(f, nan=-1.0)) and torch.equal(X.e4m3(r.qt), c)
+    assert int(torch.isnan(r.scales).sum()) == 4 and int(torch.isnan(r.st).sum()) == 4
+
+
+# ---------------------------------------------------------------- products
+
+def _small(shape, seed):
+    """Small whole numbers: their codes are exact, and so is every product and sum."""
+    return torch.randint(-8, 9, shape, device=DEV, generator=_gen(seed)).float().bfloat16()
+
+
+def _bounds(sizes):
+    b = [0]
+    for n in sizes:
+        b.append(b[-1] + n)
+    return b
+
+
+def _plain_product(x, w, bounds, index=None):
+    y = torch.zeros(bounds[-1], w.shape[2], dtype=torch.float64, device=DEV)
+    for e, (a, b) in enumerate(zip(bounds[:-1], bounds[1:])):
+        if b > a:
+            y[a:b] = (x[a:b] if index is None else x[index[a:b].long()]).double() @ w[e].double()
+    return y
+
+
+def _bf16(v):
+    return v.float().bfloat16()
+
+
+GROUPS = [[1], [0, 1, 0], [16, 17], [3] * 8, [129, 0, 64, 1], [400, 0, 7], [256, 255, 257, 1, 0, 300], [1000, 24], [0] * 30 + [5] + [0] * 60 + [2]]
+
+
+@pytest.mark.parametrize("K,N", [(1, 1), (128, 16), (130, 7), (256, 128), (384, 200), (1008, 720), (640, 264)])
+@pytest.mark.parametrize("sizes", GROUPS)
+def test_products_are_exact_on_whole_numbers(sizes, K, N):
+    bounds = _bounds(sizes)
+    E, n = len(sizes), bounds[-1]
+    rows = n + 19                       # 19 of no group
+    x, w = _small((max(5, n // 2), K), n + K), _small((E, K, N), N)
+    index = torch.randint(0, x.shape[0], (rows,), device=DEV, generator=_gen(K)).int()
+    off = _i32(bounds)
+    want = _plain_product(x, w, bounds, index)
+    wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, along=False, turned=True)
+    turned, along = B.make_grouped_desc(rows, N, K, E), B.make_grouped_desc(rows, N, K, E, turned_w=False)
+    xq = B.loka_grouped_quantize(x)
+    out, y = torch.full((rows, N), -7.0, dtype=torch.bfloat16, device=DEV), torch.full((rows, N), -7.0, device=DEV)
+    B.loka_grouped_gemm(turned, xq.q, xq.scales, wq.qt, wq.st, off, index=index, out=out, y=y, want_y=True)
+    assert torch.equal(y[:n].double(), want) and torch.equal(out[:n], _bf16(want))
+    assert bool((out[n:] == -7).all()) and bool((y[n:] == -7).all())
+    # the other form of the weights, no index, one output at a time
+    wa = B.loka_grouped_quantize(w.transpose(1, 2).contiguous().view(E * N, K))
+    xg = B.loka_grouped_quantize(x[index.long()])
+    _, y2 = B.loka_grouped_gemm(along, xg.q, xg.scales, wa.q, wa.scales, off, want_out=False, want_y=True)
+    assert torch.equal(y2[:n].double(), want)
+    # from bf16
+    o3, _ = B.loka_grouped_linear(turned, x, wq.qt, wq.st, off, index=index)
+    assert torch.equal(o3[:n], out[:n])
+    o4, y4 = B.loka_grouped_linear(along, x[index.long()], wa.q, wa.scales, off, want_y=True)
+    assert torch.equal(o4[:n], out[:n]) and torch.equal(y4[:n], y[:n])
+
+
+@pytest.mark.parametrize("sizes,K,N", [([1], 4096, 256), ([5, 11, 16, 3], 1024, 512), ([40, 0, 90], 700, 300), ([600, 424], 1152, 512)])
+def test_products_of_random_numbers(sizes, K, N):
+    bounds = _bounds(sizes)
+    E, n = len(sizes), bounds[-1]
+    x, w = _randn(n, K, seed=K).bfloat16(), (_randn(E * K, N, seed=N) / math.sqrt(K)).bfloat16()
+    off = _i32(bounds)
+    wq = B.loka_grouped_quantize(w, groups=E, along=False, turned=True)
+    out, y = B.loka_grouped_linear(B.make_grouped_desc(n, N, K, E), x, wq.qt, wq.st, off, want_y=True)
+    xv = X.along_values(*X.along(x), K)
+    nb = -(-K // 128)
+    for e, (a, b) in enumerate(zip(bounds[:-1], bounds[1:])):
+        if b == a:
+            continue
+        wv = X.turned_values(X.e4m3(wq.qt[e * nb:(e + 1) * nb]), wq.st[e * nb:(e + 1) * nb], K)
+        want, tol = xv[a:b] @ wv, X.product_bound(xv[a:b], wv, K)
+        assert bool(((y[a:b].double() - want).abs() <= tol).all())
+        assert torch.equal(out[a:b], y[a:b].bfloat16())
+        assert float((y[a:b].double() - want).norm() / want.norm()) <= 2.0 ** -10      # (a bound on each leaves room for a wrong 128th)
+
+
+def test_operands_of_the_other_calls():
+    """Codes of loka_quantize and of the residual norm are operands where whole blocks divide K."""
+    n, K, N, E = 300, 512, 256, 3
+    off = _i32([0, 100, 101, 300])
+    x, w = _randn(n, K, seed=1).bfloat16(), (_randn(E * K, N, seed=2) / 20).bfloat16()
+    wq = B.loka_grouped_quantize(w, groups=E, along=False, turned=True)
+    d = B.make_grouped_desc(n, N, K, E)
+    want, _ = B.loka_grouped_linear(d, x, wq.qt, wq.st, off)
+    q, s = B.loka_quantize(x, B.SCALE_BLOCK_1x128_POW2)
+    got, _ = B.loka_grouped_gemm(d, q, s, wq.qt, wq.st, off)
+    assert torch.equal(got, want)
+    r = B.loka_add_rmsnorm(x, out=B.RMS_OUT_E4M3, out_mode=B.SCALE_BLOCK_1x128_POW2, want_rstd=True)
+    y, _ = B.loka_grouped_gemm(d, r.y, r.scales.view(n, -1), wq.qt, wq.st, off)
+    v = X.along_values(X.e4m3(r.y), r.scales.view(n, -1), K)
+    wv = X.turned_values(X.e4m3(wq.qt[:4]), wq.st[:4], K)
+    ref = v[:100] @ wv
+    assert bool(((y[:100].double() - ref).abs() <= X.product_bound(v[:100], wv, K) + BF * ref.abs()).all())
+
+
+def test_values_that_are_not_finite_stay_in_their_rows():
+    bounds, K, N = [0, 40, 40, 300], 300, 200
+    E, n = 3, 300
+    x, w = _small((n, K), 1), _small((E, K, N), 2)
+    wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, along=False, turned=True)
+    d, off = B.make_grouped_desc(n, N, K, E), _i32(bounds)
+    clean, _ = B.loka_grouped_linear(d, x, wq.qt, wq.st, off)
+    bad = x.clone()
+    bad[7, 5], bad[39, 299], bad[40, 130], bad[299, 0] = math.nan, math.inf, -math.inf, math.nan
+    got, _ = B.loka_grouped_linear(d, bad, wq.qt, wq.st, off)
+    rows = torch.zeros(n, dtype=torch.bool, device=DEV)
+    rows[[7, 39, 40, 299]] = True
+    assert bool(torch.isnan(got[rows]).all()) and torch.equal(got[~rows], clean[~rows])
+    dy = _small((n, N), 3)
+    bt, ct, yt = (B.loka_grouped_quantize(m, offsets=off, along=False, turned=True) for m in (bad, x, dy))
+    dw, _ = B.loka_grouped_wgrad(d, bt.qt, bt.st, yt.qt, yt.st, off)
+    ref, _ = B.loka_grouped_wgrad(d, ct.qt, ct.st, yt.qt, yt.st, off)
+    hit = torch.zeros(E, K, dtype=torch.bool, device=DEV)
+    hit[0, 5] = hit[0, 299] = hit[2, 130] = hit[2, 0] = True
+    assert bool(torch.isnan(dw[hit]).all()) and torch.equal(dw[~hit], ref[~hit])
+
+
+def test_indices_outside_are_read_as_the_nearest():
+    x, w = _small((6, 128), 1), _small((1, 128, 32), 2)
+    wq = B.loka_grouped_quantize(w.view(128, 32), along=False, turned=True)
+    for n in (9, 300):
+        index = torch.arange(-3, n - 3, device=DEV).int()
+        got, _ = B.loka_grouped_linear(B.make_grouped_desc(n, 32, 128, 1), x, wq.qt, wq.st, _i32([0, n]), index=index)
+        assert torch.equal(got, _bf16(x[index.long().clamp(0, 5)].double() @ w[0].double()))
+
+
+def test_offsets_out_of_range_reach_nothing_else():
+    """Offsets outside 0 .. rows are cut; whatever they hold, nothing but the rows is written."""
+    x, w = _small((50, 64), 1), _small((3, 64, 24), 2)
+    wq = B.loka_grouped_quantize(w.view(192, 24), groups=3, along=False, turned=True)
+    room = torch.full((70, 24), -7.0, dtype=torch.bfloat16, device=DEV)
+    out, d = room[10:60], B.make_grouped_desc(50, 24, 64, 3)
+    B.loka_grouped_linear(d, x, wq.qt, wq.st, _i32([-5, 20, 20, 1000]), out=out)
+    assert torch.equal(out[:20], _bf16(x[:20].double() @ w[0].double())) and torch.equal(out[20:], _bf16(x[20:].double() @ w[2].double()))
+    for off in ([-1 << 31, (1 << 31) - 1, -1 << 31, (1 << 31) - 1], [40, 10, 50, 3], [60, 70, 80, 90], [0, 50, 0, 50]):
+        B.loka_grouped_linear(d, x, wq.qt, wq.st, _i32(off), out=out)
+        r = B.loka_grouped_quantize(x, offsets=_i32(off), turned=True)
+        B.loka_grouped_wgrad(B.make_grouped_desc(50, 64, 64, 3), r.qt, r.st, r.qt, r.st, _i32(off))
+    assert bool((room[:10] == -7).all()) and bool((room[60:] == -7).all())
+
+
+@pytest.mark.parametrize("K,N", [(1, 1), (16, 130), (200, 7), (128, 128), (300, 520), (1008, 720)])
+@pytest.mark.parametrize("sizes", [[1], [0, 0], [128], [5, 0, 130, 256, 1], [700], [3] * 70, [1500, 600]])
+def test_weight_gradients_are_exact_on_whole_numbers(sizes, K, N):
+    bounds = _bounds(sizes)
+    E, n = len(sizes), bounds[-1]
+    rows = n + 9
+    x, dy = _small((rows, K), K), _small((rows, N), N + 1)
+    off = _i32(bounds)
+    xt, yt = (B.loka_grouped_quantize(m, offsets=off, along=False, turned=True) for m in (x, dy))
+    dw, dw32 = B.loka_grouped_wgrad(B.make_grouped_desc(rows, N, K, E), xt.qt, xt.st, yt.qt, yt.st, off, want_y=True)
+    assert dw.shape == dw32.shape == (E, K, N)
+    want = torch.stack([x[a:b].double().t().contiguous() @ dy[a:b].double() for a, b in zip(bounds[:-1], bounds[1:])])
+    assert torch.equal(dw32.double(), want) and torch.equal(dw, _bf16(want))
+
+
+# ---------------------------------------------------------------- sums
+
+@pytest.mark.parametrize("weighted,residual", [(True, True), (True, False), (False, False), (False, True)])
+@pytest.mark.parametrize("T,k,C", [(1, 1, 1), (1, 8, 4096), (5, 3, 7), (33, 16, 100), (300, 2, 1008), (130, 4, 512), (3, 2, 9000)])
+def test_combine(T, k, C, weighted, residual):
+    rows = T * k + 3
+    y = _randn(rows, C, seed=C).bfloat16()
+    slots = torch.randperm(rows, device=DEV, generator=_gen(T))[:T * k].view(T, k).int()
+    slots[T // 2, 0] = -1
+    slots[0, k - 1] = rows              # outside
+    live = (slots >= 0) & (slots < rows)
+    w = _randn(T, k, seed=2) if weighted else None
+    res = _randn(T, C, seed=3).bfloat16() if residual else None
+    plain = torch.where(live, slots, -1)
+    want = X.combine(y, plain, w, res)
+    got = B.loka_combine(y, slots, w, res)
+    size = X.combine(y.abs(), plain, None if w is None else w.abs(), None if res is None else res.abs())
+    tol = BF * want.abs() + (k + 1) * P.F32 * size * (1 + BF)
+    assert bool(((got.double() - want).abs() <= tol).all())
+    if residual:                        # over the residual
+        r = res.clone()
+        assert B.loka_combine(y, slots, w, r, out=r).data_ptr() == r.data_ptr() and torch.equal(r, got)
+    dout = _randn(T, C, seed=4).bfloat16()
+    dy = torch.full((rows, C), -7.0, dtype=torch.bfloat16, device=DEV)
+    _, dw = B.loka_combine_backward(dout, y, slots, w, dy=dy)
+    ey, ew = X.combine_backward(dout, y, plain, w, rows)
+    named = torch.zeros(rows, dtype=torch.bool, device=DEV)
+    named[slots[live].long()] = True
+    assert torch.equal(dy[named], _bf16(ey[named].float())) and bool((dy[~named] == -7).all())
+    _, size = X.combine_backward(dout.abs(), y.abs(), plain, w, rows)
+    assert bool(((dw.double() - ew).abs() <= (C / 256 + 8 + 8 + 2) * P.F32 * size).all()) and bool((dw[~live] == 0).all())
+    d1, none = B.loka_combine_backward(dout, None, slots, w, rows=rows, want_dweights=False)
+    assert none is None and torch.equal(d1[named], dy[named])
+    none, w1 = B.loka_combine_backward(dout, y, slots, w, want_dy=False)
+    assert none is None and torch.equal(w1, dw)
+
+
+# ---------------------------------------------------------------- as they are used
+
+def _layer(x, logits, w, wq, k):
+    r = B.loka_route(logits, k)
+    d = B.make_grouped_desc(r.rows.numel(), w.shape[2], w.shape[1], w.shape[0])
+    y, _ = B.loka_grouped_linear(d, x, wq.qt, wq.st, r.offsets, index=r.rows)
+    return r, d, y, B.loka_combine(y, r.slots, r.weights)
+
+
+def test_a_training_step_of_the_layer():
+    T, E, k, K, N = 333, 7, 3, 200, 136
+    x, dout = _randn(T, K, seed=1).bfloat16(), _randn(T, N, seed=2).bfloat16()
+    w = (_randn(E, K, N, seed=3) / math.sqrt(K)).bfloat16()
+    logits = _randn(T, E, seed=4)
+    logits[:, 5] = -math.inf            # an expert that nobody may take
+    wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, turned=True)
+    r, d, y, out = _layer(x, logits, w, wq, k)
+    dy, dweights = B.loka_combine_backward(dout, y, r.slots, r.weights)
+    dlogits = B.loka_route_backward(logits, r.experts, dweights)
+    xt = B.loka_grouped_quantize(x, offsets=r.offsets, index=r.rows, along=False, turned=True)
+    yq = B.loka_grouped_quantize(dy, offsets=r.offsets, turned=True)
+    dxr, _ = B.loka_grouped_gemm(B.make_grouped_desc(T * k, K, N, E, turned_w=False), yq.q, yq.scales, wq.q, wq.scales, r.offsets)
+    dx = B.loka_combine(dxr, r.slots)
+    dw, _ = B.loka_grouped_wgrad(d, xt.qt, xt.st, yq.qt, yq.st, r.offsets)
+    # the same without 8 bits, in fp64 on the CPU by autograd
+    xc, wc, lc = (t.double().cpu().requires_grad_(True) for t in (x, w, logits))
+    e = X.choose(logits, k).cpu()
+    a = X.weights(lc, e, "softmax", True)
+    ref = torch.zeros(T, N, dtype=torch.float64)
+    for j in range(k):
+        for n in range(E):
+            on = e[:, j] == n
+            if bool(on.any()):
+                ref = ref.index_add(0, on.nonzero().flatten(), a[on, j:j + 1] * (xc[on] @ wc[n]))
+    (ref * dout.double().cpu()).sum().backward()
+    # Codes are off by 2^-4 of their value at most, evenly: 2^-4 / sqrt 3 of its size or less in the norm, for each of a product's
+    # operands; dweights' product has y's error alone, which the softmax's gradient carries on
+    for name, got, want in (("out", out, ref), ("dx", dx, xc.grad), ("dw", dw, wc.grad), ("dlogits", dlogits, torch.nan_to_num(lc.grad))):
+        err = float((got.double().cpu() - want).norm() / want.norm())
+        assert err <= 2 * 2.0 ** -4 / math.sqrt(3), (name, err)
+    assert not bool(dw[5].any()) and not bool(dlogits[:, 5].any())
+
+
+def test_a_serving_step_in_a_graph():
+    """Captured once, replayed on other inputs, with eager work between; two graphs side by side."""
+    E, k, K, N = 16, 4, 512, 384
+    w = (_randn(E, K, N, seed=3) / 20).bfloat16()
+    wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, turned=True)
+    state = []
+    for T in (1, 200):
+        x, logits = torch.zeros(T, K, dtype=torch.bfloat16, device=DEV), torch.zeros(T, E, device=DEV)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            _layer(x, logits, w, wq, k)
+        torch.cuda.current_stream().wait_stream(s)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = _layer(x, logits, w, wq, k)[3]
+        state.append((T, x, logits, g, out))
+    for i in range(5):
+        for T, x, logits, g, out in state:
+            x.copy_(_randn(T, K, seed=10 * i + T).bfloat16())
+            logits.copy_(_randn(T, E, seed=10 * i + T + 1))
+            g.replay()
+        torch.cuda.synchronize()
+        for T, x, logits, g, out in state:
+            assert torch.equal(out, _layer(x, logits, w, wq, k)[3]), (i, T)
+
+
+def test_calls_on_two_streams_at_once():
+    E, k, K, N, T = 8, 2, 384, 256, 500
+    w = (_randn(E, K, N, seed=3) / 20).bfloat16()
+    wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, turned=True)
+    xs = [(_randn(T, K, seed=i).bfloat16(), _randn(T, E, seed=50 + i)) for i in range(2)]
+    want = [_layer(x, l, w, wq, k)[3] for x, l in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (x, l) in enumerate(xs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(_layer(x, l, w, wq, k)[3])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_operands_beyond_four_gigabytes():
+    """Codes of 1.1 million rows x 4096: rows on both sides of 2^32 bytes."""
+    T, K, N = (1 << 20) + 70000, 4096, 64
+    x = torch.zeros(T, K, dtype=torch.bfloat16, device=DEV)
+    at = [0, 5, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T - 1]
+    x[at] = _small((6, K), 1)
+    w = _small((2, K, N), 2)
+    wq = B.loka_grouped_quantize(w.view(2 * K, N), groups=2, along=False, turned=True)
+    index = _i32(at + at[::-1])
+    for reps in (1, 50):                # few rows, and many
+        ix = index.repeat(reps)
+        n = 12 * reps
+        got, _ = B.loka_grouped_linear(B.make_grouped_desc(n, N, K, 2), x, wq.qt, wq.st, _i32([0, n // 2, n]), index=ix)
+        v = x[ix.long()].double()
+        assert torch.equal(got, _bf16(torch.cat([v[:n // 2] @ w[0].double(), v[n // 2:] @ w[1].double()])))
+    del x
+    torch.cuda.empty_cache()
