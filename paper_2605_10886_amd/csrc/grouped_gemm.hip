@@ -16,7 +16,7 @@ struct GgArgs {
     uint16_t* out;
     float* y;
     int64_t N;
-    int rows, x_rows, groups, ksteps;  // ksteps: K in steps of 128
+    int rows, x_rows, groups, ksteps;  // x_rows: of the operand X; ksteps: K in steps of 128
     int M, blocks;                     // weight gradient: rows of a result; blocks of 128 rows that the operands have
     // element (row r, step k) of an operand lies r * row + k * step bytes from its start (scales: floats), a group's part of it `group` further on
     int64_t x_row, x_step, sx_row, sx_step, w_row, w_step, w_group, sw_row, sw_step, sw_group;
@@ -58,96 +58,166 @@ __device__ __forceinline__ void put8(float* row, int64_t n, int64_t N, const flo
 // Tiles in LDS.  A workgroup of WM x WN waves computes BM x BN values, each wave TM x TN tiles of 16 x 16, in steps of 128 along the
 // contraction: 128 bytes a row, two steps in LDS.  The 16-byte chunks of a row lie permuted so that the 16 rows of a read use all
 // banks: chunk c of X's row r at place c ^ (r / 2 % 8), of W's row r, whose reads take rows 8 apart, at c ^ (bits 1, 3 and 4 of r).
+//
+// A step is TM / 2 pairs of X's 16-row fragments against all of the wave's W fragments; a pair is read while the pair before it is
+// multiplied.  One barrier a step, in front of its last pair: by then the step's operands are in registers, so the loads of the
+// step after next may go where they lay, and the first pair and W's fragments of the next step are read between the matrix
+// instructions that follow.  Workgroups are persistent, and the stream of steps does not stop between result tiles: the next
+// tile's first steps arrive while this one's values are stored, and nothing waits for the stores where their number is known.
 template <int TM_, int TN_, int WM_, int WN_>
 struct GgTile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
     static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 4, STAGE = OFF_SW + BN * 4, LDS = 2 * STAGE;
-    static constexpr int LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64;
-    static constexpr int PER_CU = 163840 / LDS;
+    static constexpr int LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64, LOADS = LX + LW + 1;
+    static constexpr int PER_CU = 163840 / (LDS + 12288);   // (with the table of 1024 groups)
     static_assert(SROWS == NW && TM % 4 == 0 && TN % 2 == 0 && (NW == 4 || NW == 8));
 };
 
 template <class C, bool WGRAD>
 __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
-    constexpr int TM = C::TM, TN = C::TN;
+    constexpr int TM = C::TM, TN = C::TN, PAIRS = TM / 2, MM = 2 * TN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wm = wave / C::WN, wn = wave % C::WN;
 
-    // ---- which tile: rows m0 .. m0 + m_count - 1 of the result's rows, columns from n0 on, of `group`
-    int group, tm, tn, m_first, m_count, ksteps;
-    int64_t block0 = 0;                // weight gradient: the group's first block of 128 rows
-    if (WGRAD) {
-        const int per = a.tiles_m * a.tiles_n, t = xcd_contiguous(blockIdx.x, gridDim.x);
-        group = t / per;
-        banded_tile(t - group * per, a.tiles_m, a.tiles_n, tm, tn);
-        // (of groups that overlap: no more blocks than there are)
-        const int first = units_before(a.offsets, group, a.rows, kGroupBlock), own = (group_rows(a.offsets, group, a.rows).count + kGroupBlock - 1) / kGroupBlock;
-        block0 = first < 0 ? 0 : first < a.blocks ? first : a.blocks;
-        ksteps = a.blocks - static_cast<int>(block0) < own ? a.blocks - static_cast<int>(block0) : own;
-        m_first = tm * C::BM;
-        m_count = a.M - m_first < C::BM ? a.M - m_first : C::BM;
-    } else {
-        const int total = units_of_all(a.offsets, a.groups, a.rows, C::BM) * a.tiles_n;
-        if (static_cast<int>(blockIdx.x) >= total) return;
-        const int t = xcd_contiguous(blockIdx.x, total);
-        const UnitAt at = find_unit(a.offsets, a.groups, a.rows, C::BM, t / a.tiles_n);
-        if (at.group < 0) return;
-        group = at.group;
-        banded_tile(t - at.before * a.tiles_n, (at.count + C::BM - 1) / C::BM, a.tiles_n, tm, tn);
-        m_first = at.first + tm * C::BM;
-        m_count = at.count - tm * C::BM < C::BM ? at.count - tm * C::BM : C::BM;
-        ksteps = a.ksteps;
-    }
-    const int n0 = tn * C::BN, n_count = a.N - n0 < C::BN ? static_cast<int>(a.N - n0) : C::BN;
-
-    // ---- where the wave's loads find things: 8 rows of 128 bytes a load
-    // (rows past the end: X reads the last one, W zeros; what they give is not written)
-    auto x_source = [&](int row) __attribute__((always_inline)) {
-        int64_t s = m_first + (row < m_count ? row : m_count - 1);
-        if (!WGRAD && a.index) {
-            s = a.index[s];
-            s = s < 0 ? 0 : s >= a.x_rows ? a.x_rows - 1 : s;
+    // ---- the groups: cum[i] = units (tiles of BM rows; weight gradient: blocks of 128) of groups 0 .. i, and their rows
+    int* const cum = reinterpret_cast<int*>(smem + C::LDS);
+    int* const off = cum + a.groups;
+    {
+        int base = 0;
+        constexpr int UNIT = WGRAD ? kGroupBlock : C::BM;
+        for (int g0 = 0; g0 < a.groups; g0 += 64) {        // (every wave by itself, the same values)
+            const int i = g0 + lane;
+            const GroupRows q = i < a.groups ? group_rows(a.offsets, i, a.rows) : GroupRows{0, 0};
+            const int s = base + lanes_inclusive((q.count + UNIT - 1) / UNIT);
+            if (i < a.groups) {
+                cum[i] = s;
+                off[2 * i] = q.first;
+                off[2 * i + 1] = q.count;
+            }
+            base = __builtin_amdgcn_readlane(s, 63);
         }
-        return s;
-    };
-    const uint8_t* xp[C::LX];
-#pragma unroll
-    for (int i = 0; i < C::LX; ++i) {
-        const int row = (i * C::NW + wave) * 8 + (lane >> 3), chunk = (lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2));
-        xp[i] = a.xq + block0 * a.x_step + x_source(row) * a.x_row + chunk * 16;
+        __syncthreads();
     }
-    const int w_chunk = (lane & 7) ^ ((lane >> 4) & 1) ^ ((wave & 3) << 1);
-    const int w_lane = (lane >> 3) * static_cast<int>(a.w_row) + w_chunk * 16;
-    const uint8_t* wp = a.wq + (WGRAD ? block0 * a.w_step : group * a.w_group) + static_cast<int64_t>(n0) * a.w_row;
-    const int w_bytes = (n_count - 1) * static_cast<int>(a.w_row) + 128;
-    // scales: 64 rows a load, those of X by the first waves
-    const bool scales_of_x = wave < C::BM / 64;
-    const float* sxp = a.sx + block0 * a.sx_step + x_source(scales_of_x ? wave * 64 + lane : 0) * a.sx_row;
-    const int sw_local = (wave - C::BM / 64) * 64 + lane;
-    const float* swp = a.sw + (WGRAD ? block0 * a.sw_step : group * a.sw_group) + (n0 + (!scales_of_x && sw_local < n_count ? sw_local : 0)) * a.sw_row;
-    const float* sp = scales_of_x ? sxp : swp;
-    const int64_t s_step = scales_of_x ? a.sx_step : a.sw_step;
+    const int units = cum[a.groups - 1];
+    const int total = __builtin_amdgcn_readfirstlane(WGRAD ? a.tiles_m * a.tiles_n * a.groups : units * a.tiles_n);
+    const int workers = static_cast<int>(gridDim.x) < total ? static_cast<int>(gridDim.x) : total;
+    if (static_cast<int>(blockIdx.x) >= workers) return;
 
+    // ---- a tile: rows m_first .. of the operand X (forward: of the routed order), columns n0 .., steps of its contraction
+    struct Place { int group, m_first, m_count, n0, n_count, steps, block0; };
+    auto locate = [&](int t) __attribute__((always_inline)) {
+        Place p;
+        int tm, tn;
+        if (WGRAD) {
+            const int per = a.tiles_m * a.tiles_n;
+            p.group = t / per;
+            banded_tile(t - p.group * per, a.tiles_m, a.tiles_n, tm, tn);
+            const int first = p.group ? cum[p.group - 1] : 0, last = cum[p.group];
+            // (of groups that overlap: no more blocks than there are)
+            p.block0 = __builtin_amdgcn_readfirstlane(first < 0 ? 0 : first < a.blocks ? first : a.blocks);
+            const int own = last - first, left = a.blocks - p.block0;
+            p.steps = __builtin_amdgcn_readfirstlane(own < left ? own : left);
+            p.m_first = tm * C::BM;
+            p.m_count = a.M - p.m_first;
+        } else {
+            const int u = t / a.tiles_n;
+            int g0 = 0;
+            unsigned long long past;
+            for (;; g0 += 64) {
+                past = __builtin_amdgcn_ballot_w64(g0 + lane < a.groups && cum[g0 + lane < a.groups ? g0 + lane : 0] > u);
+                if (past || g0 + 64 >= a.groups) break;
+            }
+            p.group = past ? g0 + __builtin_ctzll(past) : a.groups - 1;
+            const int before = p.group ? cum[p.group - 1] : 0;
+            const int first = __builtin_amdgcn_readfirstlane(off[2 * p.group]), count = __builtin_amdgcn_readfirstlane(off[2 * p.group + 1]);
+            const int tiles_m = (count + C::BM - 1) / C::BM;
+            int local = t - __builtin_amdgcn_readfirstlane(before) * a.tiles_n;
+            // (always in range, unless groups that overlap have made the sums overflow)
+            if (local < 0 || local >= tiles_m * a.tiles_n) local = 0;
+            banded_tile(local, tiles_m, a.tiles_n, tm, tn);
+            p.m_first = first + tm * C::BM;
+            p.m_count = count - tm * C::BM;
+            p.steps = a.ksteps;
+            p.block0 = 0;
+        }
+        p.m_count = p.m_count < C::BM ? p.m_count : C::BM;
+        p.n0 = tn * C::BN;
+        p.n_count = a.N - p.n0 < C::BN ? static_cast<int>(a.N - p.n0) : C::BN;
+        return p;
+    };
+
+    // ---- the stream of steps: `ld` is the tile whose steps are requested
+    // (rows past the end: X reads the last one, W zeros; what they give is not written)
+    const bool scales_of_x = wave < C::BM / 64;            // 64 rows' scales a load, those of X by the first waves
+    int src[C::LX], src_s = 0;
+    auto x_rows = [&](const Place& p) __attribute__((always_inline)) {
+        auto source = [&](int row) __attribute__((always_inline)) {
+            const int s = p.m_first + (row < p.m_count ? row : p.m_count - 1);
+            return !WGRAD && a.index ? a.index[s] : s;
+        };
+#pragma unroll
+        for (int i = 0; i < C::LX; ++i) src[i] = source((i * C::NW + wave) * 8 + (lane >> 3));
+        if (scales_of_x) src_s = source(wave * 64 + lane);
+    };
+    const uint8_t *xp[C::LX], *wp;
+    const float* sp;
+    int w_bytes;
+    const int x_chunk = ((lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2))) * 16;
+    const int w_row = static_cast<int>(a.w_row), w_lane = (lane >> 3) * w_row + ((lane & 7) ^ ((lane >> 4) & 1) ^ ((wave & 3) << 1)) * 16;
+    auto aim = [&](const Place& p) __attribute__((always_inline)) {
+        auto inside = [&](int s) __attribute__((always_inline)) { return static_cast<int64_t>(s < 0 ? 0 : s >= a.x_rows ? a.x_rows - 1 : s); };
+#pragma unroll
+        for (int i = 0; i < C::LX; ++i) xp[i] = a.xq + p.block0 * a.x_step + inside(src[i]) * a.x_row + x_chunk;
+        wp = a.wq + (WGRAD ? p.block0 * a.w_step : p.group * a.w_group) + static_cast<int64_t>(p.n0) * a.w_row;
+        w_bytes = (p.n_count - 1) * w_row + 128;
+        const int local = (wave - C::BM / 64) * 64 + lane;
+        if (scales_of_x) sp = a.sx + p.block0 * a.sx_step + inside(src_s) * a.sx_row;
+        else sp = a.sw + (WGRAD ? p.block0 * a.sw_step : p.group * a.sw_group) + (p.n0 + (local < p.n_count ? local : 0)) * a.sw_row;
+    };
+    const int64_t s_step = scales_of_x ? a.sx_step : a.sw_step;
     auto to_lds = [&](const void* p, int at, auto size) __attribute__((always_inline)) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)(smem + at), size.value, 0, 0);
     };
-    auto request = [&](int stage) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < C::LX; ++i) {
+    auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
+        if (i < C::LX) {
             to_lds(xp[i], stage + (i * C::NW + wave) * 1024, std::integral_constant<int, 16>{});
             xp[i] += a.x_step;
+        } else if (i < C::LX + C::LW) {
+            const int k = (i - C::LX) * C::NW + wave;
+            const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wp), 0, w_bytes, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + k * 1024), 16, w_lane, k * 8 * w_row, 0, 0);
+            if (i == C::LX + C::LW - 1) wp += a.w_step;
+        } else {
+            to_lds(sp, stage + C::OFF_SX + wave * 256, std::integral_constant<int, 4>{});
+            sp += s_step;
         }
-        const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wp), 0, w_bytes, 0x00020000);
-#pragma unroll
-        for (int i = 0; i < C::LW; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + (i * C::NW + wave) * 1024), 16,
-                                                     w_lane, (i * C::NW + wave) * 8 * static_cast<int>(a.w_row), 0, 0);
-        wp += a.w_step;
-        to_lds(sp, stage + C::OFF_SX + wave * 256, std::integral_constant<int, 4>{});
-        sp += s_step;
+    };
+    int ld_tile = xcd_contiguous(blockIdx.x, workers), ld_k = 0;
+    Place ld = locate(ld_tile);
+    bool more = true;                  // there is a step to request
+    // the next tile that has steps (weight gradient: an empty group's has none)
+    auto skip_empty = [&]() __attribute__((always_inline)) {
+        while (ld.steps <= 0) {
+            ld_tile += workers;
+            if (ld_tile >= total) { more = false; return; }
+            ld = locate(ld_tile);
+        }
+    };
+    auto advance = [&]() __attribute__((always_inline)) {
+        if (!more || ++ld_k < ld.steps) return;
+        ld_k = 0;
+        ld_tile += workers;
+        if (ld_tile >= total) { more = false; return; }
+        ld = locate(ld_tile);
+        if (WGRAD) {
+            skip_empty();
+            if (!more) return;
+        }
+        x_rows(ld);
+        aim(ld);
     };
 
-    // ---- where it reads operands
+    // ---- operands
     const int w_r = (r >> 2) * 8 + (r & 3);                // column, of the 32 of two tiles, that row r of the first one stands for
     int x_off[2], w_off[2];
 #pragma unroll
@@ -156,55 +226,137 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         w_off[h] = C::OFF_W + (wn * TN * 16 + w_r) * 128 + ((2 * g + h) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) * 16;
     }
     const int sx_off = C::OFF_SX + (wm * TM * 16 + r) * 4, sw_off = C::OFF_SW + (wn * TN * 16 + w_r) * 4;
+    u32x4 fx[2][2][2], fw[TN][2];
+    uint32_t sx[2][2], sw[TN];
+    // read i (of 6) of pair p into its set; of W fragment j (of 3)
+    auto read_x = [&](int stage, int p, int i) __attribute__((always_inline)) {
+        const int f = i / 3, k = i % 3;
+        if (k < 2) fx[p & 1][f][k] = *reinterpret_cast<const u32x4*>(smem + stage + (2 * p + f) * 2048 + x_off[k]);
+        else sx[p & 1][f] = *reinterpret_cast<const uint32_t*>(smem + stage + sx_off + (2 * p + f) * 64);
+    };
+    auto read_w = [&](int stage, int j, int k) __attribute__((always_inline)) {
+        if (k < 2) fw[j][k] = *reinterpret_cast<const u32x4*>(smem + stage + coff_of(j) * 128 + w_off[k]);
+        else sw[j] = *reinterpret_cast<const uint32_t*>(smem + stage + sw_off + coff_of(j) * 4);
+    };
     v4f acc[TM][TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](int p, int i) __attribute__((always_inline)) {
+        const int j = i >> 1, f = i & 1;
+        acc[2 * p + f][j] = gg_mfma(join(fw[j][0], fw[j][1]), join(fx[p & 1][f][0], fx[p & 1][f][1]), acc[2 * p + f][j], scale_byte(sw[j]), scale_byte(sx[p & 1][f]));
+    };
 
-    if (ksteps > 0) request(0);
-    for (int k = 0; k < ksteps; ++k) {
-        const int stage = (k & 1) * C::STAGE;
-        if (k + 1 < ksteps) {
-            request(C::STAGE - stage);
-            wait_vmcnt<C::LX + C::LW + 1>();
+    int tile = ld_tile, stage = 0;
+    Place at = ld;
+    if (WGRAD) skip_empty();
+    if (more) {
+        x_rows(ld);
+        aim(ld);
+    }
+    bool second = false;               // (a step beyond the first was requested)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < C::LOADS; ++i) request_one(k * C::STAGE, i);
+            second = k == 1;
+        }
+        advance();
+    }
+    if (second) wait_vmcnt<C::LOADS>();
+    else wait_vmcnt<0>();
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < 6; ++i) read_x(0, 0, i);
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) read_w(0, j, k);
+    // Where a tile's values left in STORES stores, the loads of the step that was requested before them are awaited with the
+    // stores in flight.
+    constexpr int STORES = TM * TN / 2;
+    bool late = false;
+
+    for (; tile < total; tile += workers) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < at.steps; ++k) {
+#pragma unroll
+            for (int p = 0; p < PAIRS - 1; ++p)
+#pragma unroll
+                for (int i = 0; i < MM; ++i) {
+                    if (i < 6) read_x(stage, p + 1, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply(p, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if (late) wait_vmcnt<STORES>();
+            else wait_vmcnt<0>();                              // the next step has landed
+            late = false;
+            lds_barrier();                                     // ... for everyone, and everyone has this one's operands
+            const int freed = stage;
+            stage = C::STAGE - stage;
+#pragma unroll
+            for (int i = 0; i < MM; ++i) {
+                multiply(PAIRS - 1, i);
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < 6) read_x(stage, 0, i);
+                if (i & 1)
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) read_w(stage, i >> 1, q);
+                if (more)
+#pragma unroll
+                    for (int l = C::LOADS * i / MM; l < C::LOADS * (i + 1) / MM; ++l) request_one(freed, l);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            advance();
+        }
+
+        // ---- lane (r, g) holds row 16 i + r, columns 32 (j / 2) + 8 g + 0 .. 7
+        const int64_t row0 = WGRAD ? static_cast<int64_t>(at.group) * a.M + at.m_first : static_cast<int64_t>(at.m_first);
+        if (a.wide) {                  // whole runs of 8 columns; what is past the result is dropped
+            const int N = static_cast<int>(a.N), n_lane = at.n0 + wn * TN * 16 + g * 8, o_lane = (wm * TM * 16 + r) * N + n_lane;
+            // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
+            // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
+            if (a.out) {
+                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(a.out + row0 * a.N, 0, at.m_count * N * 2, 0x00020000);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; j += 2) {
+                        const v4f u = acc[i][j], v = acc[i][j + 1];
+                        const u32x4 w{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]), pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                        __builtin_amdgcn_raw_buffer_store_b128(w, o, n_lane + j * 16 < N ? (o_lane + i * 16 * N + j * 16) * 2 : 0x7FFFFFFF, 0, 0);
+                    }
+            }
+            if (a.y) {
+                const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(a.y + row0 * a.N, 0, at.m_count * N * 4, 0x00020000);
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), o,
+                                                               n_lane + (j >> 1) * 32 < N ? (o_lane + i * 16 * N + (j >> 1) * 32 + (j & 1) * 4) * 4 : 0x7FFFFFFF, 0, 0);
+            }
+            late = a.out && !a.y;
         } else {
-            wait_vmcnt<0>();
-        }
-        lds_barrier();
-        v8i w[TN];
-        int sw[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const uint8_t* p = smem + stage + coff_of(j) * 128;
-            w[j] = join(*reinterpret_cast<const u32x4*>(p + w_off[0]), *reinterpret_cast<const u32x4*>(p + w_off[1]));
-            sw[j] = scale_byte(*reinterpret_cast<const uint32_t*>(smem + stage + sw_off + coff_of(j) * 4));
-        }
+            for (int i = 0; i < TM; ++i) {
+                const int row = (wm * TM + i) * 16 + r;
+                if (row >= at.m_count) continue;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-            const uint8_t* p = smem + stage + i * 2048;
-            const v8i x = join(*reinterpret_cast<const u32x4*>(p + x_off[0]), *reinterpret_cast<const u32x4*>(p + x_off[1]));
-            const int sx = scale_byte(*reinterpret_cast<const uint32_t*>(smem + stage + sx_off + i * 64));
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = gg_mfma(w[j], x, acc[i][j], sw[j], sx);
+                for (int j = 0; j < TN; j += 2) {
+                    const int64_t n = at.n0 + wn * TN * 16 + j * 16 + g * 8;
+                    const float f[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
+                    if (a.out) put8(a.out + (row0 + row) * a.N, n, a.N, f);
+                    if (a.y) put8(a.y + (row0 + row) * a.N, n, a.N, f);
+                }
+            }
+            late = false;
         }
-        lds_barrier();
+        if (tile + workers < total) at = locate(tile + workers);
     }
-
-    // ---- lane (r, g) holds row 16 i + r, columns 32 (j / 2) + 8 g + 0 .. 7
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int row = (wm * TM + i) * 16 + r;
-        if (row >= m_count) continue;
-        const int64_t at = (WGRAD ? static_cast<int64_t>(group) * a.M + m_first + row : static_cast<int64_t>(m_first) + row) * a.N;
-#pragma unroll
-        for (int j = 0; j < TN; j += 2) {
-            const int64_t n = n0 + wn * TN * 16 + j * 16 + g * 8;
-            const float f[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
-            if (a.out) put8(a.out + at, n, a.N, f);
-            if (a.y) put8(a.y + at, n, a.N, f);
-        }
-    }
+    wait_vmcnt<0>();
 }
 
 template <class C, bool WGRAD>
@@ -231,8 +383,12 @@ template <class C, bool WGRAD>
 static loka_status gg_launch(GgArgs& a, int64_t grid, hipStream_t stream) {
     a.tiles_n = static_cast<int>((a.N + C::BN - 1) / C::BN);
     a.tiles_m = WGRAD ? (a.M + C::BM - 1) / C::BM : 0;
-    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&gg_tile_kernel<C, WGRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS));
-    gg_tile_kernel<C, WGRAD><<<static_cast<uint32_t>(grid), 64 * C::NW, C::LDS, stream>>>(a);
+    a.wide = a.N % 8 == 0;
+    const int lds = C::LDS + 12 * a.groups;
+    const int64_t slots = 256 * C::PER_CU;
+    // (on every call, a host-side table write: no process-wide state, and correct on whichever device is current)
+    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&gg_tile_kernel<C, WGRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    gg_tile_kernel<C, WGRAD><<<static_cast<uint32_t>(grid < slots ? grid : slots), 64 * C::NW, lds, stream>>>(a);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }
@@ -282,7 +438,7 @@ loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, 
     a.out = static_cast<uint16_t*>(dw);
     a.y = dw32;
     a.N = d->N;
-    a.M = static_cast<int>(d->K);
+    a.M = a.x_rows = static_cast<int>(d->K);
     a.blocks = static_cast<int>(loka_grouped_blocks(d->rows, d->groups));
     a.rows = static_cast<int>(d->rows);
     a.groups = d->groups;
