@@ -222,8 +222,8 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     int x_off[2], w_off[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        x_off[h] = (wm * TM * 16 + r) * 128 + ((2 * g + h) ^ ((r >> 1) & 7)) * 16;
-        w_off[h] = C::OFF_W + (wn * TN * 16 + w_r) * 128 + ((2 * g + h) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) * 16;
+        x_off[h] = (wm * TM * 16 + r) * 128 + ((g + 4 * h) ^ ((r >> 1) & 7)) * 16;
+        w_off[h] = C::OFF_W + (wn * TN * 16 + w_r) * 128 + ((g + 4 * h) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) * 16;
     }
     const int sx_off = C::OFF_SX + (wm * TM * 16 + r) * 4, sw_off = C::OFF_SW + (wn * TN * 16 + w_r) * 4;
     u32x4 fx[2][2][2], fw[TN][2];
