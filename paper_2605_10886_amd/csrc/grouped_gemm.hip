@@ -56,26 +56,29 @@ __device__ __forceinline__ void put8(float* row, int64_t n, int64_t N, const flo
 
 // ---------------------------------------------------------------------------------
 // Tiles in LDS.  A workgroup of WM x WN waves computes BM x BN values, each wave TM x TN tiles of 16 x 16, in steps of 128 along the
-// contraction: 128 bytes a row, two steps in LDS.  The 16-byte chunks of a row lie permuted so that the 16 rows of a read use all
+// contraction: 128 bytes a row, two steps in LDS (of the scales three).  The 16-byte chunks of a row lie permuted so that the 16 rows of a read use all
 // banks: chunk c of X's row r at place c ^ (r / 2 % 8), of W's row r, whose reads take rows 8 apart, at c ^ (bits 1, 3 and 4 of r).
 //
 // A step is TM / 2 pairs of X's 16-row fragments against all of the wave's W fragments; a pair is read while the pair before it is
-// multiplied.  One barrier a step, in front of its last pair: by then the step's operands are in registers, so the loads of the
-// step after next may go where they lay, and the first pair and W's fragments of the next step are read between the matrix
-// instructions that follow.  Workgroups are persistent, and the stream of steps does not stop between result tiles: the next
-// tile's first steps arrive while this one's values are stored, and nothing waits for the stores where their number is known.
+// multiplied, W's fragments and the first pair of the next step during the last.  Two barriers a step, in front of the second pair and
+// of the last, give LDS back as soon as it is read: behind the first one W and the first two pairs of X of the step after next are
+// requested, behind the second X's other pairs, and each is awaited 1.5 steps later (a round trip through L2 under load is longer than a
+// step; with one barrier, and one step, 32768 rows x 4096 x 4096 took 583 us).  With two pairs to a step there is one barrier.  Workgroups are
+// persistent, and the stream of steps does not stop between result tiles: the next tile's first steps arrive while this one's
+// values are stored, and nothing waits for the stores where their number is known.
 template <int TM_, int TN_, int WM_, int WN_>
 struct GgTile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
-    static constexpr int OFF_W = BM * 128, OFF_SX = OFF_W + BN * 128, OFF_SW = OFF_SX + BM * 4, STAGE = OFF_SW + BN * 4, LDS = 2 * STAGE;
-    static constexpr int LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64, LOADS = LX + LW + 1;
+    static constexpr int OFF_W = BM * 128, STAGE = OFF_W + BN * 128, OFF_S = 2 * STAGE, SCALES = (BM + BN) * 4, LDS = OFF_S + 3 * SCALES;
+    static constexpr int PAIRS = TM / 2, LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64, LOADS = LX + LW + 1;
+    static constexpr int FIRST = PAIRS == 4 ? LW + LX / 2 + 1 : LOADS, SECOND = LOADS - FIRST;      // loads behind the first barrier, and the second
     static constexpr int PER_CU = 163840 / (LDS + 12288);   // (with the table of 1024 groups)
-    static_assert(SROWS == NW && TM % 4 == 0 && TN % 2 == 0 && (NW == 4 || NW == 8));
+    static_assert(SROWS == NW && (PAIRS == 2 || PAIRS == 4) && LX == 4 && WM == 2 && TN % 2 == 0 && (NW == 4 || NW == 8));
 };
 
 template <class C, bool WGRAD>
 __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
-    constexpr int TM = C::TM, TN = C::TN, PAIRS = TM / 2, MM = 2 * TN;
+    constexpr int TM = C::TM, TN = C::TN, PAIRS = C::PAIRS, MM = 2 * TN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wm = wave / C::WN, wn = wave % C::WN;
 
@@ -143,20 +146,26 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         p.m_count = p.m_count < C::BM ? p.m_count : C::BM;
         p.n0 = tn * C::BN;
         p.n_count = a.N - p.n0 < C::BN ? static_cast<int>(a.N - p.n0) : C::BN;
+        // (all of it in scalar registers)
+        for (int* v : {&p.group, &p.m_first, &p.m_count, &p.n0, &p.n_count, &p.steps, &p.block0}) *v = __builtin_amdgcn_readfirstlane(*v);
         return p;
     };
 
-    // ---- the stream of steps: `ld` is the tile whose steps are requested
+    // ---- the stream of steps: `ld` is the tile whose steps are requested, `next` the one behind it
     // (rows past the end: X reads the last one, W zeros; what they give is not written)
     const bool scales_of_x = wave < C::BM / 64;            // 64 rows' scales a load, those of X by the first waves
-    int src[C::LX], src_s = 0;
+    // row, of the tile, of load i of X: a pair's rows of both halves of the tile (2 TM / LX pairs to a load)
+    auto x_row_of = [&](int i) __attribute__((always_inline)) {       // (of lane 0)
+        return PAIRS == 4 ? (wave >> 2) * 128 + i * 32 + (wave & 3) * 8 : (i & 1) * 64 + (i >> 1) * 32 + wave * 8;
+    };
+    int src[C::LX], src_s = 0;         // X's rows of a tile, loaded a tile ahead
     auto x_rows = [&](const Place& p) __attribute__((always_inline)) {
         auto source = [&](int row) __attribute__((always_inline)) {
             const int s = p.m_first + (row < p.m_count ? row : p.m_count - 1);
             return !WGRAD && a.index ? a.index[s] : s;
         };
 #pragma unroll
-        for (int i = 0; i < C::LX; ++i) src[i] = source((i * C::NW + wave) * 8 + (lane >> 3));
+        for (int i = 0; i < C::LX; ++i) src[i] = source(x_row_of(i) + (lane >> 3));
         if (scales_of_x) src_s = source(wave * 64 + lane);
     };
     const uint8_t *xp[C::LX], *wp;
@@ -178,43 +187,57 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     auto to_lds = [&](const void* p, int at, auto size) __attribute__((always_inline)) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p, (__attribute__((address_space(3))) void*)(smem + at), size.value, 0, 0);
     };
+    // load i of a step: W's, X's first half, the scales; X's second half
+    int ld_s = 0;                      // the scales' place
+    auto request_x = [&](int stage, int i) __attribute__((always_inline)) {
+        to_lds(xp[i], stage + x_row_of(i) * 128, std::integral_constant<int, 16>{});
+        xp[i] += a.x_step;
+    };
     auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
-        if (i < C::LX) {
-            to_lds(xp[i], stage + (i * C::NW + wave) * 1024, std::integral_constant<int, 16>{});
-            xp[i] += a.x_step;
-        } else if (i < C::LX + C::LW) {
-            const int k = (i - C::LX) * C::NW + wave;
+        if (i < C::LW) {
+            const int k = i * C::NW + wave;
             const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wp), 0, w_bytes, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + k * 1024), 16, w_lane, k * 8 * w_row, 0, 0);
-            if (i == C::LX + C::LW - 1) wp += a.w_step;
-        } else {
-            to_lds(sp, stage + C::OFF_SX + wave * 256, std::integral_constant<int, 4>{});
+            if (i == C::LW - 1) wp += a.w_step;
+        } else if (i < C::LW + C::LX / 2) {
+            request_x(stage, i - C::LW);
+        } else if (i == C::LW + C::LX / 2) {
+            to_lds(sp, C::OFF_S + ld_s + wave * 256, std::integral_constant<int, 4>{});
             sp += s_step;
+            ld_s = ld_s == 2 * C::SCALES ? 0 : ld_s + C::SCALES;
+        } else {
+            request_x(stage, i - C::LW - 1);
         }
     };
-    int ld_tile = xcd_contiguous(blockIdx.x, workers), ld_k = 0;
-    Place ld = locate(ld_tile);
-    bool more = true;                  // there is a step to request
-    // the next tile that has steps (weight gradient: an empty group's has none)
-    auto skip_empty = [&]() __attribute__((always_inline)) {
-        while (ld.steps <= 0) {
-            ld_tile += workers;
-            if (ld_tile >= total) { more = false; return; }
-            ld = locate(ld_tile);
+    // the first tile from t on that has steps (weight gradient: an empty group's has none), total where there is none
+    auto with_steps = [&](int t, Place& p) __attribute__((always_inline)) {
+        while (t < total) {
+            p = locate(t);
+            if (!WGRAD || p.steps > 0) break;
+            t += workers;
         }
+        return t;
     };
-    auto advance = [&]() __attribute__((always_inline)) {
-        if (!more || ++ld_k < ld.steps) return;
-        ld_k = 0;
-        ld_tile += workers;
-        if (ld_tile >= total) { more = false; return; }
-        ld = locate(ld_tile);
-        if (WGRAD) {
-            skip_empty();
-            if (!more) return;
-        }
+    const int first_tile = xcd_contiguous(blockIdx.x, workers);
+    Place ld, next;
+    int ld_k = 0, next_tile = with_steps(first_tile, ld);
+    const bool any = next_tile < total;
+    auto look_ahead = [&]() __attribute__((always_inline)) {
+        if (next_tile < total) next_tile = with_steps(next_tile + workers, next);
+        if (next_tile < total) x_rows(next);
+    };
+    if (any) {
         x_rows(ld);
         aim(ld);
+        look_ahead();
+    }
+    // behind the last tile's steps the same again, so that every step requests as many loads
+    auto advance = [&]() __attribute__((always_inline)) {
+        if (++ld_k < ld.steps) return;
+        ld_k = 0;
+        if (next_tile < total) ld = next;
+        aim(ld);
+        look_ahead();
     };
 
     // ---- operands
@@ -225,18 +248,19 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         x_off[h] = (wm * TM * 16 + r) * 128 + ((g + 4 * h) ^ ((r >> 1) & 7)) * 16;
         w_off[h] = C::OFF_W + (wn * TN * 16 + w_r) * 128 + ((g + 4 * h) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) * 16;
     }
-    const int sx_off = C::OFF_SX + (wm * TM * 16 + r) * 4, sw_off = C::OFF_SW + (wn * TN * 16 + w_r) * 4;
+    const int sx_off = C::OFF_S + (wm * TM * 16 + r) * 4, sw_off = C::OFF_S + C::BM * 4 + (wn * TN * 16 + w_r) * 4;
     u32x4 fx[2][2][2], fw[TN][2];
     uint32_t sx[2][2], sw[TN];
+    int scales = 0;                    // where the scales lie that are read
     // read i (of 6) of pair p into its set; of W fragment j (of 3)
     auto read_x = [&](int stage, int p, int i) __attribute__((always_inline)) {
         const int f = i / 3, k = i % 3;
         if (k < 2) fx[p & 1][f][k] = *reinterpret_cast<const u32x4*>(smem + stage + (2 * p + f) * 2048 + x_off[k]);
-        else sx[p & 1][f] = *reinterpret_cast<const uint32_t*>(smem + stage + sx_off + (2 * p + f) * 64);
+        else sx[p & 1][f] = *reinterpret_cast<const uint32_t*>(smem + scales + sx_off + (2 * p + f) * 64);
     };
     auto read_w = [&](int stage, int j, int k) __attribute__((always_inline)) {
         if (k < 2) fw[j][k] = *reinterpret_cast<const u32x4*>(smem + stage + coff_of(j) * 128 + w_off[k]);
-        else sw[j] = *reinterpret_cast<const uint32_t*>(smem + stage + sw_off + coff_of(j) * 4);
+        else sw[j] = *reinterpret_cast<const uint32_t*>(smem + scales + sw_off + coff_of(j) * 4);
     };
     v4f acc[TM][TN];
     auto multiply = [&](int p, int i) __attribute__((always_inline)) {
@@ -244,72 +268,79 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         acc[2 * p + f][j] = gg_mfma(join(fw[j][0], fw[j][1]), join(fx[p & 1][f][0], fx[p & 1][f][1]), acc[2 * p + f][j], scale_byte(sw[j]), scale_byte(sx[p & 1][f]));
     };
 
-    int tile = ld_tile, stage = 0;
-    Place at = ld;
-    if (WGRAD) skip_empty();
-    if (more) {
-        x_rows(ld);
-        aim(ld);
-    }
-    bool second = false;               // (a step beyond the first was requested)
+    int stage = 0;
+    if (any) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        if (more) {
+        for (int k = 0; k < 2; ++k) {
 #pragma unroll
             for (int i = 0; i < C::LOADS; ++i) request_one(k * C::STAGE, i);
-            second = k == 1;
+            if (k == 0) advance();
         }
-        advance();
+        wait_vmcnt<C::SECOND + C::LOADS>();
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < 6; ++i) read_x(0, 0, i);
+#pragma unroll
+        for (int j = 0; j < TN - 1; ++j)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) read_w(0, j, k);
     }
-    if (second) wait_vmcnt<C::LOADS>();
-    else wait_vmcnt<0>();
-    lds_barrier();
+    // Where a tile's values left in STORES stores, the loads that were requested before them are awaited with the stores in flight.
+    constexpr int STORES = TM * TN / 2, NEWER = PAIRS == 4 ? C::LOADS : 0;
+    int late = 0;
+    auto landed = [&]() __attribute__((always_inline)) {
+        if (late > 0) { --late; wait_vmcnt<NEWER + STORES>(); }
+        else wait_vmcnt<NEWER>();
+        lds_barrier();
+    };
+    // the matrix instructions of pair p, and between them the LDS reads of the pair behind it (a burst would hold the issue stage up)
+    // and `count` of the loads from `from` on into `freed`
+    auto pair = [&](int p, int freed, int from, int count) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 6; ++i) read_x(0, 0, i);
+        for (int i = 0; i < MM; ++i) {
+            multiply(p, i);
+            __builtin_amdgcn_sched_barrier(0);
+            if (p == 0 && i == 0)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+                for (int q = 0; q < 3; ++q) read_w(stage, TN - 1, q);
+            if (i < 6) read_x(stage, p + 1, i);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) read_w(0, j, k);
-    // Where a tile's values left in STORES stores, the loads of the step that was requested before them are awaited with the
-    // stores in flight.
-    constexpr int STORES = TM * TN / 2;
-    bool late = false;
+            for (int l = from + count * i / MM; l < from + count * (i + 1) / MM; ++l) request_one(freed, l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 
-    for (; tile < total; tile += workers) {
+    Place at = locate(first_tile);
+    for (int tile = first_tile; tile < total; tile += workers) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
         for (int k = 0; k < at.steps; ++k) {
-#pragma unroll
-            for (int p = 0; p < PAIRS - 1; ++p)
-#pragma unroll
-                for (int i = 0; i < MM; ++i) {
-                    if (i < 6) read_x(stage, p + 1, i);
-                    __builtin_amdgcn_sched_barrier(0);
-                    multiply(p, i);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            if (late) wait_vmcnt<STORES>();
-            else wait_vmcnt<0>();                              // the next step has landed
-            late = false;
-            lds_barrier();                                     // ... for everyone, and everyone has this one's operands
+            pair(0, 0, 0, 0);
+            advance();                                         // (of the loads, which are two steps ahead)
+            if constexpr (PAIRS == 4) {
+                landed();                                      // this step's other pairs; everyone has W and the first two
+                pair(1, stage, 0, C::FIRST / 2 + 1);
+                pair(2, stage, C::FIRST / 2 + 1, C::FIRST - C::FIRST / 2 - 1);
+            }
+            landed();                                          // the next step's W and first pairs; everyone has this one's operands
             const int freed = stage;
+            constexpr int FROM = PAIRS == 4 ? C::FIRST : 0;
             stage = C::STAGE - stage;
+            scales = scales == 2 * C::SCALES ? 0 : scales + C::SCALES;
 #pragma unroll
             for (int i = 0; i < MM; ++i) {
                 multiply(PAIRS - 1, i);
                 __builtin_amdgcn_sched_barrier(0);
                 if (i < 6) read_x(stage, 0, i);
-                if (i & 1)
+                if ((i & 1) && i < MM - 1)                     // (the last one behind the next step's first instruction, which does not wait for it)
 #pragma unroll
                     for (int q = 0; q < 3; ++q) read_w(stage, i >> 1, q);
-                if (more)
 #pragma unroll
-                    for (int l = C::LOADS * i / MM; l < C::LOADS * (i + 1) / MM; ++l) request_one(freed, l);
+                for (int l = FROM + (C::LOADS - FROM) * i / MM; l < FROM + (C::LOADS - FROM) * (i + 1) / MM; ++l) request_one(freed, l);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            advance();
         }
 
         // ---- lane (r, g) holds row 16 i + r, columns 32 (j / 2) + 8 g + 0 .. 7
@@ -338,7 +369,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), o,
                                                                n_lane + (j >> 1) * 32 < N ? (o_lane + i * 16 * N + (j >> 1) * 32 + (j & 1) * 4) * 4 : 0x7FFFFFFF, 0, 0);
             }
-            late = a.out && !a.y;
+            late = a.out && !a.y ? (PAIRS == 4 ? 3 : 1) : 0;
         } else {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
@@ -352,7 +383,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
                     if (a.y) put8(a.y + (row0 + row) * a.N, n, a.N, f);
                 }
             }
-            late = false;
+            late = 0;
         }
         if (tile + workers < total) at = locate(tile + workers);
     }
