@@ -1,15 +1,18 @@
 // The choice of experts, and the sum of their results (include/loka.h: loka_route, loka_combine and their backward passes).
 #include "experts.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace loka {
 
 // ---------------------------------------------------------------------------------
-// The choice.  L lanes hold a token's logits, V each (entry lane + L v), as keys whose order as unsigned integers is the logits'
-// order: 0 for what may not be chosen.  A choice is the largest key over the lanes, then the lowest entry that has it.
-constexpr int kRouteChunk = 128;       // tokens of a workgroup
-constexpr int kRouteThreads = 256;
+// The choice.  L lanes hold a token's logits, V each, in runs of R that follow each other in memory, as keys whose order as unsigned
+// integers is the logits' order: 0 for what may not be chosen.  A choice is the largest key over the lanes, then the lowest entry that has it.  A
+// bf16's key has room for the entry as well, so that all keys differ and the largest one is the choice.
+constexpr int kRouteMostChunk = 128;   // tokens of a workgroup, at most
+constexpr int kRouteThreads = 256;     // ... and its threads, of a small call and of the gradient
+constexpr int kRouteMost = 1024;       // ... of a call of more tokens
 
 __device__ __forceinline__ uint32_t key_of(float x) {
     if (x != x) return 0xFFC00000u;                        // above plus infinity
@@ -28,6 +31,44 @@ template <bool BF16>
 __device__ __forceinline__ float logit_at(const void* logits, int64_t i) {
     return BF16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(logits)[i]) : static_cast<const float*>(logits)[i];
 }
+// entry v of lane l
+template <int L, int R>
+__device__ __forceinline__ int entry_of(int l, int v) { return ((v / R) * L + l) * R + v % R; }
+// A lane's logits of the row at element `at`; minus infinity past the experts
+template <int L, int V, int R, bool BF16>
+__device__ __forceinline__ void load_logits(const void* logits, int64_t at, int experts, int l, float (&x)[V]) {
+#pragma unroll
+    for (int b = 0; b < V; b += R) {
+        const int e = entry_of<L, R>(l, b);
+        if constexpr (R == 1) {
+            x[b] = e < experts ? logit_at<BF16>(logits, at + e) : -INFINITY;
+        } else {                       // (runs are whole)
+            const bool in = e < experts;
+            const int64_t i = at + (in ? e : 0);
+            if constexpr (!BF16) {
+                const v4f v = *reinterpret_cast<const v4f*>(static_cast<const float*>(logits) + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[b + k] = in ? v[k] : -INFINITY;
+            } else {
+                uint32_t w[R / 2];
+                if constexpr (R == 8) {
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(logits) + i);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w[k] = v[k];
+                } else {
+                    const u32x2 v = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(logits) + i);
+                    w[0] = v.x;
+                    w[1] = v.y;
+                }
+#pragma unroll
+                for (int k = 0; k < R / 2; ++k) {
+                    x[b + 2 * k] = in ? bf16_lo(w[k]) : -INFINITY;
+                    x[b + 2 * k + 1] = in ? bf16_hi(w[k]) : -INFINITY;
+                }
+            }
+        }
+    }
+}
 
 struct RouteArgs {
     const void* logits;
@@ -36,8 +77,8 @@ struct RouteArgs {
     float scale;
     int32_t *expert, *slot, *row, *offsets;
     float* weight;
-    int32_t* counts;                   // [chunks + 1][experts]: of a chunk's tokens, then the same of all earlier chunks; the last: of all
-    int chunks;
+    int32_t* counts;                   // [chunks + 1][pitch]: of a chunk's tokens; scanned: of all earlier chunks, the last of all
+    int chunks, chunk_tokens, pitch;   // pitch: experts up to a power of two, 4 at least
     const float* dweight;
     void* dlogits;
 };
@@ -66,12 +107,13 @@ __device__ __forceinline__ int block_exclusive(int v, int* lds, int& total) {
 }
 
 // first[e] = rows of the experts before e, from the counts of all (in LDS); returns their sum
+template <int THREADS>
 __device__ __forceinline__ int first_rows(const int* count, int* first, int experts, int* lds) {
     int base = 0;
-    for (int e0 = 0; e0 < experts; e0 += kRouteThreads) {
+    for (int e0 = 0; e0 < experts; e0 += THREADS) {
         const int e = e0 + static_cast<int>(threadIdx.x);
         int total;
-        const int s = block_exclusive<kRouteThreads>(e < experts ? count[e] : 0, lds, total);
+        const int s = block_exclusive<THREADS>(e < experts ? count[e] : 0, lds, total);
         if (e < experts) first[e] = base + s;
         base += total;
     }
@@ -80,52 +122,72 @@ __device__ __forceinline__ int first_rows(const int* count, int* first, int expe
 
 // Choices and weights of a chunk's tokens, and each choice's place among those of the chunk with the same expert: a 128-bit mask
 // of tokens per expert (atomic OR: no order), whose bits below a token's are counted.  One chunk alone is finished here.
-template <int L, int V, bool BF16>
-__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(const RouteArgs a) {
+template <int L, int V, int R, bool BF16, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     unsigned long long* const mask = reinterpret_cast<unsigned long long*>(smem);          // [experts][2]
     int* const count = reinterpret_cast<int*>(mask + 2 * a.experts);
     int* const first = count + a.experts;
     int* const lds = first + a.experts;
     const int t = static_cast<int>(threadIdx.x), l = t % L, k = a.top_k;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRouteChunk;
-    const int tokens = a.tokens - t0 < kRouteChunk ? static_cast<int>(a.tokens - t0) : kRouteChunk;
-    for (int i = t; i < 2 * a.experts; i += kRouteThreads) mask[i] = 0;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.chunk_tokens;
+    const int tokens = a.tokens - t0 < a.chunk_tokens ? static_cast<int>(a.tokens - t0) : a.chunk_tokens;
+    for (int i = t; i < 2 * a.experts; i += THREADS) mask[i] = 0;
     __syncthreads();
-    constexpr int PER = kRouteThreads / L;
+    constexpr int PER = THREADS / L;
     for (int i = t / L; i < (tokens + PER - 1) / PER * PER; i += PER) {       // (whole waves: the lanes' exchanges need all of them)
         const bool in = i < tokens;
         const int64_t at = (t0 + (in ? i : 0)) * a.ld;
         uint32_t key[V];
+        {
+            float x[V];
+            load_logits<L, V, R, BF16>(a.logits, at, a.experts, l, x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = l + L * v < a.experts ? key_of(logit_at<BF16>(a.logits, at + l + L * v)) : 0u;
+            for (int v = 0; v < V; ++v) {
+                key[v] = key_of(x[v]);
+                if (BF16) key[v] = key[v] ? (key[v] >> 16 << 10) | (1023u - static_cast<unsigned>(entry_of<L, R>(l, v))) : 0u;
+            }
+        }
+        auto number = [](uint32_t k) __attribute__((always_inline)) { return value_of(BF16 ? (k >> 25 ? k >> 10 << 16 : k >> 10 << 16 | 0xFFFFu) : k); };
         float all = 0.f;
         if (a.score == LOKA_SCORE_SOFTMAX && !a.renorm) {
             uint32_t m = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v) m = key[v] > m ? key[v] : m;
-            const float top = value_of(lanes_max_bits<L>(m));
+            const float top = number(lanes_max_bits<L>(m));
 #pragma unroll
-            for (int v = 0; v < V; ++v) all += key[v] ? expf(value_of(key[v]) - top) : 0.f;
+            for (int v = 0; v < V; ++v) all += key[v] ? expf(number(key[v]) - top) : 0.f;
             all = lanes_sum<L>(all);
         }
         int mine = -1;                 // lane j: choice j
         uint32_t mine_key = 0, top_key = 0;
+        uint32_t m = BF16 ? 1u << 26 : 0u;                 // the choice before
         for (int j = 0; j < k; ++j) {
-            uint32_t m = 0;
+            int e;
+            if (BF16) {
+                // the largest key below it: of the differences, as unsigned numbers, those of smaller keys are the large ones
+                uint32_t d = 0;
 #pragma unroll
-            for (int v = 0; v < V; ++v) m = key[v] > m ? key[v] : m;
-            m = lanes_max_bits<L>(m);
-            unsigned low = 0;          // 65535 - entry
+                for (int v = 0; v < V; ++v) d = key[v] - m > d ? key[v] - m : d;
+                d = lanes_max_bits<L>(d);
+                m = d >> 31 ? m + d : 0u;
+                e = 1023 - static_cast<int>(m & 1023u);
+            } else {
+                m = 0;
 #pragma unroll
-            for (int v = V - 1; v >= 0; --v) low = key[v] == m ? 65535u - static_cast<unsigned>(l + L * v) : low;
-            const int e = 65535 - static_cast<int>(lanes_max_bits<L>(low));
+                for (int v = 0; v < V; ++v) m = key[v] > m ? key[v] : m;
+                m = lanes_max_bits<L>(m);
+                unsigned low = 0;      // 65535 - entry
 #pragma unroll
-            for (int v = 0; v < V; ++v) key[v] = l + L * v == e ? 0u : key[v];
+                for (int v = V - 1; v >= 0; --v) low = key[v] == m ? 65535u - static_cast<unsigned>(entry_of<L, R>(l, v)) : low;
+                e = 65535 - static_cast<int>(lanes_max_bits<L>(low));
+#pragma unroll
+                for (int v = 0; v < V; ++v) key[v] = entry_of<L, R>(l, v) == e ? 0u : key[v];
+            }
             if (j == 0) top_key = m;
             if (l == j && m) { mine = e; mine_key = m; }
         }
-        const float x = value_of(mine_key), top = value_of(top_key);
+        const float x = number(mine_key), top = number(top_key);
         float w = 0.f;
         if (a.score == LOKA_SCORE_SOFTMAX) {
             w = mine >= 0 ? expf(x - top) : 0.f;
@@ -148,17 +210,17 @@ __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(const Route
         }
     }
     __syncthreads();
-    for (int e = t; e < a.experts; e += kRouteThreads) {
+    for (int e = t; e < a.experts; e += THREADS) {
         const int n = __popcll(mask[2 * e]) + __popcll(mask[2 * e + 1]);
         count[e] = n;
-        if (a.chunks > 1) a.counts[static_cast<int64_t>(blockIdx.x) * a.experts + e] = n;
+        if (a.chunks > 1) a.counts[static_cast<int64_t>(blockIdx.x) * a.pitch + e] = n;
     }
     __syncthreads();
     const bool alone = a.chunks == 1;
     int total = 0;
-    if (alone) total = first_rows(count, first, a.experts, lds);
+    if (alone) total = first_rows<THREADS>(count, first, a.experts, lds);
     __syncthreads();
-    for (int i = t; i < tokens * k; i += kRouteThreads) {
+    for (int i = t; i < tokens * k; i += THREADS) {
         const int e = a.expert[t0 * k + i], m = i / k;
         if (e >= 0) {
             const unsigned long long below = (1ull << (m & 63)) - 1;
@@ -171,7 +233,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(const Route
         if (alone && i >= total) a.row[i] = -1;
     }
     if (alone) {
-        for (int e = t; e < a.experts; e += kRouteThreads) a.offsets[e] = first[e];
+        for (int e = t; e < a.experts; e += THREADS) a.offsets[e] = first[e];
         if (t == 0) a.offsets[a.experts] = total;
     }
 }
@@ -184,37 +246,83 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(const RouteAr
     for (int c0 = 0; c0 < a.chunks; c0 += kRouteThreads) {
         const int c = c0 + static_cast<int>(threadIdx.x);
         int total;
-        int32_t* const p = a.counts + static_cast<int64_t>(c) * a.experts + e;
+        int32_t* const p = a.counts + static_cast<int64_t>(c) * a.pitch + e;
         const int s = block_exclusive<kRouteThreads>(c < a.chunks ? *p : 0, lds, total);
         if (c < a.chunks) *p = base + s;
         base += total;
     }
-    if (threadIdx.x == 0) a.counts[static_cast<int64_t>(a.chunks) * a.experts + e] = base;
+    if (threadIdx.x == 0) a.counts[static_cast<int64_t>(a.chunks) * a.pitch + e] = base;
 }
 
-__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteArgs a) {
+// Rows of the routed order.  The chunks' counts are added up here (SCANNED: by route_scan_kernel): threads take four experts of
+// every so many-th chunk, and their sums meet in LDS.
+template <bool SCANNED>
+__global__ __launch_bounds__(kRouteMost) void route_place_kernel(const RouteArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     int* const count = reinterpret_cast<int*>(smem);
     int* const first = count + a.experts;
-    int* const lds = first + a.experts;
-    const int t = static_cast<int>(threadIdx.x), k = a.top_k;
-    for (int e = t; e < a.experts; e += kRouteThreads) count[e] = a.counts[static_cast<int64_t>(a.chunks) * a.experts + e];
+    int* const before = first + a.experts;                 // of earlier chunks
+    int* const lds = before + a.experts;
+    const int t = static_cast<int>(threadIdx.x), k = a.top_k, chunk = static_cast<int>(blockIdx.x);
+    const int64_t t0 = static_cast<int64_t>(chunk) * a.chunk_tokens;
+    const int tokens = a.tokens - t0 < a.chunk_tokens ? static_cast<int>(a.tokens - t0) : a.chunk_tokens;
+    // (a thread's first choice travels while the counts are added up)
+    const int my_expert = t < tokens * k ? a.expert[t0 * k + t] : -1, my_rank = t < tokens * k ? a.slot[t0 * k + t] : 0;
+    if (SCANNED) {
+        for (int e = t; e < a.experts; e += kRouteMost) {
+            count[e] = a.counts[static_cast<int64_t>(a.chunks) * a.pitch + e];
+            before[e] = a.counts[static_cast<int64_t>(chunk) * a.pitch + e];
+        }
+    } else {
+        for (int e = t; e < a.experts; e += kRouteMost) count[e] = before[e] = 0;
+        __syncthreads();
+        const int quads = a.pitch / 4, parts = kRouteMost / quads;         // (pitch: a power of two)
+        const int q = t & (quads - 1);
+        v4i all = {0, 0, 0, 0}, own = {0, 0, 0, 0};
+        constexpr int U = 8;           // loads in flight
+        for (int c0 = t / quads; c0 < a.chunks; c0 += parts * U) {
+            v4i n[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = c0 + u * parts;
+                n[u] = v4i{0, 0, 0, 0};
+                if (c < a.chunks) n[u] = *reinterpret_cast<const v4i*>(a.counts + static_cast<int64_t>(c) * a.pitch + q * 4);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                all += n[u];
+                if (c0 + u * parts < chunk) own += n[u];
+            }
+        }
+        // lanes of a wave with the same experts add up first
+        for (int d = quads; d < 64; d <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                all[i] += __shfl_xor(all[i], d, 64);
+                own[i] += __shfl_xor(own[i], d, 64);
+            }
+        if ((t & 63) < quads)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (q * 4 + i < a.experts) {
+                    if (all[i]) atomicAdd(count + q * 4 + i, all[i]);      // (whole numbers: no order)
+                    if (own[i]) atomicAdd(before + q * 4 + i, own[i]);
+                }
+    }
     __syncthreads();
-    const int total = first_rows(count, first, a.experts, lds);
+    const int total = first_rows<kRouteMost>(count, first, a.experts, lds);
     __syncthreads();
     if (blockIdx.x == 0) {
-        for (int e = t; e < a.experts; e += kRouteThreads) a.offsets[e] = first[e];
+        for (int e = t; e < a.experts; e += kRouteMost) a.offsets[e] = first[e];
         if (t == 0) a.offsets[a.experts] = total;
     }
-    for (int e = t; e < a.experts; e += kRouteThreads) first[e] += a.counts[static_cast<int64_t>(blockIdx.x) * a.experts + e];
+    for (int e = t; e < a.experts; e += kRouteMost) before[e] += first[e];
     __syncthreads();
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kRouteChunk;
-    const int tokens = a.tokens - t0 < kRouteChunk ? static_cast<int>(a.tokens - t0) : kRouteChunk;
-    for (int i = t; i < tokens * k; i += kRouteThreads) {
+    for (int i = t; i < tokens * k; i += kRouteMost) {
         const int64_t o = t0 * k + i;
-        const int e = a.expert[o];
+        const int e = i == t ? my_expert : a.expert[o];
         if (e >= 0) {
-            const int s = first[e] + a.slot[o];
+            const int s = before[e] + (i == t ? my_rank : a.slot[o]);
             a.slot[o] = s;
             a.row[s] = static_cast<int32_t>(t0 + i / k);
         }
@@ -227,7 +335,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteA
 //   softmax           q_e (g_e - sum_i g_i q_i), g_e = 0 where not chosen
 //   sigmoid, renorm   q_j (g_j - sum_i g_i q_i) (1 - s_j)            others 0
 //   sigmoid           g_j s_j (1 - s_j)                              others 0
-template <int L, int V, bool BF16>
+template <int L, int V, int R, bool BF16>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
     const int t = static_cast<int>(threadIdx.x), l = t % L, k = a.top_k;
     constexpr int PER = kRouteThreads / L;
@@ -242,9 +350,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     float lx[V], top = -INFINITY, all = 0.f;
     if (dense) {
         uint32_t m = 0;
+        load_logits<L, V, R, BF16>(a.logits, at, a.experts, l, lx);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            lx[v] = l + L * v < a.experts ? logit_at<BF16>(a.logits, at + l + L * v) : -INFINITY;
             const uint32_t key = key_of(lx[v]);
             m = key > m ? key : m;
         }
@@ -265,7 +373,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
         const float sum = a.renorm ? lanes_sum<L>(q) : all;
         q = mine >= 0 ? q / sum : 0.f;
         const float inner = lanes_sum<L>(g * q);
-        d = a.renorm ? q * (g - inner) : g * q;
+        d = q * (g - inner);
         if (dense)
 #pragma unroll
             for (int v = 0; v < V; ++v) lx[v] = lx[v] == 0.f ? 0.f : -(lx[v] / all) * inner;
@@ -289,33 +397,64 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
         const int e = __shfl(mine, j, L);
         const float dj = __shfl(d, j, L);
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (l + L * v == e) lx[v] += dj;
+        for (int v = 0; v < V; ++v) lx[v] = entry_of<L, R>(l, v) == e ? dj : lx[v];
     }
     if (!in) return;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (l + L * v < a.experts) {
-            const int64_t at_out = token * a.experts + l + L * v;
-            if (BF16) static_cast<uint16_t*>(a.dlogits)[at_out] = static_cast<uint16_t>(f32_to_bf16_rne(lx[v]));
-            else static_cast<float*>(a.dlogits)[at_out] = lx[v];
+    for (int b = 0; b < V; b += R) {
+        const int e = entry_of<L, R>(l, b);
+        if (e >= a.experts) continue;
+        const int64_t o = token * a.experts + e;
+        if constexpr (!BF16) {
+            float* const p = static_cast<float*>(a.dlogits) + o;
+            if constexpr (R == 4) *reinterpret_cast<v4f*>(p) = v4f{lx[b], lx[b + 1], lx[b + 2], lx[b + 3]};
+            else *p = lx[b];
+        } else {
+            uint16_t* const p = static_cast<uint16_t*>(a.dlogits) + o;
+            if constexpr (R == 8)
+                *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(lx[b], lx[b + 1]), pack_bf16x2(lx[b + 2], lx[b + 3]), pack_bf16x2(lx[b + 4], lx[b + 5]), pack_bf16x2(lx[b + 6], lx[b + 7])};
+            else if constexpr (R == 4) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(lx[b], lx[b + 1]), pack_bf16x2(lx[b + 2], lx[b + 3])};
+            else *p = static_cast<uint16_t>(f32_to_bf16_rne(lx[b]));
         }
+    }
 }
 
+static int route_pitch(int experts) {
+    int p = 4;
+    while (p < experts) p *= 2;
+    return p;
+}
+// Tokens of a workgroup: all of a small call's (one launch), else as few as leave 256 workgroups (each of which adds up the counts of all: 300
+// tokens of 160 experts, 6 choices, 17 -> 8.5 us against 128; 32768 of 256 would take longer on less).
+static int64_t route_chunk(const loka_route_desc* d) {
+    if (d->tokens <= 64) return 64;
+    int64_t c = 16;
+    while (c < kRouteMostChunk && d->tokens > 256 * c) c *= 2;
+    return c;
+}
 size_t route_workspace_bytes(const loka_route_desc* d) {
-    const int64_t chunks = (d->tokens + kRouteChunk - 1) / kRouteChunk;
-    return chunks > 1 ? static_cast<size_t>(chunks + 1) * static_cast<size_t>(d->experts) * 4 : 0;
+    const int64_t c = route_chunk(d), chunks = (d->tokens + c - 1) / c;
+    return chunks > 1 ? static_cast<size_t>(chunks + 1) * static_cast<size_t>(route_pitch(d->experts)) * 4 : 0;
 }
 
-// Lanes and logits a lane, by the number of experts
+// Lanes, logits a lane and their runs: by the number of experts, and in runs of 16 bytes (8 where a lane has four bf16) where rows are whole runs
 template <class F>
-static void by_experts(int experts, F&& f) {
+static void by_experts(const loka_route_desc* d, const void* logits, const void* dlogits, F&& f) {
+    auto with = [&](auto l, auto v) {
+        auto typed = [&](auto bf16) {
+            constexpr int run = bf16.value ? (v.value < 8 ? v.value : 8) : 4;
+            if (d->experts % run == 0 && d->ld % run == 0 && aligned16(logits) && aligned16(dlogits)) f(l, v, std::integral_constant<int, run>{}, bf16);
+            else f(l, v, std::integral_constant<int, 1>{}, bf16);
+        };
+        if (d->bf16) typed(std::true_type{});
+        else typed(std::false_type{});
+    };
     using std::integral_constant;
-    if (experts <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-    else if (experts <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-    else if (experts <= 256) f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-    else if (experts <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-    else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+    if (d->experts <= 64) with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    else if (d->experts <= 128) with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    else if (d->experts <= 256) with(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    else if (d->experts <= 512) with(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+    else with(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
 
 static RouteArgs args_of(const loka_route_desc* d, const void* logits) {
@@ -328,7 +467,9 @@ static RouteArgs args_of(const loka_route_desc* d, const void* logits) {
     a.score = d->score;
     a.renorm = d->renorm != 0;
     a.scale = d->scale;
-    a.chunks = static_cast<int>((d->tokens + kRouteChunk - 1) / kRouteChunk);
+    a.chunk_tokens = static_cast<int>(route_chunk(d));
+    a.chunks = static_cast<int>((d->tokens + a.chunk_tokens - 1) / a.chunk_tokens);
+    a.pitch = route_pitch(d->experts);
     return a;
 }
 
@@ -342,15 +483,21 @@ loka_status route_launch(const loka_route_desc* d, const void* logits, int32_t* 
     a.offsets = offsets;
     a.counts = static_cast<int32_t*>(ws);
     const size_t lds = static_cast<size_t>(d->experts) * 24 + 64;
-    by_experts(d->experts, [&](auto l, auto v) {
-        if (d->bf16) route_choose_kernel<l.value, v.value, true><<<a.chunks, kRouteThreads, lds, stream>>>(a);
-        else route_choose_kernel<l.value, v.value, false><<<a.chunks, kRouteThreads, lds, stream>>>(a);
+    by_experts(d, logits, nullptr, [&](auto l, auto v, auto r, auto bf16) {
+        if (std::min<int64_t>(a.chunk_tokens, d->tokens) * l.value <= kRouteThreads) route_choose_kernel<l.value, v.value, r.value, bf16.value, kRouteThreads><<<a.chunks, kRouteThreads, lds, stream>>>(a);
+        else route_choose_kernel<l.value, v.value, r.value, bf16.value, kRouteMost><<<a.chunks, kRouteMost, lds, stream>>>(a);
     });
     LOKA_HIP_TRY(hipGetLastError());
     if (a.chunks == 1) return LOKA_OK;
-    route_scan_kernel<<<d->experts, kRouteThreads, 0, stream>>>(a);
-    LOKA_HIP_TRY(hipGetLastError());
-    route_place_kernel<<<a.chunks, kRouteThreads, static_cast<size_t>(d->experts) * 8 + 64, stream>>>(a);
+    const size_t place = static_cast<size_t>(d->experts) * 12 + 64;
+    // A workgroup adds up every chunk's counts: chunks^2 of them in all
+    if (a.chunks <= 1024) {
+        route_place_kernel<false><<<a.chunks, kRouteMost, place, stream>>>(a);
+    } else {
+        route_scan_kernel<<<d->experts, kRouteThreads, 0, stream>>>(a);
+        LOKA_HIP_TRY(hipGetLastError());
+        route_place_kernel<true><<<a.chunks, kRouteMost, place, stream>>>(a);
+    }
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }
@@ -361,10 +508,9 @@ loka_status route_backward_launch(const loka_route_desc* d, const void* logits, 
     a.expert = const_cast<int32_t*>(expert);
     a.dweight = dweight;
     a.dlogits = dlogits;
-    by_experts(d->experts, [&](auto l, auto v) {
+    by_experts(d, logits, dlogits, [&](auto l, auto v, auto r, auto bf16) {
         const uint32_t grid = static_cast<uint32_t>((d->tokens * l.value + kRouteThreads - 1) / kRouteThreads);
-        if (d->bf16) route_backward_kernel<l.value, v.value, true><<<grid, kRouteThreads, 0, stream>>>(a);
-        else route_backward_kernel<l.value, v.value, false><<<grid, kRouteThreads, 0, stream>>>(a);
+        route_backward_kernel<l.value, v.value, r.value, bf16.value><<<grid, kRouteThreads, 0, stream>>>(a);
     });
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
