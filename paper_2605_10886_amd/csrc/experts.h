@@ -20,6 +20,9 @@ loka_status combine_backward_launch(const loka_combine_desc* d, const void* dout
 loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const void* x, const int32_t* index, const int32_t* offsets, uint8_t* q,
                                     float* scales, uint8_t* qt, float* st, hipStream_t stream);
 bool grouped_gemm_fits(const loka_grouped_desc* d);
+bool grouped_linear_fused(const loka_grouped_desc* d, bool gathered);
+loka_status grouped_linear_fused_launch(const loka_grouped_desc* d, const void* x, int64_t ld, const int32_t* index, const int32_t* offsets,
+                                        const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream);
 loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
                                 const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream);
 bool grouped_wgrad_fits(const loka_grouped_desc* d);
@@ -38,14 +41,14 @@ __device__ __forceinline__ GroupRows group_rows(const int32_t* offsets, int g, i
     const int a = lo < 0 ? 0 : lo > rows ? rows : lo, b = hi > rows ? rows : hi;
     return {a, b > a ? b - a : 0};
 }
-// inclusive sums over the wave's lanes
+// inclusive sums over the wave's lanes, by moves of the vector unit (a shuffle is an LDS round trip)
 __device__ __forceinline__ int lanes_inclusive(int v) {
-    const int lane = static_cast<int>(threadIdx.x) & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d, 64);
-        if (lane >= d) v += o;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);         // within 16 lanes: 1, 2, 4, 8 to the left
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);        // lane 15 to the second 16, lane 47 to the fourth
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);        // lane 31 to the upper half
     return v;
 }
 // Units of `unit` rows that all groups take (each its own), by a wave; uniform.
@@ -77,6 +80,24 @@ __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, 
 // Units of the groups before `group`, by a wave; uniform.
 __device__ __forceinline__ int units_before(const int32_t* offsets, int group, int rows, int unit) {
     return units_of_all(offsets, group, rows, unit);
+}
+// Scale and factor of 128 elements from the bits of their largest magnitude (a bf16's).  False where that is not finite: the scale is a NaN then,
+// the codes are zeros.
+__device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale, float& inv) {
+    group_scale_pow2(bf16_bits_to_f32(amax), scale, inv);
+    if (amax < 0x7F80u) return true;
+    scale = __uint_as_float(0x7FC00000u);
+    return false;
+}
+__device__ __forceinline__ uint32_t max_abs8(u32x4 v) {
+    uint32_t a = max_abs_bf16x2(v.x & 0x7FFF7FFFu, v.y);
+    a = max_abs_bf16x2(max_abs_bf16x2(a, v.z), v.w);
+    return max_of_halves(a);
+}
+__device__ __forceinline__ u32x2 gq_codes8(u32x4 v, float inv, bool finite) {
+    const u32x2 c{e4m3x4_finite(bf16_lo(v.x) * inv, bf16_hi(v.x) * inv, bf16_lo(v.y) * inv, bf16_hi(v.y) * inv),
+                  e4m3x4_finite(bf16_lo(v.z) * inv, bf16_hi(v.z) * inv, bf16_lo(v.w) * inv, bf16_hi(v.w) * inv)};
+    return finite ? c : u32x2{0u, 0u};
 }
 #endif
 

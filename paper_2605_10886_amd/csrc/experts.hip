@@ -87,12 +87,7 @@ struct RouteArgs {
 template <int THREADS>
 __device__ __forceinline__ int block_exclusive(int v, int* lds, int& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(s, d, 64);
-        if (lane >= d) s += o;
-    }
+    const int s = lanes_inclusive(v);
     if (lane == 63) lds[wave] = s;
     __syncthreads();
     int before = 0;

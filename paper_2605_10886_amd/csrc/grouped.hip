@@ -14,23 +14,6 @@ struct GqArgs {
     int groups, col_tiles;
 };
 
-// Scale and factor of a group of 128 from the bits of its largest magnitude (a bf16's): NaN, and a factor that is not used, where it is not finite
-__device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale, float& inv) {
-    group_scale_pow2(bf16_bits_to_f32(amax), scale, inv);
-    if (amax < 0x7F80u) return true;
-    scale = __uint_as_float(0x7FC00000u);
-    return false;
-}
-__device__ __forceinline__ uint32_t max_abs8(u32x4 v) {
-    uint32_t a = max_abs_bf16x2(v.x & 0x7FFF7FFFu, v.y);
-    a = max_abs_bf16x2(max_abs_bf16x2(a, v.z), v.w);
-    return max_of_halves(a);
-}
-__device__ __forceinline__ u32x2 gq_codes8(u32x4 v, float inv, bool finite) {
-    const u32x2 c{e4m3x4_finite(bf16_lo(v.x) * inv, bf16_hi(v.x) * inv, bf16_lo(v.y) * inv, bf16_hi(v.y) * inv),
-                  e4m3x4_finite(bf16_lo(v.z) * inv, bf16_hi(v.z) * inv, bf16_lo(v.w) * inv, bf16_hi(v.w) * inv)};
-    return finite ? c : u32x2{0u, 0u};
-}
 // the source row of row p, or -1: a row of zeros
 __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
     if (!a.index) return p;
@@ -38,26 +21,31 @@ __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
     return s >= 0 && s < a.x_rows ? s : -1;
 }
 
-// ALONG: 16 lanes take 128 elements of a row, 8 each.
+// ALONG: 16 lanes take 128 elements of a row, 8 each; U such blocks at a time, 16 blocks apart.  (One division, of 32 bits where they do.)
 template <int U>
 __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
     const int t = static_cast<int>(threadIdx.x), l = t & 15;
-    const int64_t nb = (a.cols + kGroupBlock - 1) / kGroupBlock;
+    const int nb = a.col_tiles;
     int64_t rows = a.rows;
     if (a.offsets) {
         const int last = a.offsets[a.groups];
         rows = last < 0 ? 0 : last < rows ? last : rows;
     }
     const int64_t total = rows * nb, first = (a.first_wg + blockIdx.x) * (16 * U) + (t >> 4);
+    int64_t row = first >> 32 ? first / nb : static_cast<int64_t>(static_cast<uint32_t>(first) / static_cast<uint32_t>(nb));
+    int b = static_cast<int>(first - row * nb);
+    const int step_row = 16 / nb, step_b = 16 - step_row * nb;
     u32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t unit = first + u * 16, row = unit / nb, c = (unit - row * nb) * kGroupBlock + l * 8;
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (unit < total) {
+        if (first + u * 16 < total) {
             const int64_t s = gq_source(a, row);
-            if (s >= 0) v[u] = mx_load8(a.x + s * a.ld, c, a.cols);
+            if (s >= 0) v[u] = mx_load8(a.x + s * a.ld, b * kGroupBlock + l * 8, a.cols);
         }
+        row += step_row;
+        b += step_b;
+        if (b >= nb) { b -= nb; ++row; }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -80,7 +68,8 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     __shared__ __align__(16) uint8_t codes[128 * 128];
     __shared__ __align__(16) u32x4 maxima[4][16];
     const int t = static_cast<int>(threadIdx.x), cg = t & 15, rg = t >> 4, wave = t >> 6;
-    const int64_t wg = a.first_wg + blockIdx.x, block = wg / a.col_tiles, ct = wg - block * a.col_tiles;
+    const int64_t wg = a.first_wg + blockIdx.x;
+    const int64_t block = wg >> 32 ? wg / a.col_tiles : static_cast<int64_t>(static_cast<uint32_t>(wg) / static_cast<uint32_t>(a.col_tiles)), ct = wg - block * a.col_tiles;
     int64_t row0;
     int count;
     if (a.offsets) {
@@ -90,7 +79,7 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
         row0 = at.first + skip;
         count = at.count - skip;
     } else {
-        const int64_t g = block / a.blocks_per_group, skip = (block - g * a.blocks_per_group) * kGroupBlock;
+        const int64_t g = static_cast<uint32_t>(block) / static_cast<uint32_t>(a.blocks_per_group), skip = (block - g * a.blocks_per_group) * kGroupBlock;
         row0 = g * a.per_group + skip;
         count = static_cast<int>(a.per_group - skip < kGroupBlock ? a.per_group - skip : kGroupBlock);
     }

@@ -22,6 +22,8 @@ struct GgArgs {
     int64_t x_row, x_step, sx_row, sx_step, w_row, w_step, w_group, sw_row, sw_step, sw_group;
     int tiles_n, tiles_m;              // (tiles_m: weight gradient)
     bool wide;                         // rows of whole 16-byte runs
+    const uint16_t* x;                 // few rows, quantized in the kernel: bf16 [x_rows, ldx]
+    int64_t ldx, K;
 };
 
 __device__ __forceinline__ v4f gg_mfma(const v8i a, const v8i b, v4f c, int sa, int sb) {
@@ -399,6 +401,150 @@ __global__ __launch_bounds__(64 * C::NW, C::NW * C::PER_CU / 4) void gg_tile_ker
 using GgLarge = GgTile<8, 4, 2, 4>;
 using GgSmall = GgTile<4, 4, 2, 2>;
 
+// ---------------------------------------------------------------------------------
+// Few rows a group: bound by the weights' traffic.  A workgroup of 8 waves owns 16 MT rows x 16 NT columns of a group; the waves take the
+// steps of the contraction in turn, straight from memory into registers, U of them in flight, and add their sums in LDS in wave order.
+// FUSED: X is quantized here: a lane holds 32 of a row's 128 elements, and the row's four lanes share the maximum.
+constexpr int kStreamWaves = 8;
+
+// the larger of the four lanes l % 16 + 0, 16, 32, 48, in all of them
+__device__ __forceinline__ uint32_t row_lanes_max(uint32_t v) {
+    u32_pair r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = r.x > r.y ? r.x : r.y;
+    r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return r.x > r.y ? r.x : r.y;
+}
+
+template <int MT, int NT, bool FUSED>
+__global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    v4f* const part = reinterpret_cast<v4f*>(smem);        // [wave][MT * NT][64]
+    constexpr int U = FUSED ? 2 : NT * MT >= 8 ? 1 : NT * MT >= 4 ? 2 : 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int u = static_cast<int>(blockIdx.x) / a.tiles_n, nt = static_cast<int>(blockIdx.x) - u * a.tiles_n;
+    const UnitAt at = find_unit(a.offsets, a.groups, a.rows, 16 * MT, u);
+    if (at.group < 0) return;
+    const int skip = (u - at.before) * (16 * MT), m_first = at.first + skip, m_count = at.count - skip;
+    const int64_t n0 = static_cast<int64_t>(nt) * (16 * NT);
+
+    // rows past the end read the last one; what they give is not written
+    const uint8_t *wp[NT], *xp[MT];
+    const float *swp[NT], *sxp[MT];
+    const uint16_t* xb[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int64_t n = n0 + j * 16 + r < a.N ? n0 + j * 16 + r : a.N - 1;
+        wp[j] = a.wq + at.group * a.w_group + n * a.w_row + g * 32;
+        swp[j] = a.sw + at.group * a.sw_group + n * a.sw_row;
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int m = m_first + (i * 16 + r < m_count ? i * 16 + r : m_count - 1);
+        int64_t s = a.index ? a.index[m] : m;
+        s = s < 0 ? 0 : s >= a.x_rows ? a.x_rows - 1 : s;
+        if (FUSED) {
+            xb[i] = a.x + s * a.ldx;
+        } else {
+            xp[i] = a.xq + s * a.x_row + g * 32;
+            sxp[i] = a.sx + s * a.sx_row;
+        }
+    }
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = wave; k0 < a.ksteps; k0 += kStreamWaves * U) {
+        v8i w[U][NT], x[U][MT];
+        int sw[U][NT], sx[U][MT];
+        u32x4 raw[FUSED ? U : 1][FUSED ? MT : 1][4];
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            // (steps past the last one: the last one again, with zeros for X)
+            const int k = k0 + q * kStreamWaves < a.ksteps ? k0 + q * kStreamWaves : a.ksteps - 1;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if constexpr (FUSED) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) raw[q][i][e] = mx_load8(xb[i], static_cast<int64_t>(k) * kGroupBlock + g * 32 + e * 8, a.K);
+                } else {
+                    const u32x4* p = reinterpret_cast<const u32x4*>(xp[i] + k * a.x_step);
+                    x[q][i] = join(p[0], p[1]);
+                    sx[q][i] = scale_byte(__float_as_uint(sxp[i][k * a.sx_step]));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const u32x4* p = reinterpret_cast<const u32x4*>(wp[j] + k * a.w_step);
+                w[q][j] = join(p[0], p[1]);
+                sw[q][j] = scale_byte(__float_as_uint(swp[j][k * a.sw_step]));
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            if (k0 + q * kStreamWaves >= a.ksteps) continue;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if constexpr (FUSED) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t o = max_abs8(raw[q][i][e]);
+                        m = o > m ? o : m;
+                    }
+                    float scale, inv;
+                    const bool finite = gq_scale(row_lanes_max(m), scale, inv);
+                    sx[q][i] = scale_byte(__float_as_uint(scale));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const u32x2 c = gq_codes8(raw[q][i][e], inv, finite);
+                        x[q][i][2 * e] = static_cast<int>(c.x);
+                        x[q][i][2 * e + 1] = static_cast<int>(c.y);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = gg_mfma(w[q][j], x[q][i], acc[i][j], sw[q][j], sx[q][i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) part[(wave * MT * NT + i * NT + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    // value (m, n) of tile (i, j) lies in lane (n % 16) / 4 * 16 + m % 16, component n % 4
+    for (int k = threadIdx.x; k < MT * NT * 64; k += 64 * kStreamWaves) {
+        const int tile = k >> 6, l = k & 63, m = (tile / NT) * 16 + (l & 15);
+        if (m >= m_count) continue;
+        v4f s = part[tile * 64 + l];
+#pragma unroll
+        for (int v = 1; v < kStreamWaves; ++v) s += part[(v * MT * NT + tile) * 64 + l];
+        const int64_t n = n0 + (tile % NT) * 16 + (l >> 4) * 4, o = static_cast<int64_t>(m_first + m) * a.N + n;
+        if (n + 4 <= a.N) {
+            if (a.out) *reinterpret_cast<u32x2_any*>(a.out + o) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
+            if (a.y) *reinterpret_cast<u32x4_any*>(a.y + o) = __builtin_bit_cast(u32x4, s);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < a.N) {
+                    if (a.out) a.out[o + e] = static_cast<uint16_t>(f32_to_bf16_rne(s[e]));
+                    if (a.y) a.y[o + e] = s[e];
+                }
+        }
+    }
+}
+
+template <int MT, int NT, bool FUSED>
+static loka_status stream_launch(GgArgs& a, hipStream_t stream) {
+    constexpr int LDS = kStreamWaves * MT * NT * 1024;
+    const int64_t some = a.rows < a.groups ? a.rows : a.groups;
+    a.tiles_n = static_cast<int>((a.N + 16 * NT - 1) / (16 * NT));
+    const int64_t grid = (a.rows + (16 * MT - 1) * some) / (16 * MT) * a.tiles_n;
+    gg_stream_kernel<MT, NT, FUSED><<<static_cast<uint32_t>(grid), 64 * kStreamWaves, LDS, stream>>>(a);
+    LOKA_HIP_TRY(hipGetLastError());
+    return LOKA_OK;
+}
+
 template <class C>
 static int64_t tiles_of(const loka_grouped_desc* d) {       // that the groups can take
     const int64_t some = d->rows < d->groups ? d->rows : d->groups;
@@ -424,12 +570,9 @@ static loka_status gg_launch(GgArgs& a, int64_t grid, hipStream_t stream) {
     return LOKA_OK;
 }
 
-loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
-                                const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream) {
+static GgArgs gemm_args(const loka_grouped_desc* d, const int32_t* index, const int32_t* offsets, const uint8_t* wq, const float* sw, void* out, float* y) {
     GgArgs a{};
     const int64_t kb = group_blocks(d->K), N = d->N;
-    a.xq = xq;
-    a.sx = sx;
     a.wq = wq;
     a.sw = sw;
     a.index = index;
@@ -437,6 +580,7 @@ loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, c
     a.out = static_cast<uint16_t*>(out);
     a.y = y;
     a.N = N;
+    a.K = d->K;
     a.rows = static_cast<int>(d->rows);
     a.x_rows = index ? static_cast<int>(d->x_rows) : a.rows;
     a.groups = d->groups;
@@ -452,8 +596,47 @@ loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, c
     a.sw_row = turned ? 1 : kb;
     a.sw_step = turned ? N : 1;
     a.sw_group = N * kb;
-    if (d->rows >= 192 * static_cast<int64_t>(d->groups) && N > 128) return gg_launch<GgLarge, false>(a, tiles_of<GgLarge>(d), stream);
-    return gg_launch<GgSmall, false>(a, tiles_of<GgSmall>(d), stream);
+    return a;
+}
+
+// What runs a product
+enum { GG_STREAM16 = 0, GG_STREAM32 = 1, GG_SMALL = 2, GG_LARGE = 3 };
+static int gemm_form(const loka_grouped_desc* d) {
+    const double rows = static_cast<double>(d->rows), some = static_cast<double>(d->rows < d->groups ? d->rows : d->groups), each = rows / some;
+    if (each <= 12.0) return GG_STREAM16;
+    if (each <= 24.0) return GG_STREAM32;
+    if (d->rows >= 192 * static_cast<int64_t>(d->groups) && d->N > 128) return GG_LARGE;
+    return GG_SMALL;
+}
+template <bool FUSED>
+static loka_status stream16(GgArgs& a, hipStream_t stream) {
+    const int64_t some = a.rows < a.groups ? a.rows : a.groups, runs = some * ((a.N + 15) / 16);
+    if (runs >= 2048) return stream_launch<1, 4, FUSED>(a, stream);
+    if (runs >= 1024) return stream_launch<1, 2, FUSED>(a, stream);
+    return stream_launch<1, 1, FUSED>(a, stream);
+}
+
+loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
+                                const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream) {
+    GgArgs a = gemm_args(d, index, offsets, wq, sw, out, y);
+    a.xq = xq;
+    a.sx = sx;
+    switch (gemm_form(d)) {
+        case GG_STREAM16: return stream16<false>(a, stream);
+        case GG_STREAM32: return stream_launch<2, 2, false>(a, stream);
+        case GG_LARGE: return gg_launch<GgLarge, false>(a, tiles_of<GgLarge>(d), stream);
+        default: return gg_launch<GgSmall, false>(a, tiles_of<GgSmall>(d), stream);
+    }
+}
+
+bool grouped_linear_fused(const loka_grouped_desc* d, bool) { return gemm_form(d) == GG_STREAM16; }
+
+loka_status grouped_linear_fused_launch(const loka_grouped_desc* d, const void* x, int64_t ld, const int32_t* index, const int32_t* offsets,
+                                        const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream) {
+    GgArgs a = gemm_args(d, index, offsets, wq, sw, out, y);
+    a.x = static_cast<const uint16_t*>(x);
+    a.ldx = ld;
+    return stream16<true>(a, stream);
 }
 
 size_t grouped_wgrad_workspace_bytes(const loka_grouped_desc*) { return 0; }
