@@ -71,6 +71,7 @@ __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, 
             const int l = __builtin_ctzll(past), before = base + __builtin_amdgcn_readlane(s - n, l);
             // (always so, unless groups that overlap have made the sums overflow: then the unit is nobody's)
             const bool inside = target >= before && target - before < __builtin_amdgcn_readlane(n, l);
+            // (as scalars: addresses that follow from them are)
             return {inside ? g0 + l : -1, before, __builtin_amdgcn_readlane(r.first, l), __builtin_amdgcn_readlane(r.count, l)};
         }
         base += __builtin_amdgcn_readlane(s, 63);

@@ -416,8 +416,7 @@ __device__ __forceinline__ uint32_t row_lanes_max(uint32_t v) {
 }
 
 template <int MT, int NT, bool FUSED>
-__global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgArgs a) {
-    extern __shared__ __align__(16) uint8_t smem[];
+__device__ __forceinline__ void gg_stream(const GgArgs& a, uint8_t* smem) {
     v4f* const part = reinterpret_cast<v4f*>(smem);        // [wave][MT * NT][64]
     constexpr int U = FUSED ? 2 : NT * MT >= 8 ? 1 : NT * MT >= 4 ? 2 : 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
@@ -427,16 +426,14 @@ __global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgAr
     const int skip = (u - at.before) * (16 * MT), m_first = at.first + skip, m_count = at.count - skip;
     const int64_t n0 = static_cast<int64_t>(nt) * (16 * NT);
 
-    // rows past the end read the last one; what they give is not written
-    const uint8_t *wp[NT], *xp[MT];
-    const float *swp[NT], *sxp[MT];
+    // rows past the end: of W zeros, of X the last one; what they give is not written
+    const int n_count = a.N - n0 < 16 * NT ? static_cast<int>(a.N - n0) : 16 * NT, w_row = static_cast<int>(a.w_row), sw_row = static_cast<int>(a.sw_row) * 4;
+    const uint8_t* const wp = a.wq + at.group * a.w_group + n0 * a.w_row;
+    const float* const swp = a.sw + at.group * a.sw_group + n0 * a.sw_row;
+    const int w_lane = r * w_row + g * 32, sw_lane = r * sw_row, w_bytes = (n_count - 1) * w_row + 128, sw_bytes = (n_count - 1) * sw_row + 4;
+    const uint8_t* xp[MT];
+    const float* sxp[MT];
     const uint16_t* xb[MT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int64_t n = n0 + j * 16 + r < a.N ? n0 + j * 16 + r : a.N - 1;
-        wp[j] = a.wq + at.group * a.w_group + n * a.w_row + g * 32;
-        swp[j] = a.sw + at.group * a.sw_group + n * a.sw_row;
-    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int m = m_first + (i * 16 + r < m_count ? i * 16 + r : m_count - 1);
@@ -454,14 +451,15 @@ __global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgAr
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int k0 = wave; k0 < a.ksteps; k0 += kStreamWaves * U) {
-        v8i w[U][NT], x[U][MT];
-        int sw[U][NT], sx[U][MT];
-        u32x4 raw[FUSED ? U : 1][FUSED ? MT : 1][4];
+    // steps k0, k0 + 8, ... of the contraction, so many at a time
+    auto steps = [&](int k0, auto n) __attribute__((always_inline)) {
+        constexpr int S = n.value;
+        v8i w[S][NT], x[S][MT];
+        int sw[S][NT], sx[S][MT];
+        u32x4 raw[FUSED ? S : 1][FUSED ? MT : 1][4];
 #pragma unroll
-        for (int q = 0; q < U; ++q) {
-            // (steps past the last one: the last one again, with zeros for X)
-            const int k = k0 + q * kStreamWaves < a.ksteps ? k0 + q * kStreamWaves : a.ksteps - 1;
+        for (int q = 0; q < S; ++q) {
+            const int k = k0 + q * kStreamWaves;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 if constexpr (FUSED) {
@@ -473,16 +471,17 @@ __global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgAr
                     sx[q][i] = scale_byte(__float_as_uint(sxp[i][k * a.sx_step]));
                 }
             }
+            const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wp + k * a.w_step), 0, w_bytes, 0x00020000);
+            const __amdgpu_buffer_rsrc_t swr = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(swp + k * a.sw_step), 0, sw_bytes, 0x00020000);
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const u32x4* p = reinterpret_cast<const u32x4*>(wp[j] + k * a.w_step);
-                w[q][j] = join(p[0], p[1]);
-                sw[q][j] = scale_byte(__float_as_uint(swp[j][k * a.sw_step]));
+                const u32x4 lo = __builtin_amdgcn_raw_buffer_load_b128(wr, w_lane, j * 16 * w_row, 0), hi = __builtin_amdgcn_raw_buffer_load_b128(wr, w_lane + 16, j * 16 * w_row, 0);
+                w[q][j] = join(lo, hi);
+                sw[q][j] = scale_byte(__builtin_amdgcn_raw_buffer_load_b32(swr, sw_lane, j * 16 * sw_row, 0));
             }
         }
 #pragma unroll
-        for (int q = 0; q < U; ++q) {
-            if (k0 + q * kStreamWaves >= a.ksteps) continue;
+        for (int q = 0; q < S; ++q) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 if constexpr (FUSED) {
@@ -506,7 +505,11 @@ __global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgAr
                 for (int j = 0; j < NT; ++j) acc[i][j] = gg_mfma(w[q][j], x[q][i], acc[i][j], sw[q][j], sx[q][i]);
             }
         }
-    }
+    };
+    int k0 = wave;
+    if constexpr (U > 1)
+        for (; k0 + (U - 1) * kStreamWaves < a.ksteps; k0 += U * kStreamWaves) steps(k0, std::integral_constant<int, U>{});
+    for (; k0 < a.ksteps; k0 += kStreamWaves) steps(k0, std::integral_constant<int, 1>{});
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -532,6 +535,13 @@ __global__ __launch_bounds__(64 * kStreamWaves) void gg_stream_kernel(const GgAr
                 }
         }
     }
+}
+
+// (512 threads, 4 waves on a SIMD: 128 registers, so that two workgroups share a CU)
+template <int MT, int NT, bool FUSED>
+__global__ __launch_bounds__(64 * kStreamWaves, 4) void gg_stream_kernel(const GgArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    gg_stream<MT, NT, FUSED>(a, smem);
 }
 
 template <int MT, int NT, bool FUSED>
