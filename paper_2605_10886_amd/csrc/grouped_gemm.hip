@@ -7,6 +7,8 @@
 #include "experts.h"
 #include "gemm_common.h"
 
+#include <cmath>
+
 namespace loka {
 
 struct GgArgs {
@@ -609,14 +611,21 @@ static GgArgs gemm_args(const loka_grouped_desc* d, const int32_t* index, const 
     return a;
 }
 
-// What runs a product
+// What runs a product.  How the rows spread over the groups is not known here: tiles are counted as if every group left half a tile empty.
+// Microseconds fitted to launches (rows x groups x K x N, measured / estimated): large tiles 3000 x 4 x 512 x 1024 14.4 / 15.5, 3000 x 4 x 4096 x 1024 50 / 51,
+// 10026 x 23 x 1008 x 720 21.7 / 20.5; small ones 3000 x 4 x 512 x 1024 8.0 / 9.2, 3000 x 4 x 2048 x 1024 16.2 / 15.8, 12000 x 4 x 1024 x 1024 25.8 / 24.5,
+// 12000 x 4 x 4096 x 1024 74 / 73 (large 53 / 51).
 enum { GG_STREAM16 = 0, GG_STREAM32 = 1, GG_SMALL = 2, GG_LARGE = 3 };
+static int tile_form(double large, double small, double steps) {
+    const double us_large = 7.5 + std::ceil(large / 256) * (3.0 + 1.25 * steps), us_small = 5.5 + std::ceil(small / 512) * (1.5 + (small <= 256 ? 0.55 : 1.0) * steps);
+    return us_large < us_small ? GG_LARGE : GG_SMALL;
+}
 static int gemm_form(const loka_grouped_desc* d) {
     const double rows = static_cast<double>(d->rows), some = static_cast<double>(d->rows < d->groups ? d->rows : d->groups), each = rows / some;
     if (each <= 12.0) return GG_STREAM16;
     if (each <= 24.0) return GG_STREAM32;
-    if (d->rows >= 192 * static_cast<int64_t>(d->groups) && d->N > 128) return GG_LARGE;
-    return GG_SMALL;
+    auto tiles = [&](double b) { return std::fmax(some, rows / b + some / 2) * std::ceil(static_cast<double>(d->N) / b); };
+    return tile_form(tiles(256), tiles(128), std::ceil(static_cast<double>(d->K) / kGroupBlock));
 }
 template <bool FUSED>
 static loka_status stream16(GgArgs& a, hipStream_t stream) {
@@ -672,7 +681,9 @@ loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, 
     a.sx_row = a.sw_row = 1;
     a.sx_step = d->K;
     a.sw_step = d->N;
-    if (d->K > 128 && d->N > 128 && wgrad_tiles_of<GgLarge>(d) >= 256) return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
+    const double steps = std::ceil(static_cast<double>(d->rows) / static_cast<double>(d->groups) / kGroupBlock + 0.5);
+    if (tile_form(static_cast<double>(wgrad_tiles_of<GgLarge>(d)), static_cast<double>(wgrad_tiles_of<GgSmall>(d)), steps) == GG_LARGE)
+        return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
     return gg_launch<GgSmall, true>(a, wgrad_tiles_of<GgSmall>(d), stream);
 }
 
