@@ -512,23 +512,28 @@ loka_status route_backward_launch(const loka_route_desc* d, const void* logits, 
 }
 
 // ---------------------------------------------------------------------------------
-// The sum of a token's results.  A lane takes 8 columns of a token; bytes only.
+// The sum of a token's results, and its gradients.  A lane takes 8 columns of a token; bytes only, so a token's rows (K of them at
+// most) are all requested before the first is used.  Tokens of more than 256 columns: a wave takes 512 of them, and its token's slots and weights are
+// scalars; narrower ones share a wave, 2^lg lanes each.
 struct CombineArgs {
     const uint16_t *y, *residual, *dout;
     const int32_t* slot;
     const float* weight;
     uint16_t *out, *dy;
     float* dweight;
-    int64_t tokens, cols, rows;
-    int64_t runs;                      // of 8 columns of a token
-    int64_t first_wg;
-    int top_k;
+    int64_t tokens, cols, rows, first_wg;
+    int segments;                      // of 512 columns of a token
+    int top_k, lg;
 };
 
 // Eight columns from c on; a row may start anywhere
+template <bool STREAMED>
 __device__ __forceinline__ void store8(uint16_t* row, int64_t c, int64_t cols, u32x4 v) {
-    if (c + 8 <= cols) { *reinterpret_cast<u32x4_any*>(row + c) = v; return; }
-#pragma unroll
+    if (c + 8 <= cols) {
+        if (STREAMED) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(row + c));
+        else *reinterpret_cast<u32x4_any*>(row + c) = v;
+        return;
+    }
     for (int e = 0; e < 8; ++e)
         if (c + e < cols) row[c + e] = static_cast<uint16_t>(v[e >> 1] >> ((e & 1) * 16));
 }
@@ -542,62 +547,140 @@ __device__ __forceinline__ void widen(u32x4 v, float (&f)[8]) {
 __device__ __forceinline__ u32x4 narrow(const float (&f)[8]) {
     return u32x4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
 }
-
-__global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
-    const int64_t i = (a.first_wg + blockIdx.x) * 256 + threadIdx.x;
-    const int64_t t = i / a.runs, c = (i - t * a.runs) * 8;
-    if (t >= a.tokens) return;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.top_k; ++j) {
-        const int64_t slot = a.slot[t * a.top_k + j];
-        if (slot < 0 || slot >= a.rows) continue;
-        const float w = a.weight ? a.weight[t * a.top_k + j] : 1.f;
-        float f[8];
-        widen(mx_load8(a.y + slot * a.cols, c, a.cols), f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = fmaf(w, f[e], s[e]);
+// Eight columns of a row from c on, zeros behind the last: whole runs by one load, from the row's last eight where the row's end cuts
+template <bool STREAMED>
+__device__ __forceinline__ u32x4 load8(const uint16_t* row, int64_t c, int64_t cols) {
+    if (c + 8 <= cols) {
+        if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(row + c));
+        return *reinterpret_cast<const u32x4_any*>(row + c);
     }
+    return mx_load8(row, c, cols);
+}
+
+// Slots (-1: none) and weights of token t
+template <int K, bool WAVE>
+__device__ __forceinline__ void choices(const CombineArgs& a, int64_t t, int64_t (&slot)[K], float (&w)[K]) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        int s = -1;
+        float f = 0.f;
+        if (j < a.top_k) {
+            s = a.slot[t * a.top_k + j];
+            f = a.weight ? a.weight[t * a.top_k + j] : 1.f;
+        }
+        if (WAVE) s = __builtin_amdgcn_readfirstlane(s);
+        slot[j] = s < 0 || s >= a.rows ? -1 : s;
+        w[j] = f;
+    }
+}
+template <bool WAVE>
+__device__ __forceinline__ int64_t my_token(const CombineArgs& a, int64_t& c) {
+    const int64_t wg = a.first_wg + blockIdx.x;
+    if (!WAVE) {
+        c = (static_cast<int>(threadIdx.x) & ((1 << a.lg) - 1)) * 8;
+        return (wg * 256 + threadIdx.x) >> a.lg;
+    }
+    const int64_t unit = wg * 4 + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    const int64_t t = unit >> 32 ? unit / a.segments : static_cast<int64_t>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(a.segments));
+    c = (unit - t * a.segments) * 512 + (threadIdx.x & 63) * 8;
+    return t;
+}
+
+template <int K, bool WAVE, bool STREAMED>
+__global__ __launch_bounds__(256) void combine_kernel(const CombineArgs a) {
+    int64_t c;
+    const int64_t t = my_token<WAVE>(a, c);
+    if (t >= a.tokens) return;
+    int64_t slot[K];
+    float w[K];
+    choices<K, WAVE>(a, t, slot, w);
+    if (c >= a.cols) return;
+    u32x4 v[K], res = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        v[j] = u32x4{0u, 0u, 0u, 0u};
+        if (slot[j] >= 0) v[j] = load8<STREAMED>(a.y + slot[j] * a.cols, c, a.cols);
+    }
+    if (a.residual) res = load8<STREAMED>(a.residual + t * a.cols, c, a.cols);
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, f[8];
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        if (slot[j] >= 0) {
+            widen(v[j], f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = fmaf(w[j], f[e], s[e]);
+        }
     if (a.residual) {
-        float f[8];
-        widen(mx_load8(a.residual + t * a.cols, c, a.cols), f);
+        widen(res, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] += f[e];
     }
-    store8(a.out + t * a.cols, c, a.cols, narrow(s));
+    store8<false>(a.out + t * a.cols, c, a.cols, narrow(s));
 }
 
-// A workgroup takes a token, so that its threads' parts of dweight meet in it.
+// WAVE: a workgroup takes a token, 2048 columns at a time, so that its threads' parts of dweight meet in it; else 2^lg lanes do.
+template <int K, bool WAVE, bool STREAMED>
 __global__ __launch_bounds__(256) void combine_backward_kernel(const CombineArgs a) {
-    __shared__ float part[4][16];
+    __shared__ float part[4][K];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t t = a.first_wg + blockIdx.x;
-    for (int j = 0; j < a.top_k; ++j) {
-        const int64_t slot = a.slot[t * a.top_k + j];
-        const bool live = slot >= 0 && slot < a.rows;
-        const float w = a.weight ? a.weight[t * a.top_k + j] : 1.f;
-        float sum = 0.f;
-        if (live)
-            for (int64_t c = threadIdx.x * 8; c < a.cols; c += 2048) {
-                float d[8], o[8];
-                widen(mx_load8(a.dout + t * a.cols, c, a.cols), d);
-                if (a.dweight) {
-                    float f[8];
-                    widen(mx_load8(a.y + slot * a.cols, c, a.cols), f);
+    const int64_t first = WAVE ? a.first_wg + blockIdx.x : ((a.first_wg + blockIdx.x) * 256 + threadIdx.x) >> a.lg;
+    const bool in = first < a.tokens;
+    const int64_t t = in ? first : a.tokens - 1;
+    int64_t slot[K];
+    float w[K], sum[K];
+    choices<K, WAVE>(a, t, slot, w);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum = fmaf(d[e], f[e], sum);
-                }
-                if (a.dy) {
+    for (int j = 0; j < K; ++j) sum[j] = 0.f;
+    const int64_t c0 = WAVE ? threadIdx.x * 8 : (threadIdx.x & ((1 << a.lg) - 1)) * 8;
+    if (in)
+        for (int64_t c = c0; c < a.cols; c += 2048) {
+            u32x4 v[K];
+            const u32x4 dv = load8<STREAMED>(a.dout + t * a.cols, c, a.cols);
+            if (a.dweight)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = w * d[e];
-                    store8(a.dy + slot * a.cols, c, a.cols, narrow(o));
+                for (int j = 0; j < K; ++j) {
+                    v[j] = u32x4{0u, 0u, 0u, 0u};
+                    if (slot[j] >= 0) v[j] = load8<STREAMED>(a.y + slot[j] * a.cols, c, a.cols);
                 }
-            }
-        sum = lanes_sum<64>(sum);
-        if (lane == 0) part[wave][j] = sum;
+            float d[8], f[8];
+            widen(dv, d);
+            if (a.dy)
+#pragma unroll
+                for (int j = 0; j < K; ++j)
+                    if (slot[j] >= 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = w[j] * d[e];
+                        store8<STREAMED>(a.dy + slot[j] * a.cols, c, a.cols, narrow(f));
+                    }
+            if (a.dweight)
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
+                    widen(v[j], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[j] = fmaf(d[e], f[e], sum[j]);
+                }
+        }
+    if (!a.dweight) return;
+    if (WAVE) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            sum[j] = lanes_sum<64>(sum[j]);
+            if (lane == 0) part[wave][j] = sum[j];
+        }
+        __syncthreads();
+        const int j = static_cast<int>(threadIdx.x);
+        // (a dead choice has no row: its sum is of zeros, unless dout is not finite)
+        if (j < a.top_k) {
+            const int s = a.slot[t * a.top_k + j];
+            a.dweight[t * a.top_k + j] = s < 0 || s >= a.rows ? 0.f : (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            for (int m = 1; m < (1 << a.lg); m <<= 1) sum[j] += __shfl_xor(sum[j], m, 64);
+            if (in && j < a.top_k && (threadIdx.x & ((1 << a.lg) - 1)) == 0) a.dweight[t * a.top_k + j] = slot[j] < 0 ? 0.f : sum[j];
+        }
     }
-    __syncthreads();
-    const int j = static_cast<int>(threadIdx.x);
-    if (a.dweight && j < a.top_k) a.dweight[t * a.top_k + j] = (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
 }
 
 static CombineArgs args_of(const loka_combine_desc* d, const int32_t* slot, const float* weight) {
@@ -608,8 +691,25 @@ static CombineArgs args_of(const loka_combine_desc* d, const int32_t* slot, cons
     a.cols = d->cols;
     a.rows = d->rows;
     a.top_k = d->top_k;
-    a.runs = (d->cols + 7) / 8;
+    a.segments = static_cast<int>((d->cols + 511) / 512);
+    while ((8 << a.lg) < d->cols) ++a.lg;
     return a;
+}
+// f(K, WAVE, STREAMED) for a call whose matrices of tokens * top_k rows have `cols` columns.  Results of 2^27 elements and more, which the 256 MB of last-level cache
+// cannot hold, pass it by.
+template <class F>
+static loka_status by_choices(const loka_combine_desc* d, F&& f) {
+    using std::integral_constant;
+    const bool streamed = d->tokens * d->top_k * d->cols >= INT64_C(1) << 27;
+    auto with = [&](auto k) {
+        if (d->cols <= 256) return f(k, std::false_type{}, std::false_type{});
+        return streamed ? f(k, std::true_type{}, std::true_type{}) : f(k, std::true_type{}, std::false_type{});
+    };
+    if (d->top_k <= 1) return with(integral_constant<int, 1>{});
+    if (d->top_k <= 2) return with(integral_constant<int, 2>{});
+    if (d->top_k <= 4) return with(integral_constant<int, 4>{});
+    if (d->top_k <= 8) return with(integral_constant<int, 8>{});
+    return with(integral_constant<int, 16>{});
 }
 
 loka_status combine_launch(const loka_combine_desc* d, const void* y, const int32_t* slot, const float* weight, const void* residual,
@@ -618,9 +718,12 @@ loka_status combine_launch(const loka_combine_desc* d, const void* y, const int3
     a.y = static_cast<const uint16_t*>(y);
     a.residual = static_cast<const uint16_t*>(residual);
     a.out = static_cast<uint16_t*>(out);
-    return in_launches((a.tokens * a.runs + 255) / 256, 256, [&](int64_t from, uint32_t grid) {
-        a.first_wg = from;
-        combine_kernel<<<grid, 256, 0, stream>>>(a);
+    return by_choices(d, [&](auto k, auto wave, auto streamed) {
+        const int64_t groups = wave.value ? (a.tokens * a.segments + 3) / 4 : ((a.tokens << a.lg) + 255) / 256;
+        return in_launches(groups, 256, [&](int64_t from, uint32_t grid) {
+            a.first_wg = from;
+            combine_kernel<k.value, wave.value, streamed.value><<<grid, 256, 0, stream>>>(a);
+        });
     });
 }
 
@@ -631,9 +734,12 @@ loka_status combine_backward_launch(const loka_combine_desc* d, const void* dout
     a.y = static_cast<const uint16_t*>(y);
     a.dy = static_cast<uint16_t*>(dy);
     a.dweight = dweight;
-    return in_launches(a.tokens, 256, [&](int64_t from, uint32_t grid) {
-        a.first_wg = from;
-        combine_backward_kernel<<<grid, 256, 0, stream>>>(a);
+    return by_choices(d, [&](auto k, auto wave, auto streamed) {
+        const int64_t groups = wave.value ? a.tokens : ((a.tokens << a.lg) + 255) / 256;
+        return in_launches(groups, 256, [&](int64_t from, uint32_t grid) {
+            a.first_wg = from;
+            combine_backward_kernel<k.value, wave.value, streamed.value><<<grid, 256, 0, stream>>>(a);
+        });
     });
 }
 

@@ -22,7 +22,8 @@ __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
 }
 
 // ALONG: 16 lanes take 128 elements of a row, 8 each; U such blocks at a time, 16 blocks apart.  (One division, of 32 bits where they do.)
-template <int U>
+// WHOLE: no run of 8 is cut by a row's end.
+template <int U, bool WHOLE>
 __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
     const int t = static_cast<int>(threadIdx.x), l = t & 15;
     const int nb = a.col_tiles;
@@ -41,7 +42,12 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
         if (first + u * 16 < total) {
             const int64_t s = gq_source(a, row);
-            if (s >= 0) v[u] = mx_load8(a.x + s * a.ld, b * kGroupBlock + l * 8, a.cols);
+            const int c = b * kGroupBlock + l * 8;
+            if (WHOLE) {
+                if (s >= 0 && c < a.cols) v[u] = *reinterpret_cast<const u32x4_any*>(a.x + s * a.ld + c);
+            } else if (s >= 0) {
+                v[u] = mx_load8(a.x + s * a.ld, c, a.cols);
+            }
         }
         row += step_row;
         b += step_b;
@@ -67,6 +73,7 @@ template <bool ALONG>
 __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     __shared__ __align__(16) uint8_t codes[128 * 128];
     __shared__ __align__(16) u32x4 maxima[4][16];
+    __shared__ __align__(16) int source[128];              // rows of x, -1 for zeros
     const int t = static_cast<int>(threadIdx.x), cg = t & 15, rg = t >> 4, wave = t >> 6;
     const int64_t wg = a.first_wg + blockIdx.x;
     const int64_t block = wg >> 32 ? wg / a.col_tiles : static_cast<int64_t>(static_cast<uint32_t>(wg) / static_cast<uint32_t>(a.col_tiles)), ct = wg - block * a.col_tiles;
@@ -84,15 +91,30 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
         count = static_cast<int>(a.per_group - skip < kGroupBlock ? a.per_group - skip : kGroupBlock);
     }
     if (count > kGroupBlock) count = kGroupBlock;
+    if (t < 128) source[t] = t < count ? static_cast<int>(gq_source(a, row0 + t)) : -1;
+    __syncthreads();
     const int64_t c = ct * 128 + cg * 8;
     u32x4 v[8];
+    {
+        // (a run that the row's end cuts comes from the row's last eight)
+        const bool few = a.cols < 8;
+        const int64_t at = c + 8 <= a.cols || few ? c : a.cols - 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = u32x4{0u, 0u, 0u, 0u};
-        const int r = rg * 8 + i;
-        if (r < count) {
-            const int64_t s = gq_source(a, row0 + r);
-            if (s >= 0) v[i] = mx_load8(a.x + s * a.ld, c, a.cols);
+        for (int i = 0; i < 8; ++i) {
+            const int64_t s = source[rg * 8 + i];
+            v[i] = u32x4{0u, 0u, 0u, 0u};
+            if (s >= 0 && !few) v[i] = *reinterpret_cast<const u32x4_any*>(a.x + s * a.ld + at);
+        }
+        if (ct * 128 + 128 > a.cols) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (few) {
+                    const int64_t s = source[rg * 8 + i];
+                    if (s >= 0) v[i] = mx_load8(a.x + s * a.ld, c, a.cols);
+                } else {
+                    v[i] = mx_from(v[i], c - at);
+                }
+            }
         }
     }
     u32x4 m = {0u, 0u, 0u, 0u};
@@ -174,11 +196,18 @@ loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const v
     a.per_group = d->rows / d->groups;
     a.blocks_per_group = group_blocks(a.per_group);
     if (!qt) {
-        constexpr int U = 4;
-        return in_launches((d->rows * a.col_tiles + 16 * U - 1) / (16 * U), 256, [&](int64_t from, uint32_t grid) {
-            a.first_wg = from;
-            gq_along_kernel<U><<<grid, 256, 0, stream>>>(a);
-        });
+        // (blocks a thread: 4 in flight where there are many, 1 where that leaves CUs idle: 5013 x 1008 7.4 -> U1 us)
+        const int64_t units = d->rows * a.col_tiles;
+        auto go = [&](auto u, auto whole) {
+            return in_launches((units + 16 * u.value - 1) / (16 * u.value), 256, [&](int64_t from, uint32_t grid) {
+                a.first_wg = from;
+                gq_along_kernel<u.value, whole.value><<<grid, 256, 0, stream>>>(a);
+            });
+        };
+        const bool many = units >= 131072;
+        using std::integral_constant;
+        if (d->cols % 8 == 0) return many ? go(integral_constant<int, 4>{}, std::true_type{}) : go(integral_constant<int, 1>{}, std::true_type{});
+        return many ? go(integral_constant<int, 4>{}, std::false_type{}) : go(integral_constant<int, 1>{}, std::false_type{});
     }
     const int64_t blocks = offsets ? loka_grouped_blocks(d->rows, d->groups) : a.blocks_per_group * d->groups;
     return in_launches(blocks * a.col_tiles, 256, [&](int64_t from, uint32_t grid) {
