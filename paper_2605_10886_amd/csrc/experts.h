@@ -82,9 +82,9 @@ __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, 
 __device__ __forceinline__ int units_before(const int32_t* offsets, int group, int rows, int unit) {
     return units_of_all(offsets, group, rows, unit);
 }
-// Scale and factor of 128 elements from the bits of their largest magnitude (a bf16's).  False where that is not finite: the scale is a NaN then,
-// the codes are zeros.
-__device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale, float& inv) {
+// Scale of 128 elements from the bits of their largest magnitude (a bf16's).  False where that is not finite: the scale is a NaN then, the codes are zeros.
+__device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale) {
+    float inv;
     group_scale_pow2(bf16_bits_to_f32(amax), scale, inv);
     if (amax < 0x7F80u) return true;
     scale = __uint_as_float(0x7FC00000u);
@@ -95,9 +95,16 @@ __device__ __forceinline__ uint32_t max_abs8(u32x4 v) {
     a = max_abs_bf16x2(max_abs_bf16x2(a, v.z), v.w);
     return max_of_halves(a);
 }
-__device__ __forceinline__ u32x2 gq_codes8(u32x4 v, float inv, bool finite) {
-    const u32x2 c{e4m3x4_finite(bf16_lo(v.x) * inv, bf16_hi(v.x) * inv, bf16_lo(v.y) * inv, bf16_hi(v.y) * inv),
-                  e4m3x4_finite(bf16_lo(v.z) * inv, bf16_hi(v.z) * inv, bf16_lo(v.w) * inv, bf16_hi(v.w) * inv)};
+// Four elements (two words of two bf16) as codes: the instruction divides by the power of two exactly and rounds to nearest even; no quotient exceeds 448.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t gq_codes4(uint32_t a, uint32_t b, float scale) {
+    s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, bf16_pair(a), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, bf16_pair(b), scale, true);
+    return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ u32x2 gq_codes8(u32x4 v, float scale, bool finite) {
+    const u32x2 c{gq_codes4(v.x, v.y, scale), gq_codes4(v.z, v.w, scale)};
     return finite ? c : u32x2{0u, 0u};
 }
 #endif

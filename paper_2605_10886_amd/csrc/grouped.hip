@@ -56,9 +56,9 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t unit = first + u * 16;
-        float scale, inv;
-        const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[u])), scale, inv);
-        const u32x2 c = gq_codes8(v[u], inv, finite);
+        float scale;
+        const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[u])), scale);
+        const u32x2 c = gq_codes8(v[u], scale, finite);
         if (unit < total) {
             *reinterpret_cast<u32x2*>(a.q + unit * kGroupBlock + l * 8) = c;
             if (l == 0) a.scales[unit] = scale;
@@ -132,12 +132,12 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
         const int64_t kb = (a.cols + kGroupBlock - 1) / kGroupBlock;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float scale, inv;
-            const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[i])), scale, inv);
+            float scale;
+            const bool finite = gq_scale(lanes_max_bits<16>(max_abs8(v[i])), scale);
             const int r = rg * 8 + i;
             if (r < count) {
                 const int64_t unit = (row0 + r) * kb + ct;
-                *reinterpret_cast<u32x2*>(a.q + unit * kGroupBlock + cg * 8) = gq_codes8(v[i], inv, finite);
+                *reinterpret_cast<u32x2*>(a.q + unit * kGroupBlock + cg * 8) = gq_codes8(v[i], scale, finite);
                 if (cg == 0) a.scales[unit] = scale;
             }
         }
@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     float scale[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        float inv;
-        const bool finite = gq_scale((k & 1) ? m[k >> 1] >> 16 : m[k >> 1] & 0xFFFFu, scale[k], inv);
-        auto val = [&](int i) __attribute__((always_inline)) { return ((k & 1) ? bf16_hi(v[i][k >> 1]) : bf16_lo(v[i][k >> 1])) * inv; };
-        const u32x2 o{e4m3x4_finite(val(0), val(1), val(2), val(3)), e4m3x4_finite(val(4), val(5), val(6), val(7))};
+        const bool finite = gq_scale((k & 1) ? m[k >> 1] >> 16 : m[k >> 1] & 0xFFFFu, scale[k]);
+        // (the column's elements of two rows as a word)
+        auto two = [&](int i) __attribute__((always_inline)) { return __builtin_amdgcn_perm(v[i + 1][k >> 1], v[i][k >> 1], (k & 1) ? 0x07060302u : 0x05040100u); };
+        const u32x2 o{gq_codes4(two(0), two(2), scale[k]), gq_codes4(two(4), two(6), scale[k])};
         *reinterpret_cast<u32x2*>(codes + (cg * 8 + k) * 128 + ((rg ^ cg) * 8)) = finite ? o : u32x2{0u, 0u};
     }
     if (rg == 0) {

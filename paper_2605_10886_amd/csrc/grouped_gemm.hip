@@ -493,12 +493,12 @@ __device__ __forceinline__ void gg_stream(const GgArgs& a, uint8_t* smem) {
                         const uint32_t o = max_abs8(raw[q][i][e]);
                         m = o > m ? o : m;
                     }
-                    float scale, inv;
-                    const bool finite = gq_scale(row_lanes_max(m), scale, inv);
+                    float scale;
+                    const bool finite = gq_scale(row_lanes_max(m), scale);
                     sx[q][i] = scale_byte(__float_as_uint(scale));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const u32x2 c = gq_codes8(raw[q][i][e], inv, finite);
+                        const u32x2 c = gq_codes8(raw[q][i][e], scale, finite);
                         x[q][i][2 * e] = static_cast<int>(c.x);
                         x[q][i][2 * e + 1] = static_cast<int>(c.y);
                     }
