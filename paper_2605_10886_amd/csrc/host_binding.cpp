@@ -601,10 +601,18 @@ bool route_desc(const at::Tensor& logits, PyObject* const* a, loka_route_desc& d
     return true;
 }
 
+// A contiguous tensor of 4-byte elements that is a part of `whole`'s memory (an allocation of its own costs a small call half a microsecond)
+at::Tensor part_of(const at::Tensor& whole, int64_t from, at::IntArrayRef size, at::ScalarType type) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::scalarTypeToTypeMeta(type));
+    t.unsafeGetTensorImpl()->set_storage_offset(from);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(size);
+    return t;
+}
+
 // route(logits, top_k, score, renorm, scale, workspace) -> (expert, weight, slot, row, offsets)
-PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t args) {
     HANDLE_TH_ERRORS
-    if (!need_args(n, 6)) return nullptr;
+    if (!need_args(args, 6)) return nullptr;
     const at::Tensor& logits = tensor(a[0]);
     loka_route_desc d;
     if (!route_desc(logits, a + 1, d)) return nullptr;
@@ -613,8 +621,10 @@ PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!is_run(ws)) return refuse("workspace: contiguous");
     if (!on_gpu(dev, {&ws})) return refuse("tensors on one GPU");
     const c10::DeviceGuard guard(dev);
-    at::Tensor expert = empty({d.tokens, d.top_k}, at::kInt, dev), weight = empty({d.tokens, d.top_k}, at::kFloat, dev), slot = empty({d.tokens, d.top_k}, at::kInt, dev),
-               row = empty({d.tokens * d.top_k}, at::kInt, dev), offsets = empty({d.experts + 1}, at::kInt, dev);
+    const int64_t n = d.tokens * d.top_k;
+    const at::Tensor whole = empty({4 * n + d.experts + 1}, at::kInt, dev);
+    at::Tensor expert = part_of(whole, 0, {d.tokens, d.top_k}, at::kInt), weight = part_of(whole, n, {d.tokens, d.top_k}, at::kFloat),
+               slot = part_of(whole, 2 * n, {d.tokens, d.top_k}, at::kInt), row = part_of(whole, 3 * n, {n}, at::kInt), offsets = part_of(whole, 4 * n, {d.experts + 1}, at::kInt);
     if (!ws.defined()) ws = scratch(loka_route_workspace(&d), dev);
     void* st_ = stream_of(dev);
     const loka_status st = unlocked([&] {
