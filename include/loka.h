@@ -474,7 +474,8 @@ loka_status loka_grouped_quantize(const loka_grouped_quantize_desc* desc, const 
  *           p of the product takes row index[p] (an index outside is read as the nearest one inside)
  *   wq, sw  w_form LOKA_W_TURNED: [groups][Kp / 128][N][128], scales [groups][Kp / 128][N] (of weights [groups, K, N])
  *           w_form LOKA_W_ALONG:  [groups][N][Kp], scales [groups][N][Kp / 128]             (of weights [groups, N, K]: dX = dY W^T)
- *   out_bf16 and / or y_fp32 [rows, N], 16-byte aligned; at least one.  Any N, K (at most 2^20).  Scales have to be powers of two (their exponents are read).
+ *   out_bf16 and / or y_fp32 [rows, N], 16-byte aligned; at least one.  Any N, K (at most 2^20; X and Y at most 2^40 elements and 2^30 tiles of
+ *   128 x 128).  Scales have to be powers of two (their exponents are read).
  * No workspace.  Results do not change from call to call. */
 typedef enum { LOKA_W_TURNED = 0, LOKA_W_ALONG = 1 } loka_w_form;
 typedef struct {
@@ -497,7 +498,7 @@ loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf1
 
 /* Gradients of the weights: dw_g[k, n] = sum over the group's rows p of x[p, k] dy[p, n] (an empty group: zeros).
  *   xt, sxt, dyt, sdyt  TURNED forms of x [rows, K] and dy [rows, N], of the same offsets
- *   dw_bf16 and / or dw_fp32 [groups][K][N], 16-byte aligned; at least one
+ *   dw_bf16 and / or dw_fp32 [groups][K][N], 16-byte aligned; at least one; at most 2^40 elements and 2^30 tiles of 128 x 128
  * Workspace: loka_grouped_wgrad_workspace(desc) bytes (partial sums where there are few results and long groups; added in a fixed order:
  * results do not change from call to call), 16-byte aligned. */
 size_t loka_grouped_wgrad_workspace(const loka_grouped_desc* desc);

@@ -654,8 +654,10 @@ static loka_status validate_grouped(const loka_grouped_desc* d, bool gathered) {
     if (d->rows <= 0 || d->rows > INT32_MAX || d->N <= 0 || d->N > kMostWidth || d->K <= 0 || d->K > kMostWidth || d->groups <= 0 || d->groups > kMostGroups)
         return LOKA_ERR_SHAPE;
     if (gathered && (d->x_rows <= 0 || d->x_rows > INT32_MAX)) return LOKA_ERR_SHAPE;
+    if (too_many(256, d->rows, d->N) || too_many(256, d->rows, d->K)) return LOKA_ERR_SHAPE;       // 2^40
     return LOKA_OK;
 }
+static bool grouped_wgrad_ok(const loka_grouped_desc* d) { return !too_many(256 * static_cast<int64_t>(d->groups), d->K, d->N) && grouped_wgrad_fits(d); }
 static loka_status validate_grouped_gemm(const loka_grouped_desc* d, bool gathered) {
     const loka_status st = validate_grouped(d, gathered);
     if (st != LOKA_OK) return st;
@@ -706,7 +708,7 @@ loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf1
 }
 
 size_t loka_grouped_wgrad_workspace(const loka_grouped_desc* desc) {
-    return validate_grouped(desc, false) != LOKA_OK || !grouped_wgrad_fits(desc) ? 0 : grouped_wgrad_workspace_bytes(desc);
+    return validate_grouped(desc, false) != LOKA_OK || !grouped_wgrad_ok(desc) ? 0 : grouped_wgrad_workspace_bytes(desc);
 }
 
 loka_status loka_grouped_wgrad(const loka_grouped_desc* desc, const uint8_t* xt, const float* sxt, const uint8_t* dyt, const float* sdyt,
@@ -714,13 +716,13 @@ loka_status loka_grouped_wgrad(const loka_grouped_desc* desc, const uint8_t* xt,
     if (!desc || !xt || !sxt || !dyt || !sdyt || !offsets || (!dw_bf16 && !dw_fp32)) return LOKA_ERR_NULL;
     const loka_status st = validate_grouped(desc, false);
     if (st != LOKA_OK) return st;
-    if (!grouped_wgrad_fits(desc)) return LOKA_ERR_SHAPE;
+    if (!grouped_wgrad_ok(desc)) return LOKA_ERR_SHAPE;
     if (!aligned16(xt) || !aligned_to(sxt, 4) || !aligned16(dyt) || !aligned_to(sdyt, 4) || !aligned_to(offsets, 4) || !aligned16(dw_bf16) || !aligned16(dw_fp32))
         return LOKA_ERR_ALIGN;
     const size_t need = grouped_wgrad_workspace_bytes(desc);
     if (need && (!workspace || ws_bytes < need)) return LOKA_ERR_WORKSPACE;
     if (need && !aligned16(workspace)) return LOKA_ERR_ALIGN;
-    return grouped_wgrad_launch(desc, xt, sxt, dyt, sdyt, offsets, dw_bf16, dw_fp32, workspace, ws_bytes, static_cast<hipStream_t>(hip_stream));
+    return grouped_wgrad_launch(desc, xt, sxt, dyt, sdyt, offsets, dw_bf16, dw_fp32, workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 static loka_status validate_combine(const loka_combine_desc* d) {

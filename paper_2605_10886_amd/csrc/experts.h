@@ -28,7 +28,7 @@ loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, c
 bool grouped_wgrad_fits(const loka_grouped_desc* d);
 size_t grouped_wgrad_workspace_bytes(const loka_grouped_desc* d);
 loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, const float* sxt, const uint8_t* dyt, const float* sdyt,
-                                 const int32_t* offsets, void* dw, float* dw32, void* ws, size_t ws_bytes, hipStream_t stream);
+                                 const int32_t* offsets, void* dw, float* dw32, void* ws, hipStream_t stream);
 
 constexpr int kGroupBlock = 128;       // elements that share a scale
 static inline int64_t group_blocks(int64_t n) { return (n + kGroupBlock - 1) / kGroupBlock; }

@@ -19,7 +19,7 @@ struct GgArgs {
     float* y;
     int64_t N;
     int rows, x_rows, groups, ksteps;  // x_rows: of the operand X; ksteps: K in steps of 128
-    int M, blocks;                     // weight gradient: rows of a result; blocks of 128 rows that the operands have
+    int M, blocks, splits;             // weight gradient: rows of a result; blocks of 128 rows that the operands have; ranges of a group's blocks, whose sums go to y
     // element (row r, step k) of an operand lies r * row + k * step bytes from its start (scales: floats), a group's part of it `group` further on
     int64_t x_row, x_step, sx_row, sx_step, w_row, w_step, w_group, sw_row, sw_step, sw_group;
     int tiles_n, tiles_m;              // (tiles_m: weight gradient)
@@ -106,20 +106,25 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         __syncthreads();
     }
     const int units = cum[a.groups - 1];
-    const int total = __builtin_amdgcn_readfirstlane(WGRAD ? a.tiles_m * a.tiles_n * a.groups : units * a.tiles_n);
+    const int total = __builtin_amdgcn_readfirstlane(WGRAD ? a.tiles_m * a.tiles_n * a.groups * a.splits : units * a.tiles_n);
     const int workers = static_cast<int>(gridDim.x) < total ? static_cast<int>(gridDim.x) : total;
     if (static_cast<int>(blockIdx.x) >= workers) return;
 
     // ---- a tile: rows m_first .. of the operand X (forward: of the routed order), columns n0 .., steps of its contraction
-    struct Place { int group, m_first, m_count, n0, n_count, steps, block0; };
+    struct Place { int group, m_first, m_count, n0, n_count, steps, block0, split; };
     auto locate = [&](int t) __attribute__((always_inline)) {
         Place p;
         int tm, tn;
         if (WGRAD) {
             const int per = a.tiles_m * a.tiles_n;
-            p.group = t / per;
-            banded_tile(t - p.group * per, a.tiles_m, a.tiles_n, tm, tn);
-            const int first = p.group ? cum[p.group - 1] : 0, last = cum[p.group];
+            const int range = t / per;
+            banded_tile(t - range * per, a.tiles_m, a.tiles_n, tm, tn);
+            p.group = range / a.splits;
+            p.split = range - p.group * a.splits;
+            int first = p.group ? cum[p.group - 1] : 0, last = cum[p.group];
+            const int each = (last - first + a.splits - 1) / a.splits;
+            first += p.split * each;
+            last = last < first + each ? last : first + each;
             // (of groups that overlap: no more blocks than there are)
             p.block0 = __builtin_amdgcn_readfirstlane(first < 0 ? 0 : first < a.blocks ? first : a.blocks);
             const int own = last - first, left = a.blocks - p.block0;
@@ -145,13 +150,13 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
             p.m_first = first + tm * C::BM;
             p.m_count = count - tm * C::BM;
             p.steps = a.ksteps;
-            p.block0 = 0;
+            p.block0 = p.split = 0;
         }
         p.m_count = p.m_count < C::BM ? p.m_count : C::BM;
         p.n0 = tn * C::BN;
         p.n_count = a.N - p.n0 < C::BN ? static_cast<int>(a.N - p.n0) : C::BN;
         // (all of it in scalar registers)
-        for (int* v : {&p.group, &p.m_first, &p.m_count, &p.n0, &p.n_count, &p.steps, &p.block0}) *v = __builtin_amdgcn_readfirstlane(*v);
+        for (int* v : {&p.group, &p.m_first, &p.m_count, &p.n0, &p.n_count, &p.steps, &p.block0, &p.split}) *v = __builtin_amdgcn_readfirstlane(*v);
         return p;
     };
 
@@ -348,7 +353,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         }
 
         // ---- lane (r, g) holds row 16 i + r, columns 32 (j / 2) + 8 g + 0 .. 7
-        const int64_t row0 = WGRAD ? static_cast<int64_t>(at.group) * a.M + at.m_first : static_cast<int64_t>(at.m_first);
+        const int64_t row0 = WGRAD ? (static_cast<int64_t>(at.split) * a.groups + at.group) * a.M + at.m_first : static_cast<int64_t>(at.m_first);
         if (a.wide) {                  // whole runs of 8 columns; what is past the result is dropped
             const int N = static_cast<int>(a.N), n_lane = at.n0 + wn * TN * 16 + g * 8, o_lane = (wm * TM * 16 + r) * N + n_lane;
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
@@ -565,8 +570,9 @@ static int64_t tiles_of(const loka_grouped_desc* d) {       // that the groups c
 template <class C>
 static int64_t wgrad_tiles_of(const loka_grouped_desc* d) { return (d->K + C::BM - 1) / C::BM * ((d->N + C::BN - 1) / C::BN) * d->groups; }
 
-bool grouped_gemm_fits(const loka_grouped_desc* d) { return tiles_of<GgSmall>(d) <= INT32_MAX / 512; }
-bool grouped_wgrad_fits(const loka_grouped_desc* d) { return wgrad_tiles_of<GgSmall>(d) <= INT32_MAX / 512; }
+// (tiles are counted in 32 bits)
+bool grouped_gemm_fits(const loka_grouped_desc* d) { return tiles_of<GgSmall>(d) <= INT32_MAX / 2; }
+bool grouped_wgrad_fits(const loka_grouped_desc* d) { return wgrad_tiles_of<GgSmall>(d) <= INT32_MAX / 2; }
 
 template <class C, bool WGRAD>
 static loka_status gg_launch(GgArgs& a, int64_t grid, hipStream_t stream) {
@@ -622,8 +628,10 @@ static int tile_form(double large, double small, double steps) {
 }
 static int gemm_form(const loka_grouped_desc* d) {
     const double rows = static_cast<double>(d->rows), some = static_cast<double>(d->rows < d->groups ? d->rows : d->groups), each = rows / some;
-    if (each <= 12.0) return GG_STREAM16;
-    if (each <= 24.0) return GG_STREAM32;
+    if ((rows / 16 + some) * std::ceil(static_cast<double>(d->N) / 16) < 4194304.0) {      // (workgroups of 512 threads in one launch)
+        if (each <= 12.0) return GG_STREAM16;
+        if (each <= 24.0) return GG_STREAM32;
+    }
     auto tiles = [&](double b) { return std::fmax(some, rows / b + some / 2) * std::ceil(static_cast<double>(d->N) / b); };
     return tile_form(tiles(256), tiles(128), std::ceil(static_cast<double>(d->K) / kGroupBlock));
 }
@@ -658,10 +666,45 @@ loka_status grouped_linear_fused_launch(const loka_grouped_desc* d, const void* 
     return stream16<true>(a, stream);
 }
 
-size_t grouped_wgrad_workspace_bytes(const loka_grouped_desc*) { return 0; }
+// Sums of the ranges' partial results, in order.
+__global__ __launch_bounds__(256) void gg_join_kernel(const float* __restrict__ part, int splits, int64_t n, int64_t first_wg, uint16_t* __restrict__ out,
+                                                      float* __restrict__ y) {
+    const int64_t i = (first_wg + blockIdx.x) * 256 + threadIdx.x;
+    if (i >= n) return;
+    float s = part[i];
+#pragma unroll 8
+    for (int k = 1; k < splits; ++k) s += part[k * n + i];
+    if (out) out[i] = static_cast<uint16_t>(f32_to_bf16_rne(s));
+    if (y) y[i] = s;
+}
+
+// Tile and ranges of a weight gradient.  Where the results are few tiles, a group's blocks are split over workgroups, as far as that saves more than the
+// partial sums cost (rows x groups x K x N: 16384 x 1 x 256 x 256 in 32 ranges 14.5 us, in one 80; 16384 x 2 x
+// 64 x 100 12.3 and 41).
+struct WgradPlan { int form, splits; };
+static WgradPlan wgrad_plan(const loka_grouped_desc* d) {
+    const double steps = std::ceil(static_cast<double>(d->rows) / static_cast<double>(d->groups) / kGroupBlock + 0.5);
+    const double small = static_cast<double>(wgrad_tiles_of<GgSmall>(d)), bytes = static_cast<double>(d->groups) * static_cast<double>(d->K) * static_cast<double>(d->N) * 4;
+    WgradPlan p{tile_form(static_cast<double>(wgrad_tiles_of<GgLarge>(d)), small, steps), 1};
+    if (p.form == GG_LARGE) return p;
+    double best = 1e30;
+    for (int s = 1; s <= 32 && (s == 1 || small * s <= 512); s *= 2) {
+        const double us = (small * s <= 256 ? 0.55 : 1.0) * std::ceil(steps / s) + (s > 1 ? 4.0 + bytes * s / 2e6 : 0.0);
+        if (us < best) {
+            best = us;
+            p.splits = s;
+        }
+    }
+    return p;
+}
+
+size_t grouped_wgrad_workspace_bytes(const loka_grouped_desc* d) {
+    const int splits = wgrad_plan(d).splits;
+    return splits > 1 ? static_cast<size_t>(splits) * static_cast<size_t>(d->groups) * static_cast<size_t>(d->K) * static_cast<size_t>(d->N) * 4 : 0;
+}
 
 loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, const float* sxt, const uint8_t* dyt, const float* sdyt,
-                                 const int32_t* offsets, void* dw, float* dw32, void*, size_t, hipStream_t stream) {
+                                 const int32_t* offsets, void* dw, float* dw32, void* ws, hipStream_t stream) {
     GgArgs a{};
     a.xq = xt;
     a.sx = sxt;
@@ -681,10 +724,18 @@ loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, 
     a.sx_row = a.sw_row = 1;
     a.sx_step = d->K;
     a.sw_step = d->N;
-    const double steps = std::ceil(static_cast<double>(d->rows) / static_cast<double>(d->groups) / kGroupBlock + 0.5);
-    if (tile_form(static_cast<double>(wgrad_tiles_of<GgLarge>(d)), static_cast<double>(wgrad_tiles_of<GgSmall>(d)), steps) == GG_LARGE)
-        return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
-    return gg_launch<GgSmall, true>(a, wgrad_tiles_of<GgSmall>(d), stream);
+    const WgradPlan p = wgrad_plan(d);
+    a.splits = p.splits;
+    if (p.form == GG_LARGE) return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
+    if (p.splits == 1) return gg_launch<GgSmall, true>(a, wgrad_tiles_of<GgSmall>(d), stream);
+    a.out = nullptr;
+    a.y = static_cast<float*>(ws);
+    const loka_status st = gg_launch<GgSmall, true>(a, wgrad_tiles_of<GgSmall>(d) * p.splits, stream);
+    if (st != LOKA_OK) return st;
+    const int64_t n = d->groups * d->K * d->N;
+    return in_launches((n + 255) / 256, 256, [&](int64_t from, uint32_t grid) {
+        gg_join_kernel<<<grid, 256, 0, stream>>>(static_cast<const float*>(ws), p.splits, n, from, static_cast<uint16_t*>(dw), dw32);
+    });
 }
 
 }  // namespace loka

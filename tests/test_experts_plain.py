@@ -87,6 +87,10 @@ def test_grouped_product_refusals():
         if kw != dict(rows=MOST, N=1 << 20):
             assert wgrad(desc(**kw)) == SHAPE and B.lib().loka_grouped_wgrad_workspace(ref(desc(**kw))) == 0
     assert wgrad(desc(N=1 << 20, K=1 << 20)) == SHAPE
+    long = desc(rows=1 << 20, N=64, K=64, groups=1)                                # few results, a long sum: partial sums
+    need = B.lib().loka_grouped_wgrad_workspace(ref(long))
+    assert need >= 2 * 64 * 64 * 4 and wgrad(long) == wgrad(long, ws=FAKE, nws=need - 1) == WORKSPACE and wgrad(long, ws=OTHER, nws=need) == ALIGN
+    assert B.lib().loka_grouped_wgrad_workspace(ref(desc())) == 0
     for x_rows in (0, MOST + 1):
         assert gemm(desc(x_rows=x_rows), index=FAKE) == linear(desc(x_rows=x_rows), index=FAKE) == SHAPE
     for form in (-1, 2):
