@@ -332,8 +332,9 @@ __global__ __launch_bounds__(kRouteMost) void route_place_kernel(const RouteArgs
 //   sigmoid           g_j s_j (1 - s_j)                              others 0
 template <int L, int V, int R, bool BF16>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
-    const int t = static_cast<int>(threadIdx.x), l = t % L, k = a.top_k;
     constexpr int PER = kRouteThreads / L;
+    __shared__ __align__(16) float rows[PER * L * V];
+    const int t = static_cast<int>(threadIdx.x), l = t % L, k = a.top_k;
     const int64_t token = static_cast<int64_t>(blockIdx.x) * PER + t / L;
     const bool in = token < a.tokens;
     const int64_t at = (in ? token : a.tokens - 1) * a.ld, o = (in ? token : a.tokens - 1) * k + (l < k ? l : 0);
@@ -388,12 +389,19 @@ __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const Rou
     if (!dense)
 #pragma unroll
         for (int v = 0; v < V; ++v) lx[v] = 0.f;
-    for (int j = 0; j < k; ++j) {
-        const int e = __shfl(mine, j, L);
-        const float dj = __shfl(d, j, L);
+    // the chosen entries' values over the others', through LDS (in registers every choice would be compared with every entry)
+    float* const row = rows + (t / L) * (L * V);
 #pragma unroll
-        for (int v = 0; v < V; ++v) lx[v] = entry_of<L, R>(l, v) == e ? dj : lx[v];
-    }
+    for (int b = 0; b < V; b += R)
+#pragma unroll
+        for (int i = 0; i < R; ++i) row[entry_of<L, R>(l, b + i)] = lx[b + i];
+    __syncthreads();
+    if (mine >= 0) row[mine] = d;
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < V; b += R)
+#pragma unroll
+        for (int i = 0; i < R; ++i) lx[b + i] = row[entry_of<L, R>(l, b + i)];
     if (!in) return;
 #pragma unroll
     for (int b = 0; b < V; b += R) {
