@@ -678,7 +678,7 @@ loka_status loka_grouped_gemm(const loka_grouped_desc* desc, const uint8_t* xq, 
 
 // The workspace of the layer: codes of x, then their scales.
 size_t loka_grouped_linear_workspace(const loka_grouped_desc* desc, int with_index) {
-    if (validate_grouped_gemm(desc, with_index != 0) != LOKA_OK || grouped_linear_fused(desc, with_index != 0)) return 0;
+    if (validate_grouped_gemm(desc, with_index != 0) != LOKA_OK || grouped_linear_fused(desc)) return 0;
     const size_t n = static_cast<size_t>(with_index ? desc->x_rows : desc->rows) * static_cast<size_t>(group_blocks(desc->K));
     return n * kGroupBlock + (n * 4 + 15) / 16 * 16;
 }
@@ -693,7 +693,7 @@ loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf1
     if (!aligned_to(x_bf16, 2) || !aligned_to(index, 4) || !aligned_to(offsets, 4) || !aligned16(wq) || !aligned_to(sw, 4) || !aligned16(out_bf16) ||
         !aligned16(y_fp32))
         return LOKA_ERR_ALIGN;
-    if (grouped_linear_fused(desc, index != nullptr))
+    if (grouped_linear_fused(desc))
         return grouped_linear_fused_launch(desc, x_bf16, ld, index, offsets, wq, sw, out_bf16, y_fp32, static_cast<hipStream_t>(hip_stream));
     const size_t need = loka_grouped_linear_workspace(desc, index != nullptr);
     if (need && (!workspace || ws_bytes < need)) return LOKA_ERR_WORKSPACE;

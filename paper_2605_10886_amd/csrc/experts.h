@@ -20,7 +20,7 @@ loka_status combine_backward_launch(const loka_combine_desc* d, const void* dout
 loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const void* x, const int32_t* index, const int32_t* offsets, uint8_t* q,
                                     float* scales, uint8_t* qt, float* st, hipStream_t stream);
 bool grouped_gemm_fits(const loka_grouped_desc* d);
-bool grouped_linear_fused(const loka_grouped_desc* d, bool gathered);
+bool grouped_linear_fused(const loka_grouped_desc* d);
 loka_status grouped_linear_fused_launch(const loka_grouped_desc* d, const void* x, int64_t ld, const int32_t* index, const int32_t* offsets,
                                         const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream);
 loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
@@ -51,13 +51,6 @@ __device__ __forceinline__ int lanes_inclusive(int v) {
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);        // lane 31 to the upper half
     return v;
 }
-// Units of `unit` rows that all groups take (each its own), by a wave; uniform.
-__device__ __forceinline__ int units_of_all(const int32_t* offsets, int groups, int rows, int unit) {
-    const int lane = static_cast<int>(threadIdx.x) & 63;
-    int n = 0;
-    for (int g = lane; g < groups; g += 64) n += (group_rows(offsets, g, rows).count + unit - 1) / unit;
-    return __builtin_amdgcn_readlane(lanes_inclusive(n), 63);
-}
 // The group that holds unit `target`, and the units of the groups before it; group = -1: there are not so many.  By a wave; uniform.
 struct UnitAt { int group, before, first, count; };
 __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, int rows, int unit, int target) {
@@ -77,10 +70,6 @@ __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, 
         base += __builtin_amdgcn_readlane(s, 63);
     }
     return {-1, base, 0, 0};
-}
-// Units of the groups before `group`, by a wave; uniform.
-__device__ __forceinline__ int units_before(const int32_t* offsets, int group, int rows, int unit) {
-    return units_of_all(offsets, group, rows, unit);
 }
 // Scale of 128 elements from the bits of their largest magnitude (a bf16's).  False where that is not finite: the scale is a NaN then, the codes are zeros.
 __device__ __forceinline__ bool gq_scale(uint32_t amax, float& scale) {

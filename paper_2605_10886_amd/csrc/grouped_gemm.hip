@@ -22,7 +22,7 @@ struct GgArgs {
     int M, blocks, splits;             // weight gradient: rows of a result; blocks of 128 rows that the operands have; ranges of a group's blocks, whose sums go to y
     // element (row r, step k) of an operand lies r * row + k * step bytes from its start (scales: floats), a group's part of it `group` further on
     int64_t x_row, x_step, sx_row, sx_step, w_row, w_step, w_group, sw_row, sw_step, sw_group;
-    int tiles_n, tiles_m;              // (tiles_m: weight gradient)
+    int tiles_n, tiles_m, tiles;       // (tiles_m: weight gradient); tiles that there can be
     bool wide;                         // rows of whole 16-byte runs
     const uint16_t* x;                 // few rows, quantized in the kernel: bf16 [x_rows, ldx]
     int64_t ldx, K;
@@ -105,8 +105,10 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         }
         __syncthreads();
     }
-    const int units = cum[a.groups - 1];
-    const int total = __builtin_amdgcn_readfirstlane(WGRAD ? a.tiles_m * a.tiles_n * a.groups * a.splits : units * a.tiles_n);
+    // (groups that overlap would have more tiles than there are, or so many that their number overflows: no more than there are are taken,
+    // and every one of them lies within its group)
+    const int units = cum[a.groups - 1], most = a.tiles / a.tiles_n;
+    const int total = __builtin_amdgcn_readfirstlane(WGRAD ? a.tiles : (units < 0 ? 0 : units < most ? units : most) * a.tiles_n);
     const int workers = static_cast<int>(gridDim.x) < total ? static_cast<int>(gridDim.x) : total;
     if (static_cast<int>(blockIdx.x) >= workers) return;
 
@@ -139,13 +141,11 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
                 past = __builtin_amdgcn_ballot_w64(g0 + lane < a.groups && cum[g0 + lane < a.groups ? g0 + lane : 0] > u);
                 if (past || g0 + 64 >= a.groups) break;
             }
-            p.group = past ? g0 + __builtin_ctzll(past) : a.groups - 1;
+            p.group = g0 + __builtin_ctzll(past);          // (u is less than the last sum)
             const int before = p.group ? cum[p.group - 1] : 0;
             const int first = __builtin_amdgcn_readfirstlane(off[2 * p.group]), count = __builtin_amdgcn_readfirstlane(off[2 * p.group + 1]);
             const int tiles_m = (count + C::BM - 1) / C::BM;
-            int local = t - __builtin_amdgcn_readfirstlane(before) * a.tiles_n;
-            // (always in range, unless groups that overlap have made the sums overflow)
-            if (local < 0 || local >= tiles_m * a.tiles_n) local = 0;
+            const int local = t - __builtin_amdgcn_readfirstlane(before) * a.tiles_n;
             banded_tile(local, tiles_m, a.tiles_n, tm, tn);
             p.m_first = first + tm * C::BM;
             p.m_count = count - tm * C::BM;
@@ -575,15 +575,16 @@ bool grouped_gemm_fits(const loka_grouped_desc* d) { return tiles_of<GgSmall>(d)
 bool grouped_wgrad_fits(const loka_grouped_desc* d) { return wgrad_tiles_of<GgSmall>(d) <= INT32_MAX / 2; }
 
 template <class C, bool WGRAD>
-static loka_status gg_launch(GgArgs& a, int64_t grid, hipStream_t stream) {
+static loka_status gg_launch(GgArgs& a, int64_t tiles, hipStream_t stream) {
     a.tiles_n = static_cast<int>((a.N + C::BN - 1) / C::BN);
     a.tiles_m = WGRAD ? (a.M + C::BM - 1) / C::BM : 0;
     a.wide = a.N % 8 == 0;
+    a.tiles = static_cast<int>(tiles);
     const int lds = C::LDS + 12 * a.groups;
     const int64_t slots = 256 * C::PER_CU;
     // (on every call, a host-side table write: no process-wide state, and correct on whichever device is current)
     LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&gg_tile_kernel<C, WGRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    gg_tile_kernel<C, WGRAD><<<static_cast<uint32_t>(grid < slots ? grid : slots), 64 * C::NW, lds, stream>>>(a);
+    gg_tile_kernel<C, WGRAD><<<static_cast<uint32_t>(tiles < slots ? tiles : slots), 64 * C::NW, lds, stream>>>(a);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
 }
@@ -617,30 +618,44 @@ static GgArgs gemm_args(const loka_grouped_desc* d, const int32_t* index, const 
     return a;
 }
 
-// What runs a product.  How the rows spread over the groups is not known here: tiles are counted as if every group left half a tile empty.
-// Microseconds fitted to launches (rows x groups x K x N, measured / estimated): large tiles 3000 x 4 x 512 x 1024 14.4 / 15.5, 3000 x 4 x 4096 x 1024 50 / 51,
-// 10026 x 23 x 1008 x 720 21.7 / 20.5; small ones 3000 x 4 x 512 x 1024 8.0 / 9.2, 3000 x 4 x 2048 x 1024 16.2 / 15.8, 12000 x 4 x 1024 x 1024 25.8 / 24.5,
-// 12000 x 4 x 4096 x 1024 74 / 73 (large 53 / 51).
-enum { GG_STREAM16 = 0, GG_STREAM32 = 1, GG_SMALL = 2, GG_LARGE = 3 };
-static int tile_form(double large, double small, double steps) {
-    const double us_large = 7.5 + std::ceil(large / 256) * (3.0 + 1.25 * steps), us_small = 5.5 + std::ceil(small / 512) * (1.5 + (small <= 256 ? 0.55 : 1.0) * steps);
-    return us_large < us_small ? GG_LARGE : GG_SMALL;
+// What runs a product: the form whose microseconds, fitted to launches, are fewest.  How the rows spread over the groups is not known here: units are
+// counted as if every group left half a one empty.  Estimated / measured (rows x groups x K x N; MT x NT: columns of 16 rows and columns each):
+//   large tiles  3000 x 4 x 512 x 1024 15.5 / 14.4, 3000 x 4 x 4096 x 1024 51 / 50, 12000 x 4 x 4096 x 1024 51 / 53, 10026 x 23 x 1008 x 720 20.5 / 21.7
+//   small tiles  3000 x 4 x 512 x 1024 7.4 / 8.0, 12000 x 4 x 4096 x 1024 73 / 74, 256 x 16 x 1024 x 4096 15.0 / 15.1, 128 x 8 x 4096 x 4096 24.8 / 26.7
+//   1 x 1, 1 x 2 and 1 x 4   8 x 64 x 1024 x 4096 12.3 / 12.4, 9.2 / 9.3 and 7.6 / 7.8;  8 x 64 x 4096 x 1024 10.5 / 9.3, 8.3 / 8.1 and 12.1 / 12.2
+//   2 x 4        256 x 16 x 1024 x 4096 17.9 / 17.2, 128 x 8 x 4096 x 4096 26.5 / 26.2 (1 x 4: 32.1 / 32.7)
+struct GgForm { bool tiles; int mt, nt; };                  // tiles: mt = 2 the large ones, 1 the small ones; else 16 mt rows x 16 nt columns a workgroup
+static double large_us(double tiles, double steps) { return 7.5 + std::ceil(tiles / 256) * (3.0 + 1.25 * steps); }
+static double small_us(double tiles, double steps) {
+    return tiles <= 256 ? 5.0 + (0.45 + 0.2 * tiles / 256) * steps : 5.5 + std::ceil(tiles / 512) * (1.5 + steps);
 }
-static int gemm_form(const loka_grouped_desc* d) {
-    const double rows = static_cast<double>(d->rows), some = static_cast<double>(d->rows < d->groups ? d->rows : d->groups), each = rows / some;
-    if ((rows / 16 + some) * std::ceil(static_cast<double>(d->N) / 16) < 4194304.0) {      // (workgroups of 512 threads in one launch)
-        if (each <= 12.0) return GG_STREAM16;
-        if (each <= 24.0) return GG_STREAM32;
+static GgForm gemm_form(const loka_grouped_desc* d) {
+    const double rows = static_cast<double>(d->rows), some = static_cast<double>(d->rows < d->groups ? d->rows : d->groups), N = static_cast<double>(d->N);
+    const double steps = std::ceil(static_cast<double>(d->K) / kGroupBlock), floor = some * N * steps * kGroupBlock / 6.5e6;      // (of the weights' bytes)
+    auto units = [&](double b) { return std::fmax(some, rows / b + some / 2); };
+    GgForm best{true, 1, 0};
+    double least = 1e30;
+    auto offer = [&](double us, GgForm f) {
+        if (us >= least) return;
+        least = us;
+        best = f;
+    };
+    auto stream = [&](int mt, int nt) {
+        const double rounds = std::ceil(units(16 * mt) * std::ceil(N / (16 * nt)) / 256);
+        return std::fmax(floor, 2.2 + rounds * (0.06 * (mt + nt) * steps + 0.3 * mt));
+    };
+    // (the others with the launch before them where the rows come as bf16)
+    if ((rows / 16 + some) * std::ceil(N / 16) < 4194304.0) {                               // (workgroups of 512 threads in one launch)
+        for (int nt = 4; nt >= 1; nt /= 2) offer(stream(1, nt), GgForm{false, 1, nt});
+        offer(stream(2, 4) + 2.0, GgForm{false, 2, 4});
     }
-    auto tiles = [&](double b) { return std::fmax(some, rows / b + some / 2) * std::ceil(static_cast<double>(d->N) / b); };
-    return tile_form(tiles(256), tiles(128), std::ceil(static_cast<double>(d->K) / kGroupBlock));
+    offer(std::fmax(floor, small_us(units(128) * std::ceil(N / 128), steps)) + 2.0, GgForm{true, 1, 0});
+    offer(std::fmax(floor, large_us(units(256) * std::ceil(N / 256), steps)) + 2.0, GgForm{true, 2, 0});
+    return best;
 }
 template <bool FUSED>
-static loka_status stream16(GgArgs& a, hipStream_t stream) {
-    const int64_t some = a.rows < a.groups ? a.rows : a.groups, runs = some * ((a.N + 15) / 16);
-    if (runs >= 2048) return stream_launch<1, 4, FUSED>(a, stream);
-    if (runs >= 1024) return stream_launch<1, 2, FUSED>(a, stream);
-    return stream_launch<1, 1, FUSED>(a, stream);
+static loka_status stream16(int nt, GgArgs& a, hipStream_t stream) {
+    return nt == 4 ? stream_launch<1, 4, FUSED>(a, stream) : nt == 2 ? stream_launch<1, 2, FUSED>(a, stream) : stream_launch<1, 1, FUSED>(a, stream);
 }
 
 loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, const float* sx, const int32_t* index, const int32_t* offsets,
@@ -648,22 +663,22 @@ loka_status grouped_gemm_launch(const loka_grouped_desc* d, const uint8_t* xq, c
     GgArgs a = gemm_args(d, index, offsets, wq, sw, out, y);
     a.xq = xq;
     a.sx = sx;
-    switch (gemm_form(d)) {
-        case GG_STREAM16: return stream16<false>(a, stream);
-        case GG_STREAM32: return stream_launch<2, 2, false>(a, stream);
-        case GG_LARGE: return gg_launch<GgLarge, false>(a, tiles_of<GgLarge>(d), stream);
-        default: return gg_launch<GgSmall, false>(a, tiles_of<GgSmall>(d), stream);
-    }
+    const GgForm f = gemm_form(d);
+    if (!f.tiles) return f.mt == 1 ? stream16<false>(f.nt, a, stream) : stream_launch<2, 4, false>(a, stream);
+    return f.mt == 2 ? gg_launch<GgLarge, false>(a, tiles_of<GgLarge>(d), stream) : gg_launch<GgSmall, false>(a, tiles_of<GgSmall>(d), stream);
 }
 
-bool grouped_linear_fused(const loka_grouped_desc* d, bool) { return gemm_form(d) == GG_STREAM16; }
+bool grouped_linear_fused(const loka_grouped_desc* d) {
+    const GgForm f = gemm_form(d);
+    return !f.tiles && f.mt == 1;
+}
 
 loka_status grouped_linear_fused_launch(const loka_grouped_desc* d, const void* x, int64_t ld, const int32_t* index, const int32_t* offsets,
                                         const uint8_t* wq, const float* sw, void* out, float* y, hipStream_t stream) {
     GgArgs a = gemm_args(d, index, offsets, wq, sw, out, y);
     a.x = static_cast<const uint16_t*>(x);
     a.ldx = ld;
-    return stream16<true>(a, stream);
+    return stream16<true>(gemm_form(d).nt, a, stream);
 }
 
 // Sums of the ranges' partial results, in order.
@@ -681,12 +696,12 @@ __global__ __launch_bounds__(256) void gg_join_kernel(const float* __restrict__ 
 // Tile and ranges of a weight gradient.  Where the results are few tiles, a group's blocks are split over workgroups, as far as that saves more than the
 // partial sums cost (rows x groups x K x N: 16384 x 1 x 256 x 256 in 32 ranges 14.5 us, in one 80; 16384 x 2 x
 // 64 x 100 12.3 and 41).
-struct WgradPlan { int form, splits; };
+struct WgradPlan { bool large; int splits; };
 static WgradPlan wgrad_plan(const loka_grouped_desc* d) {
     const double steps = std::ceil(static_cast<double>(d->rows) / static_cast<double>(d->groups) / kGroupBlock + 0.5);
     const double small = static_cast<double>(wgrad_tiles_of<GgSmall>(d)), bytes = static_cast<double>(d->groups) * static_cast<double>(d->K) * static_cast<double>(d->N) * 4;
-    WgradPlan p{tile_form(static_cast<double>(wgrad_tiles_of<GgLarge>(d)), small, steps), 1};
-    if (p.form == GG_LARGE) return p;
+    WgradPlan p{large_us(static_cast<double>(wgrad_tiles_of<GgLarge>(d)), steps) < small_us(small, steps), 1};
+    if (p.large) return p;
     double best = 1e30;
     for (int s = 1; s <= 32 && (s == 1 || small * s <= 512); s *= 2) {
         const double us = (small * s <= 256 ? 0.55 : 1.0) * std::ceil(steps / s) + (s > 1 ? 4.0 + bytes * s / 2e6 : 0.0);
@@ -726,7 +741,7 @@ loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, 
     a.sw_step = d->N;
     const WgradPlan p = wgrad_plan(d);
     a.splits = p.splits;
-    if (p.form == GG_LARGE) return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
+    if (p.large) return gg_launch<GgLarge, true>(a, wgrad_tiles_of<GgLarge>(d), stream);
     if (p.splits == 1) return gg_launch<GgSmall, true>(a, wgrad_tiles_of<GgSmall>(d), stream);
     a.out = nullptr;
     a.y = static_cast<float*>(ws);

@@ -293,6 +293,28 @@ def test_products_are_exact_on_whole_numbers(sizes, K, N):
     assert torch.equal(o4[:n], out[:n]) and torch.equal(y4[:n], y[:n])
 
 
+# sizes of which each form of the product takes some: 16 rows at a time and 64, 32 or 16 columns, 32 rows at a time, small tiles, large ones
+FORMS = [([7] * 16, 700, 520), ([1, 0, 9], 1000, 2000), ([31] * 16, 700, 100), ([5, 16, 17], 2000, 301), ([16] * 40, 2000, 301), ([20, 0, 33, 31, 32, 1], 2000, 2003),
+         ([900, 0, 901, 127, 2000], 100, 520), ([300] * 16, 100, 517), ([2499, 1, 2501, 0, 0, 700], 130, 301), ([40] * 300, 200, 300), ([900, 1100, 255, 257, 1500], 300, 2000),
+         ([2500, 2501], 300, 2003), ([300] * 16, 385, 2000), ([0] * 70 + [3000, 1, 0, 2000], 700, 1500), ([0] * 70 + [9000, 1, 8999], 300, 260)]
+
+
+@pytest.mark.parametrize("sizes,K,N", FORMS)
+def test_every_form_of_the_product_is_exact_on_whole_numbers(sizes, K, N):
+    test_products_are_exact_on_whole_numbers(sizes, K, N)
+
+
+def test_groups_that_overlap_reach_nothing_else():
+    """More tiles than there are, in both sizes of tile: only the rows are written."""
+    for n, K, N in ((4500, 100, 520), (4500, 300, 2000)):
+        x, w = _small((n, K), 1), _small((5 * K, N), 2)
+        wq, xq = B.loka_grouped_quantize(w, groups=5, along=False, turned=True), B.loka_grouped_quantize(x)
+        room = torch.full((n + 600, N), -7.0, dtype=torch.bfloat16, device=DEV)
+        for off in ([0, n, 0, n, 0, n], [0, 0, n, 0, n, n]):
+            B.loka_grouped_gemm(B.make_grouped_desc(n, N, K, 5), xq.q, xq.scales, wq.qt, wq.st, _i32(off), out=room[300:300 + n])
+        assert bool((room[:300] == -7).all()) and bool((room[300 + n:] == -7).all())
+
+
 @pytest.mark.parametrize("sizes,K,N", [([1], 4096, 256), ([5, 11, 16, 3], 1024, 512), ([40, 0, 90], 700, 300), ([600, 424], 1152, 512)])
 def test_products_of_random_numbers(sizes, K, N):
     bounds = _bounds(sizes)
