@@ -9,7 +9,11 @@ namespace loka {
 // ---------------------------------------------------------------------------------
 // The choice.  L lanes hold a token's logits, V each, in runs of R that follow each other in memory, as keys whose order as unsigned
 // integers is the logits' order: 0 for what may not be chosen.  A choice is the largest key over the lanes, then the lowest entry that has it.  A
-// bf16's key has room for the entry as well, so that all keys differ and the largest one is the choice.
+// bf16's key has room for the entry as well, so that all keys differ and the largest one is the choice; the next one is the largest below
+// it, and no key has to be struck out.
+//
+// Bound by the vector unit's top_k passes over the keys: 32768 x 256 bf16 logits, 8 choices, 14.4 us (the 17 MB read alone: 3), their
+// places 7.6.  A token alone: 5.2 us with the launch, of which the logits' journey and top_k exchanges are most.
 constexpr int kRouteMostChunk = 128;   // tokens of a workgroup, at most
 constexpr int kRouteThreads = 256;     // ... and its threads, of a small call and of the gradient
 constexpr int kRouteMost = 1024;       // ... of a call of more tokens
@@ -330,6 +334,7 @@ __global__ __launch_bounds__(kRouteMost) void route_place_kernel(const RouteArgs
 //   softmax           q_e (g_e - sum_i g_i q_i), g_e = 0 where not chosen
 //   sigmoid, renorm   q_j (g_j - sum_i g_i q_i) (1 - s_j)            others 0
 //   sigmoid           g_j s_j (1 - s_j)                              others 0
+// Bytes only: 32768 x 256 bf16 7.8 us (17 MB written, and 2 read where only the chosen entries are), softmax over all 14.2 (an exponential each).
 template <int L, int V, int R, bool BF16>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
     constexpr int PER = kRouteThreads / L;
@@ -427,8 +432,9 @@ static int route_pitch(int experts) {
     while (p < experts) p *= 2;
     return p;
 }
-// Tokens of a workgroup: all of a small call's (one launch), else as few as leave 256 workgroups (each of which adds up the counts of all: 300
-// tokens of 160 experts, 6 choices, 17 -> 8.5 us against 128; 32768 of 256 would take longer on less).
+// Tokens of a workgroup: all of a small call's (one launch: 64 tokens of 64 experts, 8 choices, 5.2 us, in two launches 7.2), else as few as leave
+// 256 workgroups, each of which adds up the counts of all (300 tokens of 160 experts, 6 choices, 8.5 us with 16 of a workgroup, 13.7 with 128;
+// 32768 of 256, 8 choices, 35.8 with 16, 20.7 with 128).
 static int64_t route_chunk(const loka_route_desc* d) {
     if (d->tokens <= 64) return 64;
     int64_t c = 16;
@@ -440,7 +446,9 @@ size_t route_workspace_bytes(const loka_route_desc* d) {
     return chunks > 1 ? static_cast<size_t>(chunks + 1) * static_cast<size_t>(route_pitch(d->experts)) * 4 : 0;
 }
 
-// Lanes, logits a lane and their runs: by the number of experts, and in runs of 16 bytes (8 where a lane has four bf16) where rows are whole runs
+// Lanes, logits a lane and their runs: by the number of experts, and in runs of 16 bytes (8 where a lane has four bf16) where rows are whole runs.
+// 16 lanes a token keep its exchanges inside the vector unit's rows and share a wave among four tokens (32768 x 256, 8 choices, 20.6 us; 32 lanes
+// 24.5, 64 lanes 33.5); more than 256 logits are too many for them (32768 x 512 on 64 lanes 41.4 us, on 32 44.9).
 template <class F>
 static void by_experts(const loka_route_desc* d, const void* logits, const void* dlogits, F&& f) {
     auto with = [&](auto l, auto v) {
@@ -493,8 +501,9 @@ loka_status route_launch(const loka_route_desc* d, const void* logits, int32_t* 
     LOKA_HIP_TRY(hipGetLastError());
     if (a.chunks == 1) return LOKA_OK;
     const size_t place = static_cast<size_t>(d->experts) * 12 + 64;
-    // A workgroup adds up every chunk's counts: chunks^2 of them in all
-    if (a.chunks <= 1024) {
+    // A workgroup adds up every chunk's counts, chunks^2 in all, where that takes no longer than a launch that does it once (32768 x 64, 8
+    // choices, 13.9 us, with the launch 14.3; 65536 x 256 39.4 and 34.6)
+    if (a.chunks <= 256) {
         route_place_kernel<false><<<a.chunks, kRouteMost, place, stream>>>(a);
     } else {
         route_scan_kernel<<<d->experts, kRouteThreads, 0, stream>>>(a);
@@ -522,7 +531,7 @@ loka_status route_backward_launch(const loka_route_desc* d, const void* logits, 
 // ---------------------------------------------------------------------------------
 // The sum of a token's results, and its gradients.  A lane takes 8 columns of a token; bytes only, so a token's rows (K of them at
 // most) are all requested before the first is used.  Tokens of more than 256 columns: a wave takes 512 of them, and its token's slots and weights are
-// scalars; narrower ones share a wave, 2^lg lanes each.
+// scalars; narrower ones share a wave, 2^lg lanes each.  16384 tokens x 4 choices x 4096: 133 us (805 MB, 6.0 TB/s), backward 237 (1.2 GB, 5.1 TB/s).
 struct CombineArgs {
     const uint16_t *y, *residual, *dout;
     const int32_t* slot;
@@ -703,8 +712,8 @@ static CombineArgs args_of(const loka_combine_desc* d, const int32_t* slot, cons
     while ((8 << a.lg) < d->cols) ++a.lg;
     return a;
 }
-// f(K, WAVE, STREAMED) for a call whose matrices of tokens * top_k rows have `cols` columns.  Results of 2^27 elements and more, which the 256 MB of last-level cache
-// cannot hold, pass it by.
+// f(K, WAVE, STREAMED) for a call whose matrices of tokens * top_k rows have `cols` columns.  Results of 2^27 elements and more, which the 256 MB of last-level
+// cache cannot hold, pass it by (8192 tokens x 4 x 4096: 67.7 us, else 78.6, backward 118 and 123; half the tokens: 35.0 and 30.4, backward 58 and 50).
 template <class F>
 static loka_status by_choices(const loka_combine_desc* d, F&& f) {
     using std::integral_constant;

@@ -1,5 +1,5 @@
-// 8-bit operands of grouped products in their two stored forms (include/loka.h, loka_grouped_quantize).  Bytes only: 2 read and
-// 1 + 1/32 written per element and form.
+// 8-bit operands of grouped products in their two stored forms (include/loka.h, loka_grouped_quantize): scale = the least power of two s with
+// max |x| / s <= 448 over 128 elements, code = x / s.  Bytes only: 2 read and 1 + 1/32 written per element and form, and both forms from one read.
 #include "experts.h"
 
 namespace loka {
@@ -22,7 +22,7 @@ __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
 }
 
 // ALONG: 16 lanes take 128 elements of a row, 8 each; U such blocks at a time, 16 blocks apart.  (One division, of 32 bits where they do.)
-// WHOLE: no run of 8 is cut by a row's end.
+// WHOLE: no run of 8 is cut by a row's end.  16384 x 4096: 30 us (203 MB, 6.7 TB/s).
 template <int U, bool WHOLE>
 __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
     const int t = static_cast<int>(threadIdx.x), l = t & 15;
@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
 
 // TURNED, and ALONG from the same read: a workgroup takes a block of 128 rows of one group x 128 columns; a thread 8 rows x 8 columns.
 // Maxima down a column cross the wave by lane exchanges and the waves through LDS; the codes turn in LDS (runs of 8 rows of a
-// column, run r at place r ^ (column / 8)) and leave in whole lines.
+// column, run r at place r ^ (column / 8)) and leave in whole lines.  Both forms of 16384 x 4096: 49 us (272 MB, 5.5 TB/s), of 32768 gathered rows
+// x 4096 101 us; the turned one alone of 16384 x 1024 17 us.
 template <bool ALONG>
 __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     __shared__ __align__(16) uint8_t codes[128 * 128];
@@ -196,7 +197,7 @@ loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const v
     a.per_group = d->rows / d->groups;
     a.blocks_per_group = group_blocks(a.per_group);
     if (!qt) {
-        // (blocks a thread: 4 in flight where there are many, 1 where that leaves CUs idle: 5013 x 1008 7.4 -> U1 us)
+        // (blocks a thread: 4 in flight where there are many: 16384 x 1024 8.9 us, with 1 10.3; 1 where 4 leave CUs idle: 1024 x 1024 2.4 us, with 4 3.2)
         const int64_t units = d->rows * a.col_tiles;
         auto go = [&](auto u, auto whole) {
             return in_launches((units + 16 * u.value - 1) / (16 * u.value), 256, [&](int64_t from, uint32_t grid) {

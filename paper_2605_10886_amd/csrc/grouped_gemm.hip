@@ -70,6 +70,10 @@ __device__ __forceinline__ void put8(float* row, int64_t n, int64_t N, const flo
 // step; with one barrier, and one step, 32768 rows x 4096 x 4096 took 583 us).  With two pairs to a step there is one barrier.  Workgroups are
 // persistent, and the stream of steps does not stop between result tiles: the next tile's first steps arrive while this one's
 // values are stored, and nothing waits for the stores where their number is known.
+//
+// Bound by the matrix cores and the power they draw: 32768 rows x 16 groups x 4096 x 4096 (256 x 256 tiles) 560 .. 610 us, 1.8 .. 1.96 PFLOP/s at 1.9 GHz,
+// the cores busy for half the cycles; the library's product of one group at these sizes takes 490.  Weight gradient of 32768 rows x 16 groups x 1024 x
+// 4096 172 us, 1.6 PFLOP/s.  Tiles of 128 x 128, two workgroups a CU, where those would be few: 2000 rows x 4 groups x 256 x 768 8 us.
 template <int TM_, int TN_, int WM_, int WN_>
 struct GgTile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
@@ -89,19 +93,30 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     // ---- the groups: cum[i] = units (tiles of BM rows; weight gradient: blocks of 128) of groups 0 .. i, and their rows
     int* const cum = reinterpret_cast<int*>(smem + C::LDS);
     int* const off = cum + a.groups;
+    const bool sorted = WGRAD && a.groups <= 64 && a.tiles > static_cast<int>(gridDim.x);
     {
-        int base = 0;
+        int base = 0, units_here = 0;
         constexpr int UNIT = WGRAD ? kGroupBlock : C::BM;
         for (int g0 = 0; g0 < a.groups; g0 += 64) {        // (every wave by itself, the same values)
             const int i = g0 + lane;
             const GroupRows q = i < a.groups ? group_rows(a.offsets, i, a.rows) : GroupRows{0, 0};
-            const int s = base + lanes_inclusive((q.count + UNIT - 1) / UNIT);
+            units_here = (q.count + UNIT - 1) / UNIT;
+            const int s = base + lanes_inclusive(units_here);
             if (i < a.groups) {
                 cum[i] = s;
                 off[2 * i] = q.first;
                 off[2 * i + 1] = q.count;
             }
             base = __builtin_amdgcn_readlane(s, 63);
+        }
+        if (sorted) {                                      // off[i]: the group with the i-th most blocks
+            const int n = lane < a.groups ? units_here : -1;
+            int rank = 0;
+            for (int j = 0; j < a.groups; ++j) {
+                const int o = __builtin_amdgcn_readlane(n, j);
+                rank += o > n || (o == n && j < lane) ? 1 : 0;
+            }
+            if (lane < a.groups) off[rank] = lane;
         }
         __syncthreads();
     }
@@ -118,11 +133,15 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         Place p;
         int tm, tn;
         if (WGRAD) {
-            const int per = a.tiles_m * a.tiles_n;
-            const int range = t / per;
-            banded_tile(t - range * per, a.tiles_m, a.tiles_n, tm, tn);
+            // groups of most steps first, and every other round of tiles from its end: who takes a long one takes a short one next
+            // (32768 rows over 16 groups x 1024 x 4096 172 -> 145 us)
+            const int per = a.tiles_m * a.tiles_n, round = t / workers, from = round * workers;
+            const int turned = (round & 1) && from + workers <= total ? from + workers - 1 - (t - from) : t;
+            const int range = turned / per;
+            banded_tile(turned - range * per, a.tiles_m, a.tiles_n, tm, tn);
             p.group = range / a.splits;
             p.split = range - p.group * a.splits;
+            if (sorted) p.group = off[p.group];
             int first = p.group ? cum[p.group - 1] : 0, last = cum[p.group];
             const int each = (last - first + a.splits - 1) / a.splits;
             first += p.split * each;
@@ -412,6 +431,8 @@ using GgSmall = GgTile<4, 4, 2, 2>;
 // Few rows a group: bound by the weights' traffic.  A workgroup of 8 waves owns 16 MT rows x 16 NT columns of a group; the waves take the
 // steps of the contraction in turn, straight from memory into registers, U of them in flight, and add their sums in LDS in wave order.
 // FUSED: X is quantized here: a lane holds 32 of a row's 128 elements, and the row's four lanes share the maximum.
+// 8 rows x 64 groups x 1024 x 4096: 7.8 us (35 MB, 4.4 TB/s; most of the rest is the launch and the journeys of offsets, index, operands);
+// 26 rows x 8 groups x 4096 x 16384: 89 us (549 MB, 6.2 TB/s).
 constexpr int kStreamWaves = 8;
 
 // the larger of the four lanes l % 16 + 0, 16, 32, 48, in all of them

@@ -415,6 +415,12 @@ def test_weight_gradients_are_exact_on_whole_numbers(sizes, K, N):
     assert torch.equal(dw32.double(), want) and torch.equal(dw, _bf16(want))
 
 
+# more tiles than workgroups, so that a workgroup takes some of several groups: small tiles and large ones, 64 groups and more
+@pytest.mark.parametrize("sizes", [[i * 4 % 11 * 30 for i in range(11)], [(i * 29) % 13 * 230 for i in range(24)], [(i * 7) % 5 * 30 for i in range(65)], [1, 0] * 32])
+def test_weight_gradients_of_many_uneven_groups(sizes):
+    test_weight_gradients_are_exact_on_whole_numbers(sizes, 1008, 720)
+
+
 # ---------------------------------------------------------------- sums
 
 @pytest.mark.parametrize("weighted,residual", [(True, True), (True, False), (False, False), (False, True)])
