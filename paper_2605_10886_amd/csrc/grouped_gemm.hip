@@ -2,8 +2,7 @@
 // loka_grouped_linear, loka_grouped_wgrad), on v_mfma_scale_f32_16x16x128_f8f6f4.
 //
 // A lane of that instruction holds 32 codes of one row of each operand (row l % 16) and one scale byte for them; with a scale per 128
-// elements the four lanes of a row pass the same byte, the exponent field of the stored fp32 power of two.  The weights are the
-// first operand and their rows are dealt so that a lane holds 8 neighbouring columns of one row of the result per two instructions.
+// elements the four lanes of a row pass the same byte, the exponent field of the stored fp32 power of two.
 #include "experts.h"
 #include "gemm_common.h"
 
@@ -23,7 +22,7 @@ struct GgArgs {
     // element (row r, step k) of an operand lies r * row + k * step bytes from its start (scales: floats), a group's part of it `group` further on
     int64_t x_row, x_step, sx_row, sx_step, w_row, w_step, w_group, sw_row, sw_step, sw_group;
     int tiles_n, tiles_m, tiles;       // (tiles_m: weight gradient); tiles that there can be
-    bool wide;                         // rows of whole 16-byte runs
+    bool wide;                         // rows of whole runs of 4 columns
     const uint16_t* x;                 // few rows, quantized in the kernel: bf16 [x_rows, ldx]
     int64_t ldx, K;
 };
@@ -38,42 +37,40 @@ __device__ __forceinline__ v8i join(u32x4 a, u32x4 b) {
 // the scale operand from a stored scale (byte 255 where that is a NaN)
 __device__ __forceinline__ int scale_byte(uint32_t bits) { return static_cast<int>(bits >> 23); }
 
-// Eight columns n .. n + 7 of a row of N
-__device__ __forceinline__ void put8(uint16_t* row, int64_t n, int64_t N, const float (&f)[8]) {
-    const u32x4 v{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-    if (n + 8 <= N) *reinterpret_cast<u32x4_any*>(row + n) = v;
+// Four columns n .. n + 3 of a row of N
+__device__ __forceinline__ void put4(uint16_t* row, int64_t n, int64_t N, v4f f) {
+    if (n + 4 <= N) *reinterpret_cast<u32x2_any*>(row + n) = u32x2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
     else
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (n + e < N) row[n + e] = static_cast<uint16_t>(v[e >> 1] >> ((e & 1) * 16));
+        for (int e = 0; e < 4; ++e)
+            if (n + e < N) row[n + e] = static_cast<uint16_t>(f32_to_bf16_rne(f[e]));
 }
-__device__ __forceinline__ void put8(float* row, int64_t n, int64_t N, const float (&f)[8]) {
-    if (n + 8 <= N) {
-        *reinterpret_cast<u32x4_any*>(row + n) = __builtin_bit_cast(u32x4, v4f{f[0], f[1], f[2], f[3]});
-        *reinterpret_cast<u32x4_any*>(row + n + 4) = __builtin_bit_cast(u32x4, v4f{f[4], f[5], f[6], f[7]});
-    } else {
+__device__ __forceinline__ void put4(float* row, int64_t n, int64_t N, v4f f) {
+    if (n + 4 <= N) *reinterpret_cast<u32x4_any*>(row + n) = __builtin_bit_cast(u32x4, f);
+    else
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 4; ++e)
             if (n + e < N) row[n + e] = f[e];
-    }
 }
 
 // ---------------------------------------------------------------------------------
 // Tiles in LDS.  A workgroup of WM x WN waves computes BM x BN values, each wave TM x TN tiles of 16 x 16, in steps of 128 along the
 // contraction: 128 bytes a row, two steps in LDS (of the scales three).  The 16-byte chunks of a row lie permuted so that the 16 rows of a read use all
-// banks: chunk c of X's row r at place c ^ (r / 2 % 8), of W's row r, whose reads take rows 8 apart, at c ^ (bits 1, 3 and 4 of r).
+// banks: chunk c of row r at place c ^ (r / 2 % 8).  W's rows are dealt: row 16 j + r of a wave's 64 is column 4 r + j, so that a lane's four values of a row
+// are neighbours and 16 lanes store 128 bytes of it (with 64 bytes of each of 16 rows from 16 lanes each, 32768 rows x 1024 x 4096 took 192 us, so 177).
 //
 // A step is TM / 2 pairs of X's 16-row fragments against all of the wave's W fragments; a pair is read while the pair before it is
 // multiplied, W's fragments and the first pair of the next step during the last.  Two barriers a step, in front of the second pair and
 // of the last, give LDS back as soon as it is read: behind the first one W and the first two pairs of X of the step after next are
 // requested, behind the second X's other pairs, and each is awaited 1.5 steps later (a round trip through L2 under load is longer than a
-// step; with one barrier, and one step, 32768 rows x 4096 x 4096 took 583 us).  With two pairs to a step there is one barrier.  Workgroups are
+// step; with one barrier, and one step, 32768 rows x 4096 x 4096 took 583 us where this took 555).  With two pairs to a step there is one barrier.  Workgroups are
 // persistent, and the stream of steps does not stop between result tiles: the next tile's first steps arrive while this one's
 // values are stored, and nothing waits for the stores where their number is known.
 //
-// Bound by the matrix cores and the power they draw: 32768 rows x 16 groups x 4096 x 4096 (256 x 256 tiles) 560 .. 610 us, 1.8 .. 1.96 PFLOP/s at 1.9 GHz,
-// the cores busy for half the cycles; the library's product of one group at these sizes takes 490.  Weight gradient of 32768 rows x 16 groups x 1024 x
-// 4096 172 us, 1.6 PFLOP/s.  Tiles of 128 x 128, two workgroups a CU, where those would be few: 2000 rows x 4 groups x 256 x 768 8 us.
+// Bound by the matrix cores and the power they draw: 32768 rows x 16 groups x 4096 x 4096 (256 x 256 tiles) 555 .. 590 us by the card, 1.86 .. 1.98 PFLOP/s at
+// 1.9 GHz; loka_fp8_gemm_norm's kernel for one group of these sizes 490, this one 497: the rest is tiles that a group's end cuts and the last round.
+// x 1024 x 4096 177 us (158 without its stores), weight gradient 137, 2.0 PFLOP/s.  Tiles of 128 x 128, two workgroups a CU, where those would be few:
+// 4096 rows x 8 groups x 256 x 768 7 us.
 template <int TM_, int TN_, int WM_, int WN_>
 struct GgTile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NW = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
@@ -81,7 +78,7 @@ struct GgTile {
     static constexpr int PAIRS = TM / 2, LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64, LOADS = LX + LW + 1;
     static constexpr int FIRST = PAIRS == 4 ? LW + LX / 2 + 1 : LOADS, SECOND = LOADS - FIRST;      // loads behind the first barrier, and the second
     static constexpr int PER_CU = 163840 / (LDS + 12288);   // (with the table of 1024 groups)
-    static_assert(SROWS == NW && (PAIRS == 2 || PAIRS == 4) && LX == 4 && WM == 2 && TN % 2 == 0 && (NW == 4 || NW == 8));
+    static_assert(SROWS == NW && (PAIRS == 2 || PAIRS == 4) && LX == 4 && WM == 2 && TN == 4 && (NW == 4 || NW == 8));
 };
 
 template <class C, bool WGRAD>
@@ -134,7 +131,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         int tm, tn;
         if (WGRAD) {
             // groups of most steps first, and every other round of tiles from its end: who takes a long one takes a short one next
-            // (32768 rows over 16 groups x 1024 x 4096 172 -> 145 us)
+            // (32768 rows over 16 groups x 1024 x 4096 137 us, in the order of the groups 165)
             const int per = a.tiles_m * a.tiles_n, round = t / workers, from = round * workers;
             const int turned = (round & 1) && from + workers <= total ? from + workers - 1 - (t - from) : t;
             const int range = turned / per;
@@ -200,7 +197,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     const float* sp;
     int w_bytes;
     const int x_chunk = ((lane & 7) ^ ((lane >> 4) | ((wave & 1) << 2))) * 16;
-    const int w_row = static_cast<int>(a.w_row), w_lane = (lane >> 3) * w_row + ((lane & 7) ^ ((lane >> 4) & 1) ^ ((wave & 3) << 1)) * 16;
+    const int w_row = static_cast<int>(a.w_row), w_lane = (lane >> 3) * 4 * w_row + x_chunk;
     auto aim = [&](const Place& p) __attribute__((always_inline)) {
         auto inside = [&](int s) __attribute__((always_inline)) { return static_cast<int64_t>(s < 0 ? 0 : s >= a.x_rows ? a.x_rows - 1 : s); };
 #pragma unroll
@@ -223,9 +220,9 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     };
     auto request_one = [&](int stage, int i) __attribute__((always_inline)) {
         if (i < C::LW) {
-            const int k = i * C::NW + wave;
+            const int k = i * C::NW + wave, column = (k >> 3) * 64 + (k & 1) * 32 + ((k >> 1) & 3);
             const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wp), 0, w_bytes, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + k * 1024), 16, w_lane, k * 8 * w_row, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void*)(smem + stage + C::OFF_W + k * 1024), 16, w_lane, column * w_row, 0, 0);
             if (i == C::LW - 1) wp += a.w_step;
         } else if (i < C::LW + C::LX / 2) {
             request_x(stage, i - C::LW);
@@ -269,14 +266,13 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
     };
 
     // ---- operands
-    const int w_r = (r >> 2) * 8 + (r & 3);                // column, of the 32 of two tiles, that row r of the first one stands for
     int x_off[2], w_off[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         x_off[h] = (wm * TM * 16 + r) * 128 + ((g + 4 * h) ^ ((r >> 1) & 7)) * 16;
-        w_off[h] = C::OFF_W + (wn * TN * 16 + w_r) * 128 + ((g + 4 * h) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) * 16;
+        w_off[h] = C::OFF_W + (wn * TN * 16 + r) * 128 + ((g + 4 * h) ^ ((r >> 1) & 7)) * 16;
     }
-    const int sx_off = C::OFF_S + (wm * TM * 16 + r) * 4, sw_off = C::OFF_S + C::BM * 4 + (wn * TN * 16 + w_r) * 4;
+    const int sx_off = C::OFF_S + (wm * TM * 16 + r) * 4, sw_off = C::OFF_S + C::BM * 4 + (wn * TN * 16 + r * 4) * 4;
     u32x4 fx[2][2][2], fw[TN][2];
     uint32_t sx[2][2], sw[TN];
     int scales = 0;                    // where the scales lie that are read
@@ -287,13 +283,13 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         else sx[p & 1][f] = *reinterpret_cast<const uint32_t*>(smem + scales + sx_off + (2 * p + f) * 64);
     };
     auto read_w = [&](int stage, int j, int k) __attribute__((always_inline)) {
-        if (k < 2) fw[j][k] = *reinterpret_cast<const u32x4*>(smem + stage + coff_of(j) * 128 + w_off[k]);
-        else sw[j] = *reinterpret_cast<const uint32_t*>(smem + scales + sw_off + coff_of(j) * 4);
+        if (k < 2) fw[j][k] = *reinterpret_cast<const u32x4*>(smem + stage + j * 2048 + w_off[k]);
+        else sw[j] = *reinterpret_cast<const uint32_t*>(smem + scales + sw_off + j * 4);
     };
     v4f acc[TM][TN];
     auto multiply = [&](int p, int i) __attribute__((always_inline)) {
         const int j = i >> 1, f = i & 1;
-        acc[2 * p + f][j] = gg_mfma(join(fw[j][0], fw[j][1]), join(fx[p & 1][f][0], fx[p & 1][f][1]), acc[2 * p + f][j], scale_byte(sw[j]), scale_byte(sx[p & 1][f]));
+        acc[2 * p + f][j] = gg_mfma(join(fx[p & 1][f][0], fx[p & 1][f][1]), join(fw[j][0], fw[j][1]), acc[2 * p + f][j], scale_byte(sx[p & 1][f]), scale_byte(sw[j]));
     };
 
     int stage = 0;
@@ -314,7 +310,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
             for (int k = 0; k < 3; ++k) read_w(0, j, k);
     }
     // Where a tile's values left in STORES stores, the loads that were requested before them are awaited with the stores in flight.
-    constexpr int STORES = TM * TN / 2, NEWER = PAIRS == 4 ? C::LOADS : 0;
+    constexpr int STORES = TM * 4, NEWER = PAIRS == 4 ? C::LOADS : 0;
     int late = 0;
     auto landed = [&]() __attribute__((always_inline)) {
         if (late > 0) { --late; wait_vmcnt<NEWER + STORES>(); }
@@ -371,46 +367,54 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
             }
         }
 
-        // ---- lane (r, g) holds row 16 i + r, columns 32 (j / 2) + 8 g + 0 .. 7
+        // ---- lane (r, g) holds rows 16 i + 4 g + q, columns 4 r + j
         const int64_t row0 = WGRAD ? (static_cast<int64_t>(at.split) * a.groups + at.group) * a.M + at.m_first : static_cast<int64_t>(at.m_first);
-        if (a.wide) {                  // whole runs of 8 columns; what is past the result is dropped
-            const int N = static_cast<int>(a.N), n_lane = at.n0 + wn * TN * 16 + g * 8, o_lane = (wm * TM * 16 + r) * N + n_lane;
+        if (a.wide) {                  // whole runs of 4 columns; what is past the result is dropped
+            const int N = static_cast<int>(a.N), n_lane = at.n0 + wn * 64 + r * 4, o_lane = (wm * TM * 16 + g * 4) * N + n_lane;
             // (the offset is the vector register's alone: behind a 16-byte store with a scalar offset the compiler lets the next
             // instruction overwrite the data, and now and then the last lanes of its first register left with the new value)
             if (a.out) {
                 const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(a.out + row0 * a.N, 0, at.m_count * N * 2, 0x00020000);
+                int to = n_lane < N ? o_lane * 2 : 0x40000000;
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i) {
 #pragma unroll
-                    for (int j = 0; j < TN; j += 2) {
-                        const v4f u = acc[i][j], v = acc[i][j + 1];
-                        const u32x4 w{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3]), pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-                        __builtin_amdgcn_raw_buffer_store_b128(w, o, n_lane + j * 16 < N ? (o_lane + i * 16 * N + j * 16) * 2 : 0x7FFFFFFF, 0, 0);
+                    for (int q = 0; q < 4; ++q) {
+                        const u32x2 w{pack_bf16x2(acc[i][0][q], acc[i][1][q]), pack_bf16x2(acc[i][2][q], acc[i][3][q])};
+                        __builtin_amdgcn_raw_buffer_store_b64(w, o, to, 0, 0);
+                        to += q < 3 ? N * 2 : N * 26;
+                        asm volatile("" : "+v"(to));           // (else all rows' offsets are kept through the steps, in registers that these need)
                     }
+                }
             }
             if (a.y) {
                 const __amdgpu_buffer_rsrc_t o = __builtin_amdgcn_make_buffer_rsrc(a.y + row0 * a.N, 0, at.m_count * N * 4, 0x00020000);
+                int to = n_lane < N ? o_lane * 4 : 0x40000000;
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i) {
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), o,
-                                                               n_lane + (j >> 1) * 32 < N ? (o_lane + i * 16 * N + (j >> 1) * 32 + (j & 1) * 4) * 4 : 0x7FFFFFFF, 0, 0);
+                    for (int q = 0; q < 4; ++q) {
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v4f{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]}), o, to, 0, 0);
+                        to += q < 3 ? N * 4 : N * 52;
+                        asm volatile("" : "+v"(to));
+                    }
+                }
             }
             late = a.out && !a.y ? (PAIRS == 4 ? 3 : 1) : 0;
         } else {
+            int first = wm * TM * 16 + g * 4;
+            asm volatile("" : "+v"(first));
+            const int64_t n = at.n0 + wn * 64 + r * 4;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int row = (wm * TM + i) * 16 + r;
-                if (row >= at.m_count) continue;
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; j += 2) {
-                    const int64_t n = at.n0 + wn * TN * 16 + j * 16 + g * 8;
-                    const float f[8] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3], acc[i][j + 1][0], acc[i][j + 1][1], acc[i][j + 1][2], acc[i][j + 1][3]};
-                    if (a.out) put8(a.out + (row0 + row) * a.N, n, a.N, f);
-                    if (a.y) put8(a.y + (row0 + row) * a.N, n, a.N, f);
+                for (int q = 0; q < 4; ++q) {
+                    const int row = first + i * 16 + q;
+                    if (row >= at.m_count) continue;
+                    const v4f f{acc[i][0][q], acc[i][1][q], acc[i][2][q], acc[i][3][q]};
+                    if (a.out) put4(a.out + (row0 + row) * a.N, n, a.N, f);
+                    if (a.y) put4(a.y + (row0 + row) * a.N, n, a.N, f);
                 }
-            }
             late = 0;
         }
         if (tile + workers < total) at = locate(tile + workers);
@@ -599,7 +603,7 @@ template <class C, bool WGRAD>
 static loka_status gg_launch(GgArgs& a, int64_t tiles, hipStream_t stream) {
     a.tiles_n = static_cast<int>((a.N + C::BN - 1) / C::BN);
     a.tiles_m = WGRAD ? (a.M + C::BM - 1) / C::BM : 0;
-    a.wide = a.N % 8 == 0;
+    a.wide = a.N % 4 == 0;
     a.tiles = static_cast<int>(tiles);
     const int lds = C::LDS + 12 * a.groups;
     const int64_t slots = 256 * C::PER_CU;
