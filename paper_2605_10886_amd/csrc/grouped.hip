@@ -21,9 +21,17 @@ __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
     return s >= 0 && s < a.x_rows ? s : -1;
 }
 
+// Sources of 2^27 elements and more pass the last-level cache (256 MB) by, which cannot hold them (32768 x 4096: 61.5 us, else 72.0, both forms 90.5 and 105;
+// 16384 x 4096: 33.4 and 30.3, both forms 49.5 and 48.5).
+template <bool STREAMED>
+__device__ __forceinline__ u32x4 gq_load8(const uint16_t* p) {
+    if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+    return *reinterpret_cast<const u32x4_any*>(p);
+}
+
 // ALONG: 16 lanes take 128 elements of a row, 8 each; U such blocks at a time, 16 blocks apart.  (One division, of 32 bits where they do.)
 // WHOLE: no run of 8 is cut by a row's end.  16384 x 4096: 30 us (203 MB, 6.7 TB/s).
-template <int U, bool WHOLE>
+template <int U, bool WHOLE, bool STREAMED>
 __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
     const int t = static_cast<int>(threadIdx.x), l = t & 15;
     const int nb = a.col_tiles;
@@ -44,7 +52,7 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
             const int64_t s = gq_source(a, row);
             const int c = b * kGroupBlock + l * 8;
             if (WHOLE) {
-                if (s >= 0 && c < a.cols) v[u] = *reinterpret_cast<const u32x4_any*>(a.x + s * a.ld + c);
+                if (s >= 0 && c < a.cols) v[u] = gq_load8<STREAMED>(a.x + s * a.ld + c);
             } else if (s >= 0) {
                 v[u] = mx_load8(a.x + s * a.ld, c, a.cols);
             }
@@ -68,9 +76,9 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
 
 // TURNED, and ALONG from the same read: a workgroup takes a block of 128 rows of one group x 128 columns; a thread 8 rows x 8 columns.
 // Maxima down a column cross the wave by lane exchanges and the waves through LDS; the codes turn in LDS (runs of 8 rows of a
-// column, run r at place r ^ (column / 8)) and leave in whole lines.  Both forms of 16384 x 4096: 49 us (272 MB, 5.5 TB/s), of 32768 gathered rows
-// x 4096 101 us; the turned one alone of 16384 x 1024 17 us.
-template <bool ALONG>
+// column, run r at place r ^ (column / 8)) and leave in whole lines.  Both forms of 16384 x 4096: 49 us (272 MB, 5.5 TB/s), of 32768 x
+// 4096 90 us (6.0 TB/s); the turned one alone of 16384 x 1024 17 us.
+template <bool ALONG, bool STREAMED>
 __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     __shared__ __align__(16) uint8_t codes[128 * 128];
     __shared__ __align__(16) u32x4 maxima[4][16];
@@ -104,7 +112,7 @@ __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
         for (int i = 0; i < 8; ++i) {
             const int64_t s = source[rg * 8 + i];
             v[i] = u32x4{0u, 0u, 0u, 0u};
-            if (s >= 0 && !few) v[i] = *reinterpret_cast<const u32x4_any*>(a.x + s * a.ld + at);
+            if (s >= 0 && !few) v[i] = gq_load8<STREAMED>(a.x + s * a.ld + at);
         }
         if (ct * 128 + 128 > a.cols) {
 #pragma unroll
@@ -196,25 +204,31 @@ loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const v
     a.col_tiles = static_cast<int>(group_blocks(d->cols));
     a.per_group = d->rows / d->groups;
     a.blocks_per_group = group_blocks(a.per_group);
+    const bool streamed = a.rows * a.cols >= INT64_C(1) << 27;
     if (!qt) {
         // (blocks a thread: 4 in flight where there are many: 16384 x 1024 8.9 us, with 1 10.3; 1 where 4 leave CUs idle: 1024 x 1024 2.4 us, with 4 3.2)
         const int64_t units = d->rows * a.col_tiles;
-        auto go = [&](auto u, auto whole) {
+        auto go = [&](auto u, auto whole, auto past) {
             return in_launches((units + 16 * u.value - 1) / (16 * u.value), 256, [&](int64_t from, uint32_t grid) {
                 a.first_wg = from;
-                gq_along_kernel<u.value, whole.value><<<grid, 256, 0, stream>>>(a);
+                gq_along_kernel<u.value, whole.value, past.value><<<grid, 256, 0, stream>>>(a);
             });
         };
         const bool many = units >= 131072;
         using std::integral_constant;
-        if (d->cols % 8 == 0) return many ? go(integral_constant<int, 4>{}, std::true_type{}) : go(integral_constant<int, 1>{}, std::true_type{});
-        return many ? go(integral_constant<int, 4>{}, std::false_type{}) : go(integral_constant<int, 1>{}, std::false_type{});
+        const std::true_type yes;
+        const std::false_type no;
+        if (d->cols % 8 == 0 && streamed) return go(integral_constant<int, 4>{}, yes, yes);
+        if (d->cols % 8 == 0) return many ? go(integral_constant<int, 4>{}, yes, no) : go(integral_constant<int, 1>{}, yes, no);
+        return many ? go(integral_constant<int, 4>{}, no, no) : go(integral_constant<int, 1>{}, no, no);
     }
     const int64_t blocks = offsets ? loka_grouped_blocks(d->rows, d->groups) : a.blocks_per_group * d->groups;
     return in_launches(blocks * a.col_tiles, 256, [&](int64_t from, uint32_t grid) {
         a.first_wg = from;
-        if (q) gq_turned_kernel<true><<<grid, 256, 0, stream>>>(a);
-        else gq_turned_kernel<false><<<grid, 256, 0, stream>>>(a);
+        if (q && streamed) gq_turned_kernel<true, true><<<grid, 256, 0, stream>>>(a);
+        else if (q) gq_turned_kernel<true, false><<<grid, 256, 0, stream>>>(a);
+        else if (streamed) gq_turned_kernel<false, true><<<grid, 256, 0, stream>>>(a);
+        else gq_turned_kernel<false, false><<<grid, 256, 0, stream>>>(a);
     });
 }
 

@@ -189,6 +189,21 @@ def test_quantize_both_forms_of_gathered_rows(sizes, cols):
     assert torch.equal(alone.q[:n], q[:n]) and torch.equal(alone.scales[:n], s[:n])
 
 
+@pytest.mark.parametrize("cols", [1024, 1021])
+def test_quantize_more_than_the_caches_hold(cols):
+    """2^27 elements and more, against calls on parts of them."""
+    rows, each = (1 << 27) // cols + 300, 32768
+    x = torch.randn(rows, cols, device=DEV, generator=_gen(cols), dtype=torch.bfloat16)
+    r = B.loka_grouped_quantize(x, turned=True)
+    along, turned = B.loka_grouped_quantize(x), B.loka_grouped_quantize(x, along=False, turned=True)
+    assert torch.equal(along.q, r.q) and torch.equal(along.scales, r.scales) and torch.equal(turned.qt, r.qt) and torch.equal(turned.st, r.st)
+    for a in range(0, rows, each):
+        p = B.loka_grouped_quantize(x[a:a + each], turned=True)
+        n = len(p.qt)
+        assert torch.equal(r.q[a:a + each], p.q) and torch.equal(r.scales[a:a + each], p.scales)
+        assert torch.equal(r.qt[a // 128:a // 128 + n], p.qt) and torch.equal(r.st[a // 128:a // 128 + n], p.st)
+
+
 @pytest.mark.parametrize("E,K,N", [(1, 64, 64), (3, 100, 72), (5, 128, 256), (2, 300, 1000)])
 def test_quantize_weights(E, K, N):
     w = _randn(E * K, N, seed=E).bfloat16()
