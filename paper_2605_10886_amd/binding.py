@@ -374,7 +374,8 @@ RouteOut = namedtuple("RouteOut", "experts weights slots rows offsets")
 
 def loka_route(logits, top_k: int, score: int = SCORE_SOFTMAX, renorm: bool = True, scale: float = 1.0, workspace=None) -> RouteOut:
     """The top_k experts of each row of logits [tokens, experts] (bf16 or fp32), their weights fp32, and the routed order: slots
-    [tokens, top_k] (row of each choice), rows [tokens * top_k] (token of each row), offsets [experts + 1]; int32, on the device."""
+    [tokens, top_k] (row of each choice), rows [tokens * top_k] (token of each row), offsets [experts + 1]; int32, on the device.  All five
+    are parts of one allocation."""
     return tuple.__new__(RouteOut, (_native or _host()).route(logits, top_k, score, renorm, scale, workspace))
 
 

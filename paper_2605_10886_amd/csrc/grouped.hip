@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void gq_along_kernel(const GqArgs a) {
 // TURNED, and ALONG from the same read: a workgroup takes a block of 128 rows of one group x 128 columns; a thread 8 rows x 8 columns.
 // Maxima down a column cross the wave by lane exchanges and the waves through LDS; the codes turn in LDS (runs of 8 rows of a
 // column, run r at place r ^ (column / 8)) and leave in whole lines.  Both forms of 16384 x 4096: 49 us (272 MB, 5.5 TB/s), of 32768 x
-// 4096 90 us (6.0 TB/s); the turned one alone of 16384 x 1024 17 us.
+// 4096 90 us (6.0 TB/s); the turned one alone of 32768 gathered rows x 1024 18 us.
 template <bool ALONG, bool STREAMED>
 __global__ __launch_bounds__(256) void gq_turned_kernel(const GqArgs a) {
     __shared__ __align__(16) uint8_t codes[128 * 128];

@@ -96,7 +96,8 @@ def test_grouped_product_refusals():
     for form in (-1, 2):
         assert gemm(desc(w_form=form)) == linear(desc(w_form=form)) == UNSUPPORTED
     assert linear(desc(), ld=15) == SHAPE
-    many = desc(rows=4096)
+    assert B.lib().loka_grouped_linear_workspace(ref(desc()), 0) == 0                   # (quantized inside the product)
+    many = desc(rows=4096, N=1024)
     need = B.lib().loka_grouped_linear_workspace(ref(many), 0)
     assert need >= 4096 * 128 + 4096 * 4 and linear(many, ws=None, nws=0) == linear(many, nws=need - 1) == WORKSPACE and linear(many, ws=OTHER, nws=need) == ALIGN
 
