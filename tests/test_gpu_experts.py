@@ -578,3 +578,98 @@ def test_operands_beyond_four_gigabytes():
         assert torch.equal(got, _bf16(torch.cat([v[:n // 2] @ w[0].double(), v[n // 2:] @ w[1].double()])))
     del x
     torch.cuda.empty_cache()
+
+
+def test_results_beyond_four_gigabytes():
+    """1.1 million rows x 2112: results, their sums and gradients on both sides of 2^32 bytes."""
+    n, K, N = (1 << 20) + 70000, 64, 2112
+    x, w = _small((n, K), 1), _small((3, K, N), 2)
+    bounds = [0, 1000003, 1000003, n]
+    wq, xq = B.loka_grouped_quantize(w.view(3 * K, N), groups=3, along=False, turned=True), B.loka_grouped_quantize(x)
+    y, _ = B.loka_grouped_gemm(B.make_grouped_desc(n, N, K, 3), xq.q, xq.scales, wq.qt, wq.st, _i32(bounds))
+    rows = torch.cat([torch.arange(a, a + 700) for a in (0, (1 << 31) // (2 * N) - 300, 999700, (1 << 32) // (2 * N) - 300, n - 700)]).to(DEV)
+    which = torch.where(rows < 1000003, 0, 2)
+    want = torch.empty(len(rows), N, dtype=torch.float64, device=DEV)
+    for e in (0, 2):
+        want[which == e] = x[rows[which == e]].double() @ w[e].double()
+    assert torch.equal(y[rows], _bf16(want))
+    # two rows a token
+    slots = torch.stack([torch.arange(0, n // 2, device=DEV), torch.arange(n // 2, n // 2 * 2, device=DEV)], 1).int().contiguous()
+    out = B.loka_combine(y, slots)
+    t = torch.tensor([0, 1, n // 4, n // 2 - 1], device=DEV)
+    assert torch.equal(out[t], _bf16(y[t].double() + y[t + n // 2].double()))
+    dout = out.clone()
+    dy, dw = B.loka_combine_backward(dout, y, slots)
+    assert torch.equal(dy[t], dout[t]) and torch.equal(dy[t + n // 2], dout[t])
+    exact = torch.stack([(dout[t].double() * y[t].double()).sum(1), (dout[t].double() * y[t + n // 2].double()).sum(1)], 1)
+    size = torch.stack([(dout[t].double() * y[t].double()).abs().sum(1), (dout[t].double() * y[t + n // 2].double()).abs().sum(1)], 1)
+    assert bool(((dw[t].double() - exact).abs() <= (N / 256 + 10) * P.F32 * size).all())     # sums of 16 elements a lane at most, then lanes and waves
+    del out, dout, dw
+    # both stored forms of it, against the parts that hold its ends
+    r = B.loka_grouped_quantize(y, offsets=_i32(bounds), turned=True)
+    for a, b in ((0, 1280), (1000003 - 1000003 % 128, 1000003), (n - 1280, n)):
+        p = B.loka_grouped_quantize(y[a:b])
+        assert torch.equal(r.q[a:b], p.q) and torch.equal(r.scales[a:b], p.scales)
+    blocks = 1000003 // 128 + 1                                                               # of the first group
+    for a, b, block in ((0, 1280, 0), (1000003 // 128 * 128, 1000003, 1000003 // 128), (1000003 + 69000 // 128 * 128, 1000003 + 69000 // 128 * 128 + 1280, blocks + 69000 // 128)):
+        p = B.loka_grouped_quantize(y[a:b], along=False, turned=True)
+        assert torch.equal(r.qt[block:block + len(p.qt)], p.qt) and torch.equal(r.st[block:block + len(p.st)], p.st)
+    del r, y, dy
+    torch.cuda.empty_cache()
+
+
+def test_a_training_step_in_a_graph():
+    """Every call of a step captured, replayed on other inputs with eager work between.  Long groups of few results: partial sums."""
+    T, E, k, K, N = 3000, 3, 2, 200, 136
+    x, dout, logits = torch.zeros(T, K, dtype=torch.bfloat16, device=DEV), torch.zeros(T, N, dtype=torch.bfloat16, device=DEV), torch.zeros(T, E, device=DEV)
+    w = (_randn(E, K, N, seed=3) / math.sqrt(K)).bfloat16()
+    assert B.lib().loka_grouped_wgrad_workspace(B.make_grouped_desc(T * k, N, K, E)) > 0
+
+    def step():
+        wq = B.loka_grouped_quantize(w.view(E * K, N), groups=E, turned=True)
+        r, d, y, out = _layer(x, logits, w, wq, k)
+        dy, dweights = B.loka_combine_backward(dout, y, r.slots, r.weights)
+        xt = B.loka_grouped_quantize(x, offsets=r.offsets, index=r.rows, along=False, turned=True)
+        yq = B.loka_grouped_quantize(dy, offsets=r.offsets, turned=True)
+        dxr, _ = B.loka_grouped_gemm(B.make_grouped_desc(T * k, K, N, E, turned_w=False), yq.q, yq.scales, wq.q, wq.scales, r.offsets)
+        dw, dw32 = B.loka_grouped_wgrad(d, xt.qt, xt.st, yq.qt, yq.st, r.offsets, want_y=True)
+        return out, B.loka_combine(dxr, r.slots), dw, dw32, B.loka_route_backward(logits, r.experts, dweights)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            graphs.append((g, step()))
+    for i in range(5):
+        x.copy_(_randn(T, K, seed=3 * i).bfloat16())
+        dout.copy_(_randn(T, N, seed=3 * i + 1).bfloat16())
+        logits.copy_(_randn(T, E, seed=3 * i + 2))
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        want = step()
+        for _, got in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_outputs_of_the_choice_are_ordinary_tensors():
+    logits = _randn(70, 9, seed=1)
+    with torch.inference_mode():
+        inside = B.loka_route(logits, 4)
+        total = inside.weights.sum(1)
+    r = B.loka_route(logits, 4)
+    assert bool((total - 1).abs().max() <= 8 * P.F32) and all(torch.equal(a, b) for a, b in zip(inside, r))
+    # written and differentiated like any other, and no part reaches another
+    keep = [t.clone() for t in r]
+    r.weights.mul_(2.0)
+    r.slots.fill_(-1)
+    assert torch.equal(r.weights, keep[1] * 2) and all(torch.equal(r[i], keep[i]) for i in (0, 3, 4))
+    a = keep[1].requires_grad_(True)
+    r.weights.requires_grad_(True)
+    (r.weights * r.weights).sum().backward()
+    assert torch.equal(r.weights.grad, 2 * r.weights.detach()) and a.grad is None
