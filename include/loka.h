@@ -490,8 +490,8 @@ loka_status loka_grouped_gemm(const loka_grouped_desc* desc, const uint8_t* xq, 
 
 /* The same from bf16 tokens x [x_rows (without index: rows), ld], quantized in the call: the results of loka_grouped_quantize (ALONG)
  * and loka_grouped_gemm, for a serving loop's single tokens up to whole batches.
- * Workspace: loka_grouped_linear_workspace(desc, with_index) bytes, 16-byte aligned (codes and scales of x; 0 where few rows a group are
- * quantized inside the product). */
+ * Workspace: loka_grouped_linear_workspace(desc, with_index) bytes, 16-byte aligned (codes and scales of x, all x_rows of it; 0 where few
+ * rows a group are quantized inside the product). */
 size_t loka_grouped_linear_workspace(const loka_grouped_desc* desc, int with_index);
 loka_status loka_grouped_linear(const loka_grouped_desc* desc, const void* x_bf16, int64_t ld, const int32_t* index, const int32_t* offsets,
                                 const uint8_t* wq, const float* sw, void* out_bf16, float* y_fp32, void* workspace, size_t ws_bytes,
