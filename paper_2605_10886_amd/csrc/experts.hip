@@ -12,18 +12,25 @@ namespace loka {
 // bf16's key has room for the entry as well, so that all keys differ and the largest one is the choice; the next one is the largest below
 // it, and no key has to be struck out.
 //
-// Bound by the vector unit's top_k passes over the keys: 32768 x 256 bf16 logits, 8 choices, 14.4 us (the 17 MB read alone: 3), their
+// Bound by the vector unit's top_k passes over the keys: 32768 x 256 bf16 logits, 8 choices, 13.5 us (the 17 MB read alone: 3), their
 // places 7.6.  A token alone: 5.2 us with the launch, of which the logits' journey and top_k exchanges are most.
 constexpr int kRouteMostChunk = 128;   // tokens of a workgroup, at most
 constexpr int kRouteThreads = 256;     // ... and its threads, of a small call and of the gradient
 constexpr int kRouteMost = 1024;       // ... of a call of more tokens
 
 __device__ __forceinline__ uint32_t key_of(float x) {
-    if (x != x) return 0xFFC00000u;                        // above plus infinity
-    const uint32_t b = __float_as_uint(x + 0.0f);          // (-0 and +0 are equal)
-    return b == 0xFF800000u ? 0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+    x += 0.0f;                                             // (-0 and +0 are equal)
+    const uint32_t b = x != x ? 0x7FC00000u : __float_as_uint(x);          // (a NaN: above plus infinity)
+    return (b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u)) - 0x007FFFFFu;       // (of minus infinity, the least: 0)
 }
-__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+__device__ __forceinline__ float value_of(uint32_t key) {
+    const uint32_t k = key + 0x007FFFFFu;
+    return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
+// A bf16's key, and 1023 - its entry in the lower bits; below kNone: may not be chosen.  The upper bits that key_of gives a bf16 (0x7F80 to plus zero) say which it was.
+constexpr uint32_t kNone = 1024;
+__device__ __forceinline__ uint32_t short_key(uint32_t key, int entry) { return ((key >> 6) & ~1023u) | (1023u - static_cast<unsigned>(entry)); }
+__device__ __forceinline__ float value_of_short(uint32_t k) { return value_of((k >> 10 << 16) | (k >= 0x7F80u << 10 ? 1u : 0u)); }
 
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -144,10 +151,11 @@ __global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 key[v] = key_of(x[v]);
-                if (BF16) key[v] = key[v] ? (key[v] >> 16 << 10) | (1023u - static_cast<unsigned>(entry_of<L, R>(l, v))) : 0u;
+                if (BF16) key[v] = short_key(key[v], entry_of<L, R>(l, v));
             }
         }
-        auto number = [](uint32_t k) __attribute__((always_inline)) { return value_of(BF16 ? (k >> 25 ? k >> 10 << 16 : k >> 10 << 16 | 0xFFFFu) : k); };
+        auto number = [](uint32_t k) __attribute__((always_inline)) { return BF16 ? value_of_short(k) : value_of(k); };
+        constexpr uint32_t LEAST = BF16 ? kNone : 1;       // key of what may be chosen
         float all = 0.f;
         if (a.score == LOKA_SCORE_SOFTMAX && !a.renorm) {
             uint32_t m = 0;
@@ -155,7 +163,7 @@ __global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a
             for (int v = 0; v < V; ++v) m = key[v] > m ? key[v] : m;
             const float top = number(lanes_max_bits<L>(m));
 #pragma unroll
-            for (int v = 0; v < V; ++v) all += key[v] ? expf(number(key[v]) - top) : 0.f;
+            for (int v = 0; v < V; ++v) all += key[v] >= LEAST ? expf(number(key[v]) - top) : 0.f;
             all = lanes_sum<L>(all);
         }
         int mine = -1;                 // lane j: choice j
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(THREADS) void route_choose_kernel(const RouteArgs a
                 for (int v = 0; v < V; ++v) key[v] = entry_of<L, R>(l, v) == e ? 0u : key[v];
             }
             if (j == 0) top_key = m;
-            if (l == j && m) { mine = e; mine_key = m; }
+            if (l == j && m >= LEAST) { mine = e; mine_key = m; }
         }
         const float x = number(mine_key), top = number(top_key);
         float w = 0.f;
@@ -334,7 +342,7 @@ __global__ __launch_bounds__(kRouteMost) void route_place_kernel(const RouteArgs
 //   softmax           q_e (g_e - sum_i g_i q_i), g_e = 0 where not chosen
 //   sigmoid, renorm   q_j (g_j - sum_i g_i q_i) (1 - s_j)            others 0
 //   sigmoid           g_j s_j (1 - s_j)                              others 0
-// Bytes only: 32768 x 256 bf16 7.8 us (17 MB written, and 2 read where only the chosen entries are), softmax over all 14.2 (an exponential each).
+// Bytes only: 32768 x 256 bf16 7.8 us (17 MB written, and 2 read where only the chosen entries are), softmax over all 13.5 (an exponential each).
 template <int L, int V, int R, bool BF16>
 __global__ __launch_bounds__(kRouteThreads) void route_backward_kernel(const RouteArgs a) {
     constexpr int PER = kRouteThreads / L;
@@ -432,9 +440,9 @@ static int route_pitch(int experts) {
     while (p < experts) p *= 2;
     return p;
 }
-// Tokens of a workgroup: all of a small call's (one launch: 64 tokens of 64 experts, 8 choices, 5.2 us, in two launches 7.2), else as few as leave
-// 256 workgroups, each of which adds up the counts of all (300 tokens of 160 experts, 6 choices, 8.5 us with 16 of a workgroup, 13.7 with 128;
-// 32768 of 256, 8 choices, 35.8 with 16, 20.7 with 128).
+// Tokens of a workgroup: all of a small call's (one launch: 64 tokens of 64 experts, 8 choices, 5.3 us, in two launches 7.2), else as few as leave
+// 256 workgroups, each of which adds up the counts of all (300 tokens of 160 experts, 6 choices, 8.2 us with 16 of a workgroup, 12.8 with 128;
+// 32768 of 256, 8 choices, 34.8 with 16, 19.9 with 128).
 static int64_t route_chunk(const loka_route_desc* d) {
     if (d->tokens <= 64) return 64;
     int64_t c = 16;
@@ -447,8 +455,9 @@ size_t route_workspace_bytes(const loka_route_desc* d) {
 }
 
 // Lanes, logits a lane and their runs: by the number of experts, and in runs of 16 bytes (8 where a lane has four bf16) where rows are whole runs.
-// 16 lanes a token keep its exchanges inside the vector unit's rows and share a wave among four tokens (32768 x 256, 8 choices, 20.6 us; 32 lanes
-// 24.5, 64 lanes 33.5); more than 256 logits are too many for them (32768 x 512 on 64 lanes 41.4 us, on 32 44.9).
+// 16 lanes a token keep its exchanges inside the vector unit's rows and share a wave among four tokens (32768 x 256, 8 choices, 19.7 us; 32 lanes
+// 23.7, 64 lanes 32.8); more than 256 logits are too many for them (32768 x 512 on 64 lanes 39.9 us and the gradient of a softmax over all 25.3, on 32
+// 39.9 and 35.0).
 template <class F>
 static void by_experts(const loka_route_desc* d, const void* logits, const void* dlogits, F&& f) {
     auto with = [&](auto l, auto v) {
@@ -502,7 +511,7 @@ loka_status route_launch(const loka_route_desc* d, const void* logits, int32_t* 
     if (a.chunks == 1) return LOKA_OK;
     const size_t place = static_cast<size_t>(d->experts) * 12 + 64;
     // A workgroup adds up every chunk's counts, chunks^2 in all, where that takes no longer than a launch that does it once (32768 x 64, 8
-    // choices, 13.9 us, with the launch 14.3; 65536 x 256 39.4 and 34.6)
+    // choices, 13.6 us, with the launch 14.1; 65536 x 256 37.6 and 32.7)
     if (a.chunks <= 256) {
         route_place_kernel<false><<<a.chunks, kRouteMost, place, stream>>>(a);
     } else {
