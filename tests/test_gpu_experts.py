@@ -311,7 +311,8 @@ def test_products_are_exact_on_whole_numbers(sizes, K, N):
 # sizes of which each form of the product takes some: 16 rows at a time and 64, 32 or 16 columns, 32 rows at a time, small tiles, large ones
 FORMS = [([7] * 16, 700, 520), ([1, 0, 9], 1000, 2000), ([31] * 16, 700, 100), ([5, 16, 17], 2000, 301), ([16] * 40, 2000, 301), ([20, 0, 33, 31, 32, 1], 2000, 2003),
          ([900, 0, 901, 127, 2000], 100, 520), ([300] * 16, 100, 517), ([2499, 1, 2501, 0, 0, 700], 130, 301), ([40] * 300, 200, 300), ([900, 1100, 255, 257, 1500], 300, 2000),
-         ([2500, 2501], 300, 2003), ([300] * 16, 385, 2000), ([0] * 70 + [3000, 1, 0, 2000], 700, 1500), ([0] * 70 + [9000, 1, 8999], 300, 260)]
+         ([2500, 2501], 300, 2003), ([300] * 16, 385, 2000), ([0] * 70 + [3000, 1, 0, 2000], 700, 1500), ([0] * 70 + [9000, 1, 8999], 300, 260), ([0] * 1022 + [9000, 9000], 300, 260),
+         ([480 + i % 7 * 9 for i in range(1024)], 128, 512)]
 
 
 @pytest.mark.parametrize("sizes,K,N", FORMS)
@@ -434,6 +435,10 @@ def test_weight_gradients_are_exact_on_whole_numbers(sizes, K, N):
 @pytest.mark.parametrize("sizes", [[i * 4 % 11 * 30 for i in range(11)], [(i * 29) % 13 * 230 for i in range(24)], [(i * 7) % 5 * 30 for i in range(65)], [1, 0] * 32])
 def test_weight_gradients_of_many_uneven_groups(sizes):
     test_weight_gradients_are_exact_on_whole_numbers(sizes, 1008, 720)
+
+
+def test_weight_gradients_of_the_most_groups():
+    test_weight_gradients_are_exact_on_whole_numbers([i * 5 % 3 * 70 for i in range(1024)], 130, 72)
 
 
 # ---------------------------------------------------------------- sums
