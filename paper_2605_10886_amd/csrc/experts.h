@@ -34,6 +34,11 @@ constexpr int kGroupBlock = 128;       // elements that share a scale
 static inline int64_t group_blocks(int64_t n) { return (n + kGroupBlock - 1) / kGroupBlock; }
 
 #ifdef __HIPCC__
+// Units of `unit` rows that `count` rows (0 .. 2^31 - 1) take; in unsigned numbers, as count + unit - 1 may be more than an int holds
+__host__ __device__ constexpr int units_of(int count, int unit) {
+    return static_cast<int>((static_cast<uint32_t>(count) + static_cast<uint32_t>(unit) - 1u) / static_cast<uint32_t>(unit));
+}
+static_assert(units_of(0, 128) == 0 && units_of(1, 256) == 1 && units_of(INT32_MAX, 16) == 1 << 27 && units_of(INT32_MAX, 128) == 1 << 24 && units_of(INT32_MAX, 256) == 1 << 23);
 // The rows of a group from the device's offsets; whatever they hold, first and count stay within `rows`.
 struct GroupRows { int first, count; };
 __device__ __forceinline__ GroupRows group_rows(const int32_t* offsets, int g, int rows) {
@@ -58,7 +63,7 @@ __device__ __forceinline__ UnitAt find_unit(const int32_t* offsets, int groups, 
     int base = 0;
     for (int g0 = 0; g0 < groups; g0 += 64) {
         const GroupRows r = g0 + lane < groups ? group_rows(offsets, g0 + lane, rows) : GroupRows{0, 0};
-        const int n = (r.count + unit - 1) / unit, s = lanes_inclusive(n);
+        const int n = units_of(r.count, unit), s = lanes_inclusive(n);
         const unsigned long long past = __builtin_amdgcn_ballot_w64(base + s > target);
         if (past) {
             const int l = __builtin_ctzll(past), before = base + __builtin_amdgcn_readlane(s - n, l);

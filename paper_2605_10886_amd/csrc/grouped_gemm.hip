@@ -97,7 +97,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
         for (int g0 = 0; g0 < a.groups; g0 += 64) {        // (every wave by itself, the same values)
             const int i = g0 + lane;
             const GroupRows q = i < a.groups ? group_rows(a.offsets, i, a.rows) : GroupRows{0, 0};
-            units_here = (q.count + UNIT - 1) / UNIT;
+            units_here = units_of(q.count, UNIT);
             const int s = base + lanes_inclusive(units_here);
             if (i < a.groups) {
                 cum[i] = s;
@@ -160,7 +160,7 @@ __device__ __forceinline__ void gg_tiles(const GgArgs& a, uint8_t* smem) {
             p.group = g0 + __builtin_ctzll(past);          // (u is less than the last sum)
             const int before = p.group ? cum[p.group - 1] : 0;
             const int first = __builtin_amdgcn_readfirstlane(off[2 * p.group]), count = __builtin_amdgcn_readfirstlane(off[2 * p.group + 1]);
-            const int tiles_m = (count + C::BM - 1) / C::BM;
+            const int tiles_m = units_of(count, C::BM);
             const int local = t - __builtin_amdgcn_readfirstlane(before) * a.tiles_n;
             banded_tile(local, tiles_m, a.tiles_n, tm, tn);
             p.m_first = first + tm * C::BM;
