@@ -625,7 +625,6 @@ loka_status loka_route_backward(const loka_route_desc* desc, const void* logits,
 }
 
 constexpr int64_t kMostWidth = INT64_C(1) << 20;       // of a layer of experts, so that a tile's rows lie within 32-bit offsets
-constexpr int32_t kMostGroups = 1024;
 
 int64_t loka_grouped_blocks(int64_t rows, int64_t groups) {
     if (rows <= 0 || rows > INT32_MAX || groups <= 0 || groups > kMostGroups) return -1;

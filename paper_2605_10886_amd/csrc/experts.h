@@ -31,6 +31,7 @@ loka_status grouped_wgrad_launch(const loka_grouped_desc* d, const uint8_t* xt, 
                                  const int32_t* offsets, void* dw, float* dw32, void* ws, hipStream_t stream);
 
 constexpr int kGroupBlock = 128;       // elements that share a scale
+constexpr int32_t kMostGroups = 1024;
 static inline int64_t group_blocks(int64_t n) { return (n + kGroupBlock - 1) / kGroupBlock; }
 
 #ifdef __HIPCC__

@@ -77,7 +77,7 @@ struct GgTile {
     static constexpr int OFF_W = BM * 128, STAGE = OFF_W + BN * 128, OFF_S = 2 * STAGE, SCALES = (BM + BN) * 4, LDS = OFF_S + 3 * SCALES;
     static constexpr int PAIRS = TM / 2, LX = BM / (8 * NW), LW = BN / (8 * NW), SROWS = (BM + BN) / 64, LOADS = LX + LW + 1;
     static constexpr int FIRST = PAIRS == 4 ? LW + LX / 2 + 1 : LOADS, SECOND = LOADS - FIRST;      // loads behind the first barrier, and the second
-    static constexpr int PER_CU = 163840 / (LDS + 12288);   // (with the table of 1024 groups)
+    static constexpr int MOST_LDS = LDS + 12 * kMostGroups, PER_CU = 163840 / MOST_LDS;     // (with the table of the groups)
     static_assert(SROWS == NW && (PAIRS == 2 || PAIRS == 4) && LX == 4 && WM == 2 && TN == 4 && (NW == 4 || NW == 8));
 };
 
@@ -607,8 +607,9 @@ static loka_status gg_launch(GgArgs& a, int64_t tiles, hipStream_t stream) {
     a.tiles = static_cast<int>(tiles);
     const int lds = C::LDS + 12 * a.groups;
     const int64_t slots = 256 * C::PER_CU;
-    // (on every call, a host-side table write: no process-wide state, and correct on whichever device is current)
-    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&gg_tile_kernel<C, WGRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    // (on every call, a host-side table write, and correct on whichever device is current; the same value whatever the call's groups, as another
+    // thread may set it between this and the launch)
+    LOKA_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(&gg_tile_kernel<C, WGRAD>), hipFuncAttributeMaxDynamicSharedMemorySize, C::MOST_LDS));
     gg_tile_kernel<C, WGRAD><<<static_cast<uint32_t>(tiles < slots ? tiles : slots), 64 * C::NW, lds, stream>>>(a);
     LOKA_HIP_TRY(hipGetLastError());
     return LOKA_OK;
