@@ -395,7 +395,8 @@ def loka_grouped_quantize(x, groups: int = 1, offsets=None, index=None, along: b
                           qt=None, st=None) -> GroupedOut:
     """x bf16 [rows, cols], or its rows `index` in their order, as operands of grouped products.  along: codes [rows, colsp] and scales
     [rows, colsp / 128]; turned: codes [blocks, cols, 128] and scales [blocks, cols], blocks of 128 rows of one group.  The groups are
-    those of `offsets`, or `groups` equal ones (weights [groups, K, N] as [groups * K, N]).  What is not asked for is None."""
+    those of `offsets`, or `groups` equal ones (weights [groups, K, N] as [groups * K, N]).  A buffer that is given (q, scales, qt, st) asks for its
+    form as well.  What is not asked for is None."""
     return tuple.__new__(GroupedOut, (_native or _host()).grouped_quantize(x, groups, offsets, index, along, turned, q, scales, qt, st))
 
 

@@ -673,8 +673,11 @@ PyObject* grouped_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0]);
     const long long groups = PyLong_AsLongLong(a[1]);
     const at::Tensor offsets = given(a[2]), index = given(a[3]);
-    const int along = PyObject_IsTrue(a[4]), turned = PyObject_IsTrue(a[5]);
+    int along = PyObject_IsTrue(a[4]), turned = PyObject_IsTrue(a[5]);
     if (PyErr_Occurred()) return nullptr;
+    at::Tensor q = given(a[6]), s = given(a[7]), qt = given(a[8]), st = given(a[9]);
+    along |= q.defined() || s.defined();       // (a buffer that is given is written)
+    turned |= qt.defined() || st.defined();
     if (!is_rows(x)) return refuse("x: bf16 [rows, cols] with contiguous rows");
     if (offsets.defined() && !(holds(offsets, at::kInt, 2) && offsets.dim() == 1)) return refuse("offsets: contiguous int32 [groups + 1]");
     if (index.defined() && !(holds(index, at::kInt, 0) && index.dim() == 1)) return refuse("index: contiguous int32 [rows]");
@@ -684,7 +687,6 @@ PyObject* grouped_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (g <= 0 || g > 1024 || d.rows <= 0 || d.rows >= kMost || x.size(0) <= 0 || d.cols <= 0 || d.cols >= kMost || (!offsets.defined() && d.rows % g)) return fail(LOKA_ERR_SHAPE, "loka_grouped_quantize");
     const int64_t kb = (d.cols + 127) / 128, blocks = offsets.defined() ? loka_grouped_blocks(d.rows, g) : (d.rows / g + 127) / 128 * g;
     const at::Device dev = x.device();
-    at::Tensor q = given(a[6]), s = given(a[7]), qt = given(a[8]), st = given(a[9]);
     if (!on_gpu(dev, {&offsets, &index, &q, &s, &qt, &st})) return refuse("tensors on one GPU");
     const c10::DeviceGuard guard(dev);
     if (along) {
@@ -697,8 +699,6 @@ PyObject* grouped_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!st.defined()) st = empty({blocks, d.cols}, at::kFloat, dev);
         if (!holds(qt, at::kByte, blocks * d.cols * 128) || !holds(st, at::kFloat, blocks * d.cols)) return refuse("qt, st: contiguous uint8 [blocks, cols, 128] and fp32 [blocks, cols]");
     }
-    if (!along) q = s = at::Tensor();
-    if (!turned) qt = st = at::Tensor();
     void* st_ = stream_of(dev);
     const loka_status status = unlocked([&] {
         return loka_grouped_quantize(&d, ptr(x), at_or_null<int32_t>(index), at_or_null<int32_t>(offsets), at_or_null<uint8_t>(q), at_or_null<float>(s),
