@@ -508,7 +508,7 @@ loka_status loka_grouped_wgrad(const loka_grouped_desc* desc, const uint8_t* xt,
 
 /* out[t] = sum over j of weight[t, j] * y[slot[t, j]] (+ residual[t]), fp32 sums in the order of j, one rounding to bf16.  A slot outside
  * 0 .. rows - 1 adds nothing.  y_bf16 [rows, cols]; weight fp32 [tokens, top_k] or NULL (1: the sum that dX's rows take); residual
- * bf16 [tokens, cols] or NULL; out bf16 [tokens, cols], which may be the residual itself.  Matrices are contiguous; pointers 16-byte (slot, weight: 4-byte) aligned.
+ * bf16 [tokens, cols] or NULL; out bf16 [tokens, cols], which may be the residual itself.  Matrices are contiguous; any alignment of an element.
  * Backward: dy[slot[t, j]] = weight[t, j] * dout[t] (bf16; rows that no slot names are left as they were) and dweight[t, j] =
  * sum over the columns of dout[t] * y[slot[t, j]] (fp32, a fixed order; 0 for a slot outside).  dy or dweight may be NULL, y where dweight is.
  * Slots name different rows, as loka_route's do. */

@@ -737,7 +737,7 @@ loka_status loka_combine(const loka_combine_desc* desc, const void* y_bf16, cons
     if (!desc || !y_bf16 || !slot || !out_bf16) return LOKA_ERR_NULL;
     const loka_status st = validate_combine(desc);
     if (st != LOKA_OK) return st;
-    if (!aligned16(y_bf16) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned16(residual_bf16) || !aligned16(out_bf16)) return LOKA_ERR_ALIGN;
+    if (!aligned_to(y_bf16, 2) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned_to(residual_bf16, 2) || !aligned_to(out_bf16, 2)) return LOKA_ERR_ALIGN;
     return combine_launch(desc, y_bf16, slot, weight, residual_bf16, out_bf16, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -746,7 +746,7 @@ loka_status loka_combine_backward(const loka_combine_desc* desc, const void* dou
     if (!desc || !dout_bf16 || !slot || (!dy_bf16 && !dweight) || (dweight && !y_bf16)) return LOKA_ERR_NULL;
     const loka_status st = validate_combine(desc);
     if (st != LOKA_OK) return st;
-    if (!aligned16(dout_bf16) || !aligned16(y_bf16) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned16(dy_bf16) || !aligned_to(dweight, 4))
+    if (!aligned_to(dout_bf16, 2) || !aligned_to(y_bf16, 2) || !aligned_to(slot, 4) || !aligned_to(weight, 4) || !aligned_to(dy_bf16, 2) || !aligned_to(dweight, 4))
         return LOKA_ERR_ALIGN;
     return combine_backward_launch(desc, dout_bf16, y_bf16, slot, weight, dy_bf16, dweight, static_cast<hipStream_t>(hip_stream));
 }

@@ -37,3 +37,22 @@ def test_a_buffer_that_is_given_is_written():
         r = B.loka_grouped_quantize(x, along=False, turned=False, **{name: one})
         assert getattr(r, name).data_ptr() == one.data_ptr() and torch.equal(one, getattr(want, name))
         assert [t is None for t in r] == ([False, False, True, True] if name in ("q", "scales") else [True, True, False, False])
+
+
+@pytest.mark.parametrize("T,k,C", [(40, 3, 7), (33, 8, 257), (5, 2, 1001), (3, 4, 4095), (8200, 4, 4099)])
+def test_combination_of_matrices_that_start_anywhere(T, k, C):
+    """Rows from the second on of matrices of odd width, which no 16 bytes divide, against the same rows at aligned places."""
+    rows = T * k
+    y, res, dout = (_randn(n + 1, C, seed=i).bfloat16()[1:] for i, n in enumerate((rows, T, T)))
+    slots = torch.randperm(rows, device=DEV, generator=_gen(3)).view(T, k).int()
+    w = _randn(T, k, seed=4)
+    apart = [t.clone() for t in (y, res, dout)]
+    assert all(a.data_ptr() % 16 == 0 and t.data_ptr() % 16 for a, t in zip(apart, (y, res, dout)))
+    want = B.loka_combine(apart[0], slots, w, apart[1])
+    out = torch.full((T + 2, C), -7.0, dtype=torch.bfloat16, device=DEV)
+    assert torch.equal(B.loka_combine(y, slots, w, res, out=out[1:T + 1]), want) and bool((out[0] == -7).all()) and bool((out[T + 1] == -7).all())
+    dy0, dw0 = B.loka_combine_backward(apart[2], apart[0], slots, w)
+    dy = torch.full((rows + 2, C), -7.0, dtype=torch.bfloat16, device=DEV)
+    _, dw = B.loka_combine_backward(dout, y, slots, w, dy=dy[1:rows + 1])
+    assert torch.equal(dy[1:rows + 1], dy0) and torch.equal(dw, dw0) and bool((dy[0] == -7).all()) and bool((dy[rows + 1] == -7).all())
+    assert torch.equal(B.loka_combine(y, slots, w, res, out=res), want)             # over the residual
