@@ -22,7 +22,9 @@ __device__ __forceinline__ int64_t gq_source(const GqArgs& a, int64_t p) {
 }
 
 // Sources of 2^27 elements and more pass the last-level cache (256 MB) by, which cannot hold them (32768 x 4096: 61.5 us, else 72.0, both forms 90.5 and 105;
-// 16384 x 4096: 33.4 and 30.3, both forms 49.5 and 48.5).
+// 16384 x 4096: 33.4 and 30.3, both forms 49.5 and 48.5).  What counts is the source that is read, not the rows made of it: gathered rows come back to it
+// (through the cache and past it, along / turned / both: 16384 x 1024, each row 8 times, 59.7 / 46.0 / 78.8 and 67.2 / 65.8 / 95.4; 16384 x 4096, 8 times, 220 / 227 / 431
+// and 284 / 298 / 426; 24000 x 4096, 4 times, 176 / 176 / 283 and 212 / 211 / 305; both forms of 16384 x 4096, twice, are the exception: 109 and 95).
 template <bool STREAMED>
 __device__ __forceinline__ u32x4 gq_load8(const uint16_t* p) {
     if (STREAMED) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
@@ -204,7 +206,7 @@ loka_status grouped_quantize_launch(const loka_grouped_quantize_desc* d, const v
     a.col_tiles = static_cast<int>(group_blocks(d->cols));
     a.per_group = d->rows / d->groups;
     a.blocks_per_group = group_blocks(a.per_group);
-    const bool streamed = a.rows * a.cols >= INT64_C(1) << 27;
+    const bool streamed = (index && a.x_rows < a.rows ? a.x_rows : a.rows) * a.cols >= INT64_C(1) << 27;
     if (!qt) {
         // (blocks a thread: 4 in flight where there are many: 16384 x 1024 8.9 us, with 1 10.3; 1 where 4 leave CUs idle: 1024 x 1024 2.4 us, with 4 3.2)
         const int64_t units = d->rows * a.col_tiles;

@@ -17,3 +17,11 @@ def test_a_function_attribute_does_not_depend_on_the_call():
     assert len(values) == 4, values    # both tiles, forward and weight gradient
     for (kernel, _), v in values.items():
         assert len(v) == 1 and max(v) >= most[kernel], (kernel, v, most[kernel])
+
+
+def test_rows_that_are_read_again_are_not_read_past_the_cache():
+    """The quantization passes the last-level cache by where the source is larger, not where a small source is gathered many times over."""
+    sizes = [(131072, 1024, 64, 0), (131072, 1024, 64, 16384), (131072, 1024, 64, 131072), (131072, 1024, 64, 1 << 20), (131071, 1024, 64, 1 << 20), (131072, 1021, 64, 0)]
+    for along, turned in ((1, 0), (0, 1), (1, 1)):
+        past = [r["launches"][0][0].split("<")[1].rstrip(">").split(", ")[-1] for r in launch_log.record([["quantize", *s, along, turned] for s in sizes])]
+        assert past == ["true", "false", "true", "true", "false", "false"], (along, turned)

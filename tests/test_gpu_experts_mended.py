@@ -56,3 +56,24 @@ def test_combination_of_matrices_that_start_anywhere(T, k, C):
     _, dw = B.loka_combine_backward(dout, y, slots, w, dy=dy[1:rows + 1])
     assert torch.equal(dy[1:rows + 1], dy0) and torch.equal(dw, dw0) and bool((dy[0] == -7).all()) and bool((dy[rows + 1] == -7).all())
     assert torch.equal(B.loka_combine(y, slots, w, res, out=res), want)             # over the residual
+
+
+@pytest.mark.parametrize("T", [16384, 140000])
+def test_quantize_many_gathered_rows(T):
+    """2^27 elements and more of a source that the cache holds, and of one that it does not: both read the same rows."""
+    C, rows = 1024, 140000
+    x = torch.randn(T, C, device=DEV, generator=_gen(T), dtype=torch.bfloat16)
+    index = torch.randint(0, T, (rows,), device=DEV, generator=_gen(1)).int()
+    bounds = [0, 70001, 70001, rows]
+    r = B.loka_grouped_quantize(x, offsets=_i32(bounds), index=index, turned=True)
+    alone = B.loka_grouped_quantize(x, offsets=_i32(bounds), index=index)
+    only = B.loka_grouped_quantize(x, offsets=_i32(bounds), index=index, along=False, turned=True)
+    used = 547 + 547                    # blocks of 70001 and 69999 rows
+    assert torch.equal(alone.q, r.q) and torch.equal(alone.scales, r.scales)
+    assert torch.equal(only.qt[:used], r.qt[:used]) and torch.equal(only.st[:used], r.st[:used])
+    for a, b, block in ((0, 1280, 0), (69888, 70001, 546), (70001, 70001 + 1280, 547), (70001 + 546 * 128, rows, 1093)):
+        v = x[index[a:b].long()]
+        c, f = X.along(v)
+        assert torch.equal(X.e4m3(r.q[a:b]), c) and torch.equal(r.scales[a:b].double(), f)
+        c, f = X.turned(v, [0, b - a])
+        assert torch.equal(X.e4m3(r.qt[block:block + len(c)]), c) and torch.equal(r.st[block:block + len(c)].double(), f)
