@@ -66,6 +66,19 @@ def order(experts, E):
     return slots.to(**i32), torch.tensor(rows, **i32), torch.tensor(offsets, **i32)
 
 
+def order_of_many(experts, E):
+    """The same by sorting, for many tokens."""
+    T, k = experts.shape
+    flat = torch.where(experts < 0, E, experts).reshape(-1)
+    place = torch.sort(flat, stable=True).indices              # (tokens, and a token's choices, stay in their order)
+    counts = torch.bincount(flat, minlength=E + 1)[:E]
+    n = int(counts.sum())
+    slots, rows = torch.full_like(flat, -1), torch.full_like(flat, -1)
+    slots[place[:n]] = torch.arange(n, device=flat.device)
+    rows[:n] = place[:n] // k
+    return slots.view(T, k).int(), rows.int(), torch.cat([counts.new_zeros(1), counts.cumsum(0)]).int()
+
+
 # ---- stored forms
 
 def _codes(v):

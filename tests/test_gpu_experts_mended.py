@@ -1,8 +1,12 @@
 """A layer of experts: calls that are documented and were once answered wrongly or refused, or took a form that no test reached."""
+import math
+
 import pytest
 import torch
 
 import plain_experts as X
+import plain_ops as P
+import test_gpu_experts as G
 from paper_2605_10886_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -77,3 +81,53 @@ def test_quantize_many_gathered_rows(T):
         assert torch.equal(X.e4m3(r.q[a:b]), c) and torch.equal(r.scales[a:b].double(), f)
         c, f = X.turned(v, [0, b - a])
         assert torch.equal(X.e4m3(r.qt[block:block + len(c)]), c) and torch.equal(r.st[block:block + len(c)].double(), f)
+
+
+# (tokens, experts, choices, score, renorm, bf16): chunks of 16 to 128 tokens, below and above the number from which their counts have a launch of their own,
+# with every number of lanes a token; test_experts_launches.py holds them to that
+@pytest.mark.parametrize("T,E,k,score,renorm,bf16", [
+    (1000, 1024, 16, "sigmoid", True, False), (2000, 200, 3, "softmax", False, True), (4097, 64, 2, "softmax", True, True), (8192, 300, 3, "sigmoid", False, False),
+    (8193, 100, 9, "softmax", True, False), (16384, 1000, 2, "softmax", False, True), (16385, 256, 8, "sigmoid", True, True), (32768, 256, 8, "softmax", True, True),
+    (32700, 33, 5, "sigmoid", False, False), (32769, 1024, 4, "sigmoid", True, False), (40000, 512, 6, "softmax", False, True), (33000, 160, 16, "sigmoid", False, False),
+    (50001, 128, 1, "softmax", True, True), (66000, 7, 7, "sigmoid", True, True)])
+def test_route_sizes(T, E, k, score, renorm, bf16):
+    x = 1.5 * _randn(T, E, seed=T)
+    x[:, E // 3] += 3.0                 # an expert that most tokens take
+    x[torch.rand(T, E, device=DEV, generator=_gen(1)) < 0.3] = -math.inf
+    x[5:9] = -math.inf                  # tokens that choose nothing
+    x = x.bfloat16() if bf16 else x
+    r = B.loka_route(x, k, G.SCORES[score], renorm, 2.5)
+    e = X.choose(x, k)
+    assert torch.equal(r.experts.long(), e)
+    slots, rows, offsets = X.order_of_many(e, E)
+    assert torch.equal(r.slots, slots) and torch.equal(r.rows, rows) and torch.equal(r.offsets, offsets)
+    # counted as in test_gpu_experts._check_route
+    w = torch.where(e >= 0, X.weights(x, e, score, renorm, 2.5), 0.0)
+    span = float(torch.where(x.isfinite(), x.double(), 0.0).abs().max())
+    assert bool(((r.weights.double() - w).abs() <= (2 * (2 * span + 4) + 24 + 6) * P.F32 * w + 2.0 ** -126).all())
+    # the gradient: the formulas in 64 bits
+    g = _randn(T, k, seed=2)
+    got = B.loka_route_backward(x, r.experts, g, G.SCORES[score], renorm, 2.5)
+    live = e >= 0
+    gd, at = torch.where(live, 2.5 * g.double(), 0.0), e.clamp_min(0)
+    q = w / 2.5
+    sig = torch.sigmoid(x.double().gather(1, at))
+    want = torch.zeros(T, E, dtype=torch.float64, device=DEV)
+    inner = (gd * q).sum(1, keepdim=True)
+    if score == "softmax" and not renorm:
+        want = -torch.nan_to_num(torch.softmax(x.double(), 1)) * inner
+        d = gd * q
+    elif renorm:
+        d = q * (gd - inner) * (1 - sig if score == "sigmoid" else 1.0)
+    else:
+        d = gd * sig * (1 - sig)
+    want.scatter_add_(1, at, torch.where(live, d, 0.0))
+    # counted as in test_gpu_experts.test_route_backward, of logits up to `span`
+    tol = (2 * (2 * span + 4) + 24 + 16 + 8) * P.F32 * 2.5 * float(g.abs().max()) * 2
+    assert bool(((got.double() - want).abs() <= tol + (G.BF * want.abs() if bf16 else 0.0)).all()) and not bool(got[5:9].any())
+
+
+@pytest.mark.parametrize("sizes", [[200 + (i * 37) % 11 * 40 for i in range(100)]])
+def test_weight_gradients_of_many_groups(sizes):
+    """More than 64 groups in large tiles."""
+    G.test_weight_gradients_are_exact_on_whole_numbers(sizes, 1008, 720)
