@@ -35,7 +35,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-cont
 # matrix instructions (which it takes for freely movable) out of their slots to the end of the loop body, behind
 # every LDS read, and the accumulators spill.  The pass is switched off for that file (its other kernels come out
 # the same, instruction for instruction, apart from a few address computations).  mxfp4_gemm.hip: the same pass moves the first
-# half of a K tile's matrix instructions behind the barrier that the second half's operands wait for.
+# half of a K tile's matrix instructions behind the barrier that the second half's operands wait for.  grouped_gemm.hip: with the pass the large tile's
+# kernels take all 256 registers and spill (without it 253 and 245, no spill).
 EXTRA_FLAGS = {"gemm_panel32.hip": ["-mllvm", "-disable-machine-sink"], "mxfp4_gemm.hip": ["-mllvm", "-disable-machine-sink"],
                "grouped_gemm.hip": ["-mllvm", "-disable-machine-sink"]}
 

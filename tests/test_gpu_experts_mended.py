@@ -131,3 +131,21 @@ def test_route_sizes(T, E, k, score, renorm, bf16):
 def test_weight_gradients_of_many_groups(sizes):
     """More than 64 groups in large tiles."""
     G.test_weight_gradients_are_exact_on_whole_numbers(sizes, 1008, 720)
+
+
+@pytest.mark.parametrize("sizes,K,N", G.FORMS[:-1] + [([1], 4096, 1000), ([3, 0, 5], 513, 40)])
+def test_the_linear_is_the_quantization_and_the_product(sizes, K, N):
+    """The same bits, in every form of the product."""
+    n, E = sum(sizes), len(sizes)
+    off = _i32([0] + torch.tensor(sizes).cumsum(0).tolist())
+    x, w = _randn(max(5, n // 2), K, seed=K).bfloat16(), (_randn(E * K, N, seed=N) / math.sqrt(K)).bfloat16()
+    x[:, ::17] *= 20.0
+    index = torch.randint(0, len(x), (n,), device=DEV, generator=_gen(n)).int()
+    wq = B.loka_grouped_quantize(w, groups=E, along=False, turned=True)
+    d = B.make_grouped_desc(n, N, K, E)
+    out, y = B.loka_grouped_linear(d, x, wq.qt, wq.st, off, index=index, want_y=True)
+    xq = B.loka_grouped_quantize(x)
+    o2, y2 = B.loka_grouped_gemm(d, xq.q, xq.scales, wq.qt, wq.st, off, index=index, want_y=True)
+    xg = x[index.long()]
+    o3, y3 = B.loka_grouped_linear(d, xg, wq.qt, wq.st, off, want_y=True)
+    assert torch.equal(y, y2) and torch.equal(out, o2) and torch.equal(y, y3) and torch.equal(out, o3) and torch.equal(out, y.bfloat16())
