@@ -541,7 +541,7 @@ loka_status route_backward_launch(const loka_route_desc* d, const void* logits, 
 // ---------------------------------------------------------------------------------
 // The sum of a token's results, and its gradients.  A lane takes 8 columns of a token; bytes only, so a token's rows (K of them at
 // most) are all requested before the first is used.  Tokens of more than 256 columns: a wave takes 512 of them, and its token's slots and weights are
-// scalars; narrower ones share a wave, 2^lg lanes each.  16384 tokens x 4 choices x 4096: 133 us (805 MB, 6.0 TB/s), backward 237 (1.2 GB, 5.1 TB/s).
+// scalars; narrower ones share a wave, 2^lg lanes each.  16384 tokens x 4 choices x 4096: 135 .. 138 us (805 MB, 5.9 TB/s), backward 233 .. 239 (1.2 GB, 5.1 TB/s).
 struct CombineArgs {
     const uint16_t *y, *residual, *dout;
     const int32_t* slot;
